@@ -1,0 +1,361 @@
+"""Timed cases of the policy layer's token-wise operators: what a training program runs on the packed
+prefix tokens before the LM-head loss, and a rollout on single tokens.
+
+Operators
+  qk     norms of queries and keys for each head with the position rotation, forward or backward
+  drop   dropout from the counter-based generator with the residual sum, forward or backward
+  ffn    the gated feed-forward block, forward, or forward and backward ("train")
+
+Widths, token counts and completion counts are those of the repository's own workloads (d = 1536 and
+3584; 113,926 kept tokens in the 7B-shaped batch) or generic ones.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # one decoding step of 8 completions: latency
+        dict(name="qk_decode", op="qk", way="fwd", N=8, seqs=0, Hq=28, Hk=4, D=128, rot=128, inter=False, type="bf16"),
+        # an update batch of the 7B-shaped policy, heads inside the fused projection's rows
+        dict(name="qk_fwd_batch", op="qk", way="fwd", N=28481, seqs=64, Hq=28, Hk=4, D=128, rot=128, inter=False,
+             type="bf16"),
+        # its backward, with the gradients of the norms' weights
+        dict(name="qk_bwd_batch", op="qk", way="bwd", N=28481, seqs=64, Hq=28, Hk=4, D=128, rot=128, inter=False,
+             type="bf16"),
+        # odd head width, part of it rotated in neighbouring pairs, one key head, float32
+        dict(name="qk_bwd_f32", op="qk", way="bwd", N=1501, seqs=7, Hq=12, Hk=1, D=80, rot=32, inter=True, type="f32"),
+        # a short micro-batch, float32
+        dict(name="drop_short", op="drop", way="fwd", N=129, d=1536, p=0.1, rows=False, res=True, type="f32", to="f32"),
+        # the kept tokens of the 7B-shaped batch, masks by source row
+        dict(name="drop_fwd_7b", op="drop", way="fwd", N=113926, d=3584, p=0.1, rows=True, res=True, type="bf16",
+             to="bf16"),
+        # the backward behind the loss call's float32 gradient of the hidden rows
+        dict(name="drop_bwd_batch", op="drop", way="bwd", N=41003, d=3584, p=0.05, rows=True, res=False, type="f32",
+             to="bf16"),
+        # one token of one completion: bound by the weights' bytes
+        dict(name="ffn_token", op="ffn", way="fwd", N=1, d=3584, f=14336, act="silu"),
+        # one decoding step of 64 completions
+        dict(name="ffn_decode", op="ffn", way="fwd", N=64, d=1536, f=6144, act="gelu_tanh"),
+        # old-policy forward over one prompt's completions
+        dict(name="ffn_fwd", op="ffn", way="fwd", N=5003, d=3584, f=14336, act="silu"),
+        # a micro-batch of the 1.5B-shaped policy, ragged everywhere
+        dict(name="ffn_train_short", op="ffn", way="train", N=777, d=1000, f=4104, act="silu"),
+        # a training batch of the 7B-shaped policy: the largest
+        dict(name="ffn_train", op="ffn", way="train", N=8192, d=3584, f=14336, act="silu"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["qk", "drop", "ffn", "ffn"])
+    if op == "qk":
+        Hk = rng.choice([1, 2, 4, 8])
+        Hq = Hk * rng.choice([1, 2, 4, 7])
+        D = rng.choice([32, 64, 72, 80, 96, 128, 192, 256])
+        rot = rng.choice([D // 16 * 16, D // 2 // 16 * 16, 16])
+        most = int(1.1e8 / ((Hq + Hk) * D))
+        N = min(_log_int(rng, 1, 60000), most)
+        return dict(op="qk", way=rng.choice(["fwd", "bwd"]), N=N, seqs=0 if N < 9 else rng.choice([0, 1, 5, 64]),
+                    Hq=Hq, Hk=Hk, D=D, rot=max(16, rot), inter=rng.random() < 0.3,
+                    type=rng.choice(["bf16", "bf16", "f32"]))
+    if op == "drop":
+        d = 8 * _log_int(rng, 1, 1024)
+        N = min(_log_int(rng, 1, 113926), int(4e8 / d))
+        way = rng.choice(["fwd", "bwd"])
+        t = rng.choice(["bf16", "f32"])
+        return dict(op="drop", way=way, N=N, d=d, p=rng.choice([0.0, 0.05, 0.1, 0.25, 0.5]), rows=rng.random() < 0.6,
+                    res=way == "fwd" and rng.random() < 0.7, type=t,
+                    to=t if way == "fwd" else rng.choice(["bf16", "f32"]))
+    d, f = 8 * _log_int(rng, 8, 512), 8 * _log_int(rng, 16, 1792)
+    way = rng.choice(["fwd", "fwd", "train"])
+    N = min(_log_int(rng, 1, 12000), int(7e12 / (18.0 * d * f)))
+    return dict(op="ffn", way=way, N=max(1, N), d=d, f=f, act=rng.choice(["silu", "silu", "gelu_tanh"]))
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+
+def _normal(g, shape, std, dtype):
+    return (torch.randn(shape, device=DEV, generator=g) * std).to(dtype)
+
+
+def _prepare_qk(case, seed, g):
+    N, Hq, Hk, D = case["N"], case["Hq"], case["Hk"], case["D"]
+    dt = DTYPES[case["type"]]
+    rng = np.random.default_rng(seed)
+    # the fused projection's rows: queries, keys, values
+    qkv = _normal(g, (N, (Hq + 2 * Hk) * D), 1.0, torch.float32)
+    qkv = (qkv * torch.exp(0.5 * torch.randn(qkv.shape[1], device=DEV, generator=g))).to(dt)
+    s = dict(q=qkv[:, :Hq * D].view(N, Hq, D), k=qkv[:, Hq * D:(Hq + Hk) * D].view(N, Hk, D),
+             qw=(1 + _normal(g, (D,), 0.2, torch.float32)).to(dt), kw=(1 + _normal(g, (D,), 0.2, torch.float32)).to(dt),
+             inv=torch.from_numpy((10000.0 ** (-np.arange(case["rot"] // 2) * 2.0 / case["rot"])).astype(np.float32))
+             .to(DEV))
+    if case["seqs"]:
+        R = min(case["seqs"], N)
+        cut = np.sort(rng.integers(0, N + 1, R - 1))
+        cu = np.concatenate([[0], cut, [N]]).astype(np.int32)
+        s["seq"] = torch.from_numpy(np.repeat(np.arange(R), np.diff(cu)).astype(np.int32)).to(DEV)
+        s["cu"] = torch.from_numpy(cu).to(DEV)
+        s["first"] = torch.from_numpy(rng.integers(0, 2000, R).astype(np.int32)).to(DEV)
+    else:
+        s["pos"] = torch.from_numpy(rng.integers(0, 131072, N).astype(np.int32)).to(DEV)
+    if case["way"] == "bwd":
+        s["dq"] = _normal(g, (N, Hq, D), 0.01, dt)
+        s["dk"] = _normal(g, (N, Hk, D), 0.02, dt)
+    return s
+
+
+def _prepare_drop(case, seed, g):
+    N, d = case["N"], case["d"]
+    s = dict(x=_normal(g, (N, d), 1.0 if case["way"] == "fwd" else 1e-3, DTYPES[case["type"]]),
+             seed=(int(seed) * 0x9E3779B97F4A7C15 + 1) & (2 ** 64 - 1), offset=int(seed) & 0xFFFF)
+    if case["res"]:
+        s["res"] = _normal(g, (N, d), 2.0, DTYPES[case["type"]])
+    if case["rows"]:   # source rows of a packed batch: increasing, with gaps
+        gaps = torch.randint(1, 3, (N,), device=DEV, generator=g, dtype=torch.int64)
+        s["rows"] = (torch.cumsum(gaps, 0) - 1).to(torch.int32)
+    return s
+
+
+def _prepare_ffn(case, seed, g):
+    N, d, f = case["N"], case["d"], case["f"]
+    b = torch.bfloat16
+    x = _normal(g, (N, d), 1.0, torch.float32) * torch.exp(0.3 * torch.randn(d, device=DEV, generator=g))
+    s = dict(x=x.to(b), wg=_normal(g, (f, d), 1 / math.sqrt(d), b), wu=_normal(g, (f, d), 1 / math.sqrt(d), b),
+             wd=_normal(g, (d, f), 1 / math.sqrt(f), b))
+    if case["way"] == "train":
+        s["dy"] = _normal(g, (N, d), 1e-3, b)
+    return s
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(int(seed))
+    s = dict(qk=_prepare_qk, drop=_prepare_drop, ffn=_prepare_ffn)[case["op"]](case, seed, g)
+    s["case"] = dict(case)
+    return s
+
+
+# ---------------------------------------------------------------------------
+# the framework's calls
+# ---------------------------------------------------------------------------
+
+def _own(s):
+    from paper_2606_29758_amd import pspo
+    c = s["case"]
+    N = c["N"]
+    if c["op"] == "qk":
+        at = dict(positions=s.get("pos"), seq_id=s.get("seq"), cu_seqlens=s.get("cu"), first_pos=s.get("first"))
+        if c["way"] == "fwd":
+            o = pspo.qk_norm_rope(s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6, interleaved=c["inter"], **at)
+            return [o["q"], o["k"]]
+        o = pspo.qk_norm_rope_bwd(s["dq"], s["dk"], s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6,
+                                  interleaved=c["inter"], **at)
+        return [o["dq"], o["dk"], o["dq_weight"], o["dk_weight"]]
+    if c["op"] == "drop":
+        if c["way"] == "fwd":
+            return pspo.dropout_add(s["x"], N, c["p"], s["seed"], s["offset"], residual=s.get("res"),
+                                    row_ids=s.get("rows"))
+        return pspo.dropout_bwd(s["x"], N, c["p"], s["seed"], s["offset"], row_ids=s.get("rows"),
+                                out_dtype=DTYPES[c["to"]])
+    o = pspo.gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], keep=c["way"] == "train")
+    if c["way"] == "fwd":
+        return o["y"]
+    r = pspo.gated_ffn_bwd(s["dy"], s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], preact=o["preact"])
+    return [o["y"], r["dx"], r["dw_gate"], r["dw_up"], r["dw_down"]]
+
+
+# ---------------------------------------------------------------------------
+# the plain form
+# ---------------------------------------------------------------------------
+
+def _positions(s):
+    if "pos" in s:
+        return s["pos"].long()
+    seq = s["seq"].long()
+    return s["first"].long()[seq] + torch.arange(seq.shape[0], device=seq.device) - s["cu"].long()[seq]
+
+
+def _turn(z, cos, sin, rot, inter):
+    """The first `rot` of the last axis turned by the angles; pairs (i, i + rot / 2) or (2 i, 2 i + 1)."""
+    a, b = (z[..., :rot:2], z[..., 1:rot:2]) if inter else (z[..., :rot // 2], z[..., rot // 2:rot])
+    x, y = a * cos - b * sin, a * sin + b * cos
+    turned = torch.stack([x, y], -1).flatten(-2) if inter else torch.cat([x, y], -1)
+    return torch.cat([turned, z[..., rot:]], -1)
+
+
+def _plain_qk(s, c):
+    ang = _positions(s).double()[:, None] * s["inv"].double()[None]
+    cos, sin = torch.cos(ang).float()[:, None], torch.sin(ang).float()[:, None]
+    out, dws = [], []
+    for x, w, do in ((s["q"], s["qw"], s.get("dq")), (s["k"], s["kw"], s.get("dk"))):
+        x32, w32 = x.float(), w.float()
+        xhat = x32 * torch.rsqrt((x32 * x32).mean(-1, keepdim=True) + 1e-6)
+        if do is None:
+            out.append(_turn(xhat * w32, cos, sin, c["rot"], c["inter"]).to(x.dtype))
+            continue
+        dz = _turn(do.float(), cos, -sin, c["rot"], c["inter"])
+        dws.append((dz * xhat).sum((0, 1)))
+        dz = dz * w32
+        rstd = torch.rsqrt((x32 * x32).mean(-1, keepdim=True) + 1e-6)
+        out.append((rstd * (dz - xhat * (dz * xhat).mean(-1, keepdim=True))).to(x.dtype))
+    return out + dws
+
+
+def _philox(c0, c1, c2, c3, seed):
+    """Philox4x32-10: the four output words of each counter, as int64 in [0, 2^32)."""
+    M = 0xFFFFFFFF
+    k0, k1 = seed & M, seed >> 32
+    for _ in range(10):
+        p0, p1 = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = ((p1 >> 32) & M) ^ c1 ^ k0, p1 & M, ((p0 >> 32) & M) ^ c3 ^ k1, p0 & M
+        k0, k1 = (k0 + 0x9E3779B9) & M, (k1 + 0xBB67AE85) & M
+    return c0, c1, c2, c3
+
+
+def _kept(s, c):
+    """The mask [N, d]: 16 bits of the generator per element, eight elements of a row per counter."""
+    N, d = c["N"], c["d"]
+    T = min(max(int(math.floor((1.0 - c["p"]) * 65536.0 + 0.5)), 1), 65536)
+    rows = s["rows"].long() if c["rows"] else torch.arange(N, device=DEV)
+    at = torch.arange(d // 8, device=DEV)
+    c0 = rows[:, None].expand(N, d // 8).contiguous()
+    c1 = (at + 1)[None].expand(N, d // 8).contiguous()
+    off = torch.full_like(c0, s["offset"] & 0xFFFFFFFF)
+    words = _philox(c0, c1, off, torch.full_like(c0, s["offset"] >> 32), s["seed"])
+    lanes = [h for w in words for h in (w & 0xFFFF, w >> 16)]
+    return torch.stack([(h < T) for h in lanes], -1).reshape(N, d), 65536.0 / T
+
+
+def _plain_drop(s, c):
+    kept, scale = _kept(s, c)
+    scale = float(np.float32(scale))
+    y = torch.where(kept, s["x"].float() * scale, 0.0)
+    if c["res"]:
+        y = s["res"].float() + y
+    return y.to(DTYPES[c["to"]])
+
+
+def _act(g, kind):
+    """act(g) and its derivative."""
+    if kind == "silu":
+        sg = 1 / (1 + torch.exp(-g))
+        return g * sg, sg + g * sg * (1 - sg)
+    a = math.sqrt(2 / math.pi)
+    t = torch.tanh(a * (g + 0.044715 * g ** 3))
+    return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * a * (1 + 3 * 0.044715 * g * g)
+
+
+def _plain_ffn(s, c):
+    x, wg, wu, wd = (s[k].float() for k in ("x", "wg", "wu", "wd"))
+    g, u = x @ wg.t(), x @ wu.t()
+    a, da = _act(g, c["act"])
+    y = ((a * u) @ wd.t()).to(torch.bfloat16)
+    if c["way"] == "fwd":
+        return y
+    dy = s["dy"].float()
+    dh = dy @ wd
+    dg, du = dh * u * da, dh * a
+    outs = [dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dy.t() @ (a * u)]
+    return [y] + [o.to(torch.bfloat16) for o in outs]
+
+
+def run(state):
+    if own:
+        return _own(state)
+    c = state["case"]
+    return dict(qk=_plain_qk, drop=_plain_drop, ffn=_plain_ffn)[c["op"]](state, c)
+
+
+# ---------------------------------------------------------------------------
+# work, and the definition in 64 bits
+# ---------------------------------------------------------------------------
+
+def work(case):
+    c = case
+    N = c["N"]
+    if c["op"] == "qk":
+        b = 2 if c["type"] == "bf16" else 4
+        n = N * (c["Hq"] + c["Hk"]) * c["D"]
+        return dict(bytes=n * b * (2 if c["way"] == "fwd" else 3) + 4 * N * (2 if c["seqs"] else 1),
+                    flops=n * (8 if c["way"] == "fwd" else 14))
+    if c["op"] == "drop":
+        b, t = (2 if c["type"] == "bf16" else 4), (2 if c["to"] == "bf16" else 4)
+        return dict(bytes=N * c["d"] * (b + t + (b if c["res"] else 0)) + (4 * N if c["rows"] else 0),
+                    flops=N * c["d"] * 2)
+    d, f = c["d"], c["f"]
+    if c["way"] == "fwd":
+        return dict(bytes=2 * (3 * d * f + 2 * N * d), flops=6.0 * N * d * f)
+    return dict(bytes=2 * (6 * d * f + 4 * N * d), flops=18.0 * N * d * f)
+
+
+def _exact_qk(s, c):
+    """By complex numbers and autograd in 64 bits."""
+    pos = _positions(s).double()
+    turn = torch.polar(torch.ones((), dtype=torch.float64, device=DEV), pos[:, None] * s["inv"].double()[None])[:, None]
+    rot, half = c["rot"], c["rot"] // 2
+
+    def form(x, w):
+        z = w * x / torch.sqrt((x ** 2).sum(-1, keepdim=True) / c["D"] + 1e-6)
+        head = z[..., :rot].unflatten(-1, (half, 2) if c["inter"] else (2, half))
+        pair = torch.view_as_complex((head if c["inter"] else head.transpose(-1, -2)).contiguous()) * turn
+        r = torch.view_as_real(pair)
+        return torch.cat([(r if c["inter"] else r.transpose(-1, -2)).flatten(-2), z[..., rot:]], -1)
+
+    if c["way"] == "fwd":
+        return [form(s["q"].double(), s["qw"].double()), form(s["k"].double(), s["kw"].double())]
+    res = []
+    for x, w, do in ((s["q"], s["qw"], s["dq"]), (s["k"], s["kw"], s["dk"])):
+        x, w = x.double().requires_grad_(), w.double().requires_grad_()
+        res.append(torch.autograd.grad(form(x, w), (x, w), do.double()))
+    return [res[0][0], res[1][0], res[0][1], res[1][1]]
+
+
+def _exact_drop(s, c):
+    """Rows one block at a time, the generator on unsigned 64-bit integers of the host."""
+    N, d = c["N"], c["d"]
+    if N * d > 1e8:
+        return None
+    T = min(max(int(math.floor((1.0 - c["p"]) * 65536.0 + 0.5)), 1), 65536)
+    rows = s["rows"].cpu().numpy().astype(np.uint64) if c["rows"] else np.arange(N, dtype=np.uint64)
+    u = np.uint64
+    ctr = np.zeros((4, N, d // 8), dtype=np.uint64)
+    ctr[0], ctr[1] = rows[:, None], np.arange(1, d // 8 + 1, dtype=np.uint64)[None]
+    ctr[2], ctr[3] = s["offset"] & 0xFFFFFFFF, s["offset"] >> 32
+    key = [s["seed"] & 0xFFFFFFFF, s["seed"] >> 32]
+    for _ in range(10):
+        lo, hi = ctr[0] * u(0xD2511F53), ctr[2] * u(0xCD9E8D57)
+        ctr = np.stack([(hi >> u(32)) ^ ctr[1] ^ u(key[0]), hi & u(0xFFFFFFFF),
+                        (lo >> u(32)) ^ ctr[3] ^ u(key[1]), lo & u(0xFFFFFFFF)])
+        key = [(key[0] + 0x9E3779B9) % 2 ** 32, (key[1] + 0xBB67AE85) % 2 ** 32]
+    bits = np.ascontiguousarray(np.moveaxis(ctr.astype("<u4"), 0, -1)).view("<u2").reshape(N, d)
+    y = np.where(bits < T, s["x"].double().cpu().numpy() * (65536.0 / T), 0.0)
+    if c["res"]:
+        y = y + s["res"].double().cpu().numpy()
+    return y
+
+
+def _exact_ffn(s, c):
+    x, wg, wu, wd = (s[k].double().requires_grad_(c["way"] == "train") for k in ("x", "wg", "wu", "wd"))
+    g = torch.nn.functional.linear(x, wg)
+    a = torch.nn.functional.silu(g) if c["act"] == "silu" else torch.nn.functional.gelu(g, approximate="tanh")
+    y = torch.nn.functional.linear(a * torch.nn.functional.linear(x, wu), wd)
+    if c["way"] == "fwd":
+        return y
+    return [y.detach()] + list(torch.autograd.grad(y, (x, wg, wu, wd), s["dy"].double()))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return dict(qk=_exact_qk, drop=_exact_drop, ffn=_exact_ffn)[case["op"]](s, case)
