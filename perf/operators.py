@@ -152,27 +152,27 @@ def prepare(case, seed):
 # ---------------------------------------------------------------------------
 
 def _own(s):
-    from paper_2606_29758_amd import pspo
+    from paper_2606_29758_amd import layer
     c = s["case"]
     N = c["N"]
     if c["op"] == "qk":
         at = dict(positions=s.get("pos"), seq_id=s.get("seq"), cu_seqlens=s.get("cu"), first_pos=s.get("first"))
         if c["way"] == "fwd":
-            o = pspo.qk_norm_rope(s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6, interleaved=c["inter"], **at)
+            o = layer.qk_norm_rope(s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6, interleaved=c["inter"], **at)
             return [o["q"], o["k"]]
-        o = pspo.qk_norm_rope_bwd(s["dq"], s["dk"], s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6,
+        o = layer.qk_norm_rope_bwd(s["dq"], s["dk"], s["q"], s["k"], s["qw"], s["kw"], s["inv"], N, eps=1e-6,
                                   interleaved=c["inter"], **at)
         return [o["dq"], o["dk"], o["dq_weight"], o["dk_weight"]]
     if c["op"] == "drop":
         if c["way"] == "fwd":
-            return pspo.dropout_add(s["x"], N, c["p"], s["seed"], s["offset"], residual=s.get("res"),
+            return layer.dropout_add(s["x"], N, c["p"], s["seed"], s["offset"], residual=s.get("res"),
                                     row_ids=s.get("rows"))
-        return pspo.dropout_bwd(s["x"], N, c["p"], s["seed"], s["offset"], row_ids=s.get("rows"),
+        return layer.dropout_bwd(s["x"], N, c["p"], s["seed"], s["offset"], row_ids=s.get("rows"),
                                 out_dtype=DTYPES[c["to"]])
-    o = pspo.gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], keep=c["way"] == "train")
+    o = layer.gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], keep=c["way"] == "train")
     if c["way"] == "fwd":
         return o["y"]
-    r = pspo.gated_ffn_bwd(s["dy"], s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], preact=o["preact"])
+    r = layer.gated_ffn_bwd(s["dy"], s["x"], s["wg"], s["wu"], s["wd"], N, act=c["act"], preact=o["preact"])
     return [o["y"], r["dx"], r["dw_gate"], r["dw_up"], r["dw_down"]]
 
 
