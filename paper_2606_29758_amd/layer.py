@@ -1,0 +1,301 @@
+"""Python binding of the layer operators of libpspo (include/pspo_layer.h): argument marshalling only.
+
+The token-wise operators of a policy's transformer layers on packed prefix tokens: the norms of
+queries and keys with the position rotation, dropout with the residual sum, and the gated
+feed-forward block, each with its gradient.  As in ``pspo``: every step runs in the HIP kernels of
+libpspo.so on the current stream, tensors must be on the current device, a missing library raises.
+All calls take the first N rows of their per-token tensors and leave the rows behind them (of given
+outputs) as they were.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import pspo
+from .pspo import _check, _dev, _ptr, _stream
+
+TYPE_BF16, TYPE_F32 = 0, 1
+ROPE_INTERLEAVED, QK_NO_NORM = 1, 2
+
+_P = ctypes.c_void_p
+_I32, _I64, _U32, _U64, _F32, _F64, _SZ = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64,
+                                           ctypes.c_float, ctypes.c_double, ctypes.c_size_t)
+
+_SIGNATURES = {
+    "pspo_qk_norm_rope_fwd": (ctypes.c_int, [_P, _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32,
+                                             _I32, _I32, _F32, _I32, _U32, _P, _P, _P, _P]),
+    "pspo_qk_norm_rope_workspace_bytes": (_SZ, [_I32, _I32]),
+    "pspo_qk_norm_rope_bwd": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32,
+                                             _I32, _I32, _I32, _F32, _I32, _U32, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "pspo_dropout_add_fwd": (ctypes.c_int, [_P, _P, _P, _I32, _I32, _F64, _U64, _U64, _I32, _P, _P]),
+    "pspo_dropout_bwd": (ctypes.c_int, [_P, _P, _I32, _I32, _F64, _U64, _U64, _I32, _I32, _P, _P]),
+}
+
+_lib = None
+
+
+def load() -> ctypes.CDLL:
+    """libpspo.so with the signatures of the layer operators; raises if it is missing."""
+    global _lib
+    if _lib is None:
+        lib = pspo.load()
+        for name, (res, args) in _SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype = res
+            fn.argtypes = args
+        _lib = lib
+    return _lib
+
+
+def exported_symbols():
+    return list(_SIGNATURES)
+
+
+def _type(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype == torch.bfloat16:
+        return TYPE_BF16
+    if t.dtype == torch.float32:
+        return TYPE_F32
+    raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+
+
+def _rows(t: torch.Tensor, N: int, shape, name: str) -> None:
+    """t must be [>= N, *shape]."""
+    if t.dim() != 1 + len(shape) or tuple(t.shape[1:]) != tuple(shape) or t.shape[0] < N:
+        raise ValueError(f"{name} must be [>= {N}{''.join(', %d' % s for s in shape)}], got {list(t.shape)}")
+
+
+def _exact(t: torch.Tensor, shape, name: str) -> None:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def _apart(out: torch.Tensor, name: str, *ins) -> None:
+    """Outputs must not alias inputs."""
+    if out.numel() == 0:
+        return
+    lo, hi = out.data_ptr(), out.data_ptr() + out.numel() * out.element_size()
+    for t in ins:
+        if t is None or t.numel() == 0:
+            continue
+        last = sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
+        if t.data_ptr() < hi and t.data_ptr() + (last + 1) * t.element_size() > lo:
+            raise ValueError(f"{name} overlaps an input")
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str) -> None:
+    if t is None:
+        return
+    _dev(t, torch.int32, name)
+    if t.dim() != 1 or t.shape[0] < n:
+        raise ValueError(f"{name} must be [>= {n}], got {list(t.shape)}")
+
+
+def _count(N: int) -> int:
+    if N < 0:
+        raise ValueError("N must be >= 0")
+    return int(N)
+
+
+# ---------------------------------------------------------------------------
+# norms of queries and keys with the position rotation
+# ---------------------------------------------------------------------------
+
+def _heads(t: torch.Tensor, N: int, name: str, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """[>= N, heads, D] on the current device, heads contiguous, any row stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a tensor [>= N, heads, head_dim]")
+    if t.shape[0] < N:
+        raise ValueError(f"{name} has fewer than N rows")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, but the calls run on the current device "
+                         f"cuda:{torch.cuda.current_device()}")
+    if like is not None and t.dtype != like.dtype:
+        raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
+    _, H, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"the heads of {name} must be contiguous within a row")
+    return t
+
+
+def _row_stride(t: Optional[torch.Tensor]) -> int:
+    """Elements between rows (a tensor of one row may report any stride)."""
+    if t is None:
+        return 0
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos, interleaved, norm,
+               err_flag):
+    _type(q, "q")
+    _heads(q, N, "q")
+    D = q.shape[2]
+    if k is not None:
+        _heads(k, N, "k", q)
+        if k.shape[2] != D:
+            raise ValueError("q and k disagree on the head dimension")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dev(w, q.dtype, name)
+            _exact(w, (D,), name)
+    rot, R = 0, 0
+    if inv_freq is not None:
+        _dev(inv_freq, torch.float32, "inv_freq")
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq must be [rot_dim / 2]")
+        rot = 2 * inv_freq.shape[0]
+        _ints(positions, N, "positions")
+        if positions is None:
+            if seq_id is None or cu_seqlens is None:
+                raise ValueError("positions, or seq_id and cu_seqlens, must be given")
+            _ints(seq_id, N, "seq_id")
+            _ints(cu_seqlens, 1, "cu_seqlens")
+            R = cu_seqlens.shape[0] - 1
+            _ints(first_pos, R, "first_pos")
+    if err_flag is not None:
+        _dev(err_flag, torch.int32, "err_flag")
+    flags = (ROPE_INTERLEAVED if interleaved else 0) | (0 if norm else QK_NO_NORM)
+    return D, rot, R, flags
+
+
+def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq_id=None, cu_seqlens=None,
+                 first_pos=None, eps: float = 1e-6, interleaved: bool = False, norm: bool = True,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 err_flag: Optional[torch.Tensor] = None) -> dict:
+    """Head norms and position rotation of the first N rows of q [>=N, Hq, D] and k [>=N, Hk, D] (or None).
+
+    bf16 or float32; the rows may be strided (parts of a fused projection), the heads of a row
+    contiguous.  q_weight, k_weight: [D] of the same type or None (ones).  inv_freq: float32
+    [rot / 2] (None: no rotation), the first `rot` entries of a head are turned.  Positions: int32
+    [N], or from the packer's seq_id and cu_seqlens plus each completion's first position.
+    Returns q and k ([N, H, D] contiguous; k None if there is none).
+    """
+    N = _count(N)
+    D, rot, R, flags = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos,
+                                  interleaved, norm, err_flag)
+    outs = []
+    for name, x, o in (("q_out", q, q_out), ("k_out", k, k_out)):
+        if x is None:
+            outs.append(None)
+            continue
+        if o is None:
+            o = torch.empty((N, x.shape[1], D), dtype=x.dtype, device=x.device)
+        else:
+            _rows(o, N, (x.shape[1], D), name)
+            _dev(o, x.dtype, name)
+            _apart(o, name, q, k, q_weight, k_weight)
+        outs.append(o)
+    _check(load().pspo_qk_norm_rope_fwd(
+        _ptr(q), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+        _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos), N, R, q.shape[1],
+        0 if k is None else k.shape[1], D, rot, float(eps), _type(q, "q"), flags, _ptr(outs[0]), _ptr(outs[1]),
+        _ptr(err_flag), _stream()))
+    return dict(q=outs[0][:N], k=None if outs[1] is None else outs[1][:N])
+
+
+def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq_id=None,
+                     cu_seqlens=None, first_pos=None, eps: float = 1e-6, interleaved: bool = False, norm: bool = True,
+                     want_weights: bool = True, workspace: Optional[torch.Tensor] = None,
+                     err_flag: Optional[torch.Tensor] = None) -> dict:
+    """Gradient of qk_norm_rope from its inputs and the gradients of its outputs ([>=N, H, D] contiguous).
+
+    Returns dq, dk ([N, H, D] contiguous, of the inputs' type) and, for the weights that are given
+    (unless want_weights is False), dq_weight and dk_weight (float32 [D]).
+    """
+    N = _count(N)
+    D, rot, R, flags = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos,
+                                  interleaved, norm, err_flag)
+    if (k is None) != (dk_out is None):
+        raise ValueError("k and dk_out must be both given or both None")
+    dx = []
+    for name, x, g in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
+        if x is None:
+            dx.append(None)
+            continue
+        _rows(g, N, (x.shape[1], D), name)
+        _dev(g, x.dtype, name)
+        dx.append(torch.empty((N, x.shape[1], D), dtype=x.dtype, device=x.device))
+    dw = [torch.empty(D, dtype=torch.float32, device=q.device) if w is not None and want_weights else None
+          for w in (q_weight, k_weight)]
+    lib = load()
+    if workspace is None and (dw[0] is not None or dw[1] is not None):
+        need = int(lib.pspo_qk_norm_rope_workspace_bytes(N, D))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    if workspace is not None:
+        _dev(workspace, torch.uint8, "workspace")
+    _check(lib.pspo_qk_norm_rope_bwd(
+        _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight),
+        _ptr(inv_freq), _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos), N, R, q.shape[1],
+        0 if k is None else k.shape[1], D, rot, float(eps), _type(q, "q"), flags, _ptr(dx[0]), _ptr(dx[1]),
+        _ptr(dw[0]), _ptr(dw[1]), _ptr(err_flag), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+        _stream()))
+    return dict(dq=dx[0], dk=dx[1], dq_weight=dw[0], dk_weight=dw[1], workspace=workspace)
+
+
+# ---------------------------------------------------------------------------
+# dropout with the residual sum
+# ---------------------------------------------------------------------------
+
+_U64_MASK = 2 ** 64 - 1
+
+
+def dropout_add(x, N: int, p: float, seed: int, offset: int = 0, residual: Optional[torch.Tensor] = None,
+                row_ids: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + dropout(x) of the first N rows of x [>=N, d] (bf16 or float32); no mask is stored.
+
+    An entry is kept with probability T / 2^16, T = round((1 - p) 2^16), and scaled by its inverse.
+    The mask depends on (seed, offset, column, row_ids[n]) only (row_ids None: the row itself); with
+    the packer's src_row it is the same for every draw of the cutoffs.  Returns [N, d].
+    """
+    N = _count(N)
+    ty = _type(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [>= N, d]")
+    d = x.shape[1]
+    _rows(x, N, (d,), "x")
+    _dev(x, x.dtype, "x")
+    if residual is not None:
+        _rows(residual, N, (d,), "residual")
+        _dev(residual, x.dtype, "residual")
+    _ints(row_ids, N, "row_ids")
+    if out is None:
+        out = torch.empty((N, d), dtype=x.dtype, device=x.device)
+    else:
+        _rows(out, N, (d,), "out")
+        _dev(out, x.dtype, "out")
+        _apart(out, "out", x, residual)
+    _check(load().pspo_dropout_add_fwd(_ptr(x), _ptr(residual), _ptr(row_ids), N, d, float(p), seed & _U64_MASK,
+                                       offset & _U64_MASK, ty, _ptr(out), _stream()))
+    return out[:N]
+
+
+def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optional[torch.Tensor] = None,
+                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of dropout_add to x (the residual's is dy itself): the mask drawn again and applied to dy.
+
+    dy: [>=N, d] bf16 or float32 (e.g. the loss call's d_hidden); the result is of out_dtype (default: dy's).
+    """
+    N = _count(N)
+    ty = _type(dy, "dy")
+    if dy.dim() != 2:
+        raise ValueError("dy must be [>= N, d]")
+    d = dy.shape[1]
+    _rows(dy, N, (d,), "dy")
+    _dev(dy, dy.dtype, "dy")
+    _ints(row_ids, N, "row_ids")
+    if out is None:
+        out = torch.empty((N, d), dtype=out_dtype or dy.dtype, device=dy.device)
+    else:
+        _rows(out, N, (d,), "out")
+        _dev(out, out_dtype or out.dtype, "out")
+        _apart(out, "out", dy)
+    _check(load().pspo_dropout_bwd(_ptr(dy), _ptr(row_ids), N, d, float(p), seed & _U64_MASK, offset & _U64_MASK, ty,
+                                   _type(out, "out"), _ptr(out), _stream()))
+    return out[:N]
