@@ -118,6 +118,52 @@ int pspo_dropout_add_fwd(const void* x, const void* residual, const int32_t* row
 int pspo_dropout_bwd(const void* dy, const int32_t* row_ids, int32_t N, int32_t d, double p, uint64_t seed,
                      uint64_t offset, int32_t dy_type, int32_t dx_type, void* dx, hipStream_t stream);
 
+/* Activations of pspo_gated_ffn_*. */
+#define PSPO_ACT_SILU      0   /* g / (1 + exp(-g)) */
+#define PSPO_ACT_GELU_TANH 1   /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+
+/* Flags of pspo_gated_ffn_bwd (PSPO_ACCUMULATE_DW, with float32 weight gradients, adds to them). */
+#define PSPO_FFN_DW_F32   256u /* weight gradients in float32 instead of bf16 */
+/* Flags of pspo_gated_ffn_workspace_bytes. */
+#define PSPO_FFN_BACKWARD 512u /* the backward call's workspace instead of the forward's */
+#define PSPO_FFN_PREACT  1024u /* ... with the forward's pre-activations given */
+
+/* Bytes of device workspace the calls below need for N tokens (host-only); 0 for sizes they refuse. */
+size_t pspo_gated_ffn_workspace_bytes(int32_t N, int32_t d, int32_t f, uint32_t flags);
+
+/*
+ * The gated feed-forward block: for every token x (a row of d entries)
+ *   g = Wg x,  u = Wu x,  h = act(g) * u,  y = Wd h.
+ * Sums in float32; h is rounded to bf16 (the operand of the last product), y once.
+ *
+ *  x             device, bf16 bits [N, d] row-major, 16-byte aligned.
+ *  w_gate, w_up  device, bf16 bits [f, d] row-major.
+ *  w_down        device, bf16 bits [d, f] row-major.
+ *  d, f          multiples of 8, at most 2^20.
+ *  y             device, bf16 bits [N, d] out.
+ *  preact        device, float32 [N, 2 f] out (g, then u, of each token), or NULL: what
+ *                the backward needs besides its inputs.
+ *  workspace     device, 256-byte aligned, its contents need not be kept.
+ */
+int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up, const uint16_t* w_down,
+                       int32_t N, int32_t d, int32_t f, int32_t act, uint16_t* y, float* preact,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Its gradient: with dh = Wd^T dy,
+ *   dg = dh * u * act'(g),  du = dh * act(g)   (rounded to bf16),
+ *   dx = Wg^T dg + Wu^T du,  dWg = sum dg x^T,  dWu = sum du x^T,  dWd = sum dy h^T.
+ *  dy            device, bf16 bits [N, d].
+ *  preact        what the forward wrote, or NULL: computed again (in the workspace).
+ *  dx            device, bf16 bits [N, d] out.
+ *  dw_gate, dw_up, dw_down   device, of the weights' shapes, out: bf16, or float32
+ *                with PSPO_FFN_DW_F32; N = 0 writes (or adds) zeros.
+ */
+int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up,
+                       const uint16_t* w_down, const float* preact, int32_t N, int32_t d, int32_t f,
+                       int32_t act, uint32_t flags, uint16_t* dx, void* dw_gate, void* dw_up, void* dw_down,
+                       void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }  /* extern "C" */
 #endif

@@ -16,7 +16,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libpspo.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
 SOURCES = ["abi.cpp", "sampler.hip", "loss.hip", "proxy.hip", "design.hip", "probe.hip",
-           "dropout.hip", "qknorm.hip"]
+           "dropout.hip", "qknorm.hip", "ffn.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

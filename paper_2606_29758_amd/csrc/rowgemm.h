@@ -1,0 +1,319 @@
+// Tiled bf16 x bf16 -> float32 matrix-core product on operands as they lie in
+// row-major memory, with a pluggable epilogue:
+//
+//   C(m, n) = sum_k A(m, k) B(n, k),
+//
+// each operand either K-inner (rows of K entries: A[m * ld + k]) or K-outer
+// (rows of M entries: A[k * ld + m]), so that the forward (weights and tokens
+// K-inner), the input gradients (weights K-outer) and the weight gradients (both
+// K-outer) of a linear layer need no transposed copy of anything.
+//
+// Tile: a 256-thread work-group (2 x 2 wave64s) owns (32 BM) x (32 BN) entries of
+// C, each wave BM x BN blocks of v_mfma_f32_16x16x32_bf16 in the accumulator
+// registers.  K advances in stages of 64 through two LDS buffers filled by
+// buffer loads that write LDS directly; the buffer descriptor's range check
+// turns rows and K past the operand's end into zeros, so no size need be a
+// multiple of the tile.
+//  * K-inner stages hold rows of 64 K entries (128 bytes): row r keeps its
+//    16-byte chunk c at place c ^ (r & 7), so the 16-row operand reads (16 bytes
+//    a lane) meet every bank once.
+//  * K-outer stages hold one row of the tile's M entries per k, read through the
+//    LDS transpose read (16 lanes take 4 rows x 16 entries, 8 bytes each, and
+//    get 4 rows of one entry); the 32-byte pieces of row k sit at place
+//    p ^ x(k), x(k) = (k & 3) | (k >> 3 & 3) << 2, so the 16 rows that one read
+//    of a wave touches lie in 16 (8 on a 128-entry row) different places.
+// Schedule: while the MFMAs of one half stage (32 K) run on one set of operand
+// registers the other set is read, at most one LDS read or load after each MFMA;
+// one barrier per stage, in its middle, behind which the stage's buffer is free
+// for the loads of the stage after next.
+#pragma once
+
+#include "gemm.h"
+
+namespace pspo {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int kRowK = 64;                 // K entries per stage
+
+struct RowOperand {
+  const uint16_t* p[2];    // p[1]: second K segment (or the second half of interleaved rows)
+  int64_t ld;              // entries between rows in memory
+  int rows;                // M (or N) entries that exist
+  int64_t seg_off;         // K-inner: entries from one K segment to the next within a row
+};
+
+struct RowShape {
+  RowOperand a, b;
+  int K, segs;             // K per segment, number of segments (1 or 2)
+  int tiles_m, tiles_n;
+  int parts;               // K parts (grid y)
+};
+
+constexpr int kGroupRows = 4;   // row tiles x all column tiles per group of the tile order
+
+// Work-group -> tile: work-groups b, b + 8, ... share an XCD and its L2; each XCD
+// takes a contiguous run of an order in which 4 x 8 neighbours run together.
+__device__ __forceinline__ bool row_tile(const RowShape& g, int bid, int& tm, int& tn) {
+  const int total = g.tiles_m * g.tiles_n, per = (total + kNumXcd - 1) / kNumXcd;
+  const int x = bid % kNumXcd, k = bid / kNumXcd;
+  const int t = x * per + k;
+  if (k >= per || t >= total) return false;
+  const int width = kGroupRows * g.tiles_n;
+  const int first = t / width * kGroupRows, rem = t % width;
+  const int gs = min(g.tiles_m - first, kGroupRows);
+  tm = first + rem % gs;
+  tn = rem / gs;
+  return true;
+}
+
+// One operand's side of the pipeline.  kOuter: K-outer layout.  kPair: K-inner
+// rows of two matrices interleaved by blocks of 16 (even blocks p[0], odd p[1]).
+template <int Blocks, bool kOuter, bool kPair>
+struct RowSide {
+  static constexpr int kTile = 32 * Blocks;          // entries of M (or N) per tile
+  static constexpr int kBytes = kTile * kRowK * 2;   // per stage
+  static constexpr int kLoads = kTile / 32;          // 1 KB loads per wave per stage
+  static constexpr int kReads = kOuter ? 2 * Blocks : Blocks;   // per half stage
+  static constexpr int kLanesPerK = kTile * 2 / 16, kKPerLoad = 64 / kLanesPerK;
+  static constexpr int kPlaces = kTile / 16;         // 32-byte pieces of a K-outer row
+
+  uint32_t voff[kLoads];
+  uint32_t tail;        // K-inner: added in the last stage of a segment (out of range for the lanes past K)
+  uint32_t rd[2];       // LDS byte offset of the lane's reads in half stage 0 / 1
+  const unsigned char* base[2];
+  uint32_t range;       // K-inner: bytes of the tile's rows
+  int64_t rows_bytes;   // bytes between rows in memory
+  int64_t seg_bytes;
+  int64_t col;          // K-outer: bytes from a row's start to the tile
+
+  static __device__ __forceinline__ int place(int k) { return ((k & 3) | ((k >> 3) & 3) << 2) & (kPlaces - 1); }
+
+  __device__ __forceinline__ void init(const RowOperand& o, int tile, int K, int wave, int side, int lane) {
+    rows_bytes = o.ld * 2;
+    seg_bytes = o.seg_off * 2;
+    if constexpr (kOuter) {
+      col = (int64_t)tile * kTile * 2;
+      base[0] = reinterpret_cast<const unsigned char*>(o.p[0]) + col;
+      base[1] = reinterpret_cast<const unsigned char*>(o.p[1]) + col;
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) {
+        const int k = (q * 4 + wave) * kKPerLoad + lane / kLanesPerK;
+        voff[q] = (uint32_t)(k * rows_bytes) + (uint32_t)(((lane % kLanesPerK) ^ (2 * place(k))) << 4);
+      }
+      // lane's row of the 4 x 16 piece: k = 8 (lane / 16) + (lane % 16) / 4, 8 bytes (lane % 4)
+      const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
+      rd[0] = (uint32_t)(k * (kTile * 2) + (((side * Blocks) ^ place(k)) << 5) + (lane & 3) * 8);
+      rd[1] = rd[0] + 32 * (kTile * 2);
+    } else {
+      constexpr int kRows = kPair ? kTile / 2 : kTile;   // rows of one matrix
+      const int64_t row0 = (int64_t)tile * kRows;
+      const int64_t have = min((int64_t)o.rows - row0, (int64_t)kRows);
+      range = (uint32_t)(have * rows_bytes);
+      base[0] = reinterpret_cast<const unsigned char*>(kPair && (wave >> 1) ? o.p[1] : o.p[0]) + row0 * rows_bytes;
+      const int chunk = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) {
+        // LDS row (4 q + wave) 8 + lane / 8; of a pair, block 2 q + wave / 2 is rows 16 q .. of matrix wave / 2
+        const int row = kPair ? q * 16 + (wave & 1) * 8 + (lane >> 3) : (q * 4 + wave) * 8 + (lane >> 3);
+        voff[q] = (uint32_t)(row * rows_bytes) + (uint32_t)(chunk << 4);
+      }
+      const int last = (K + kRowK - 1) / kRowK - 1;
+      tail = last * kRowK + chunk * 8 < K ? 0u : 0x80000000u;
+      const int row = side * Blocks * 16 + (lane & 15);
+      rd[0] = (uint32_t)(row * (kRowK * 2) + (((lane >> 4) ^ (row & 7)) << 4));
+      rd[1] = rd[0] ^ 64u;
+    }
+  }
+
+  // Descriptor, scalar offset and lane addend of stage `s` (K entries from s * 64 of a segment).
+  struct Stage {
+    u32x4 rsrc;
+    uint32_t soff, add;
+  };
+  // `live` false: an empty range, so the loads read nothing and write zeros.
+  __device__ __forceinline__ Stage stage(int seg, int s, int K, bool live) const {
+    Stage st;
+    const unsigned char* p;
+    uint32_t num;
+    if constexpr (kOuter) {
+      const int64_t left = ((int64_t)K - (int64_t)s * kRowK) * rows_bytes - col;
+      num = (uint32_t)max((int64_t)0, min(left, (int64_t)0x7FFFFFFF));
+      p = (seg ? base[1] : base[0]) + (int64_t)s * kRowK * rows_bytes;
+      st.soff = 0;
+      st.add = 0;
+    } else {
+      num = range;
+      p = base[0];
+      st.soff = (uint32_t)(seg * seg_bytes) + (uint32_t)s * (kRowK * 2);
+      st.add = (s + 1) * kRowK > K ? tail : 0u;
+    }
+    if (!live) num = st.soff = 0;
+    // raw buffer descriptor: 48-bit base, no stride, bytes in range, 32-bit data format
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    st.rsrc = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+                    (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu)),
+                    (uint32_t)__builtin_amdgcn_readfirstlane((int)num), 0x00020000u};
+    st.soff = (uint32_t)__builtin_amdgcn_readfirstlane((int)st.soff);
+    return st;
+  }
+  // Load Q of the stage, to its 1 KB of the LDS buffer at byte offset `lds`.  Written as
+  // asm, which has no output register: beside the builtin the compiler waits for every
+  // load in flight before each transpose read.  It knows nothing of these loads:
+  // row_barrier waits for them, and settle() keeps the wait states that a vector write
+  // of a scalar register needs before a load reads it.
+  template <int Q>
+  __device__ __forceinline__ void load(const Stage& st, uint32_t lds, int wave) const {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(lds + (Q * 4 + wave) * 1024), "v"(voff[Q] + st.add), "s"(st.rsrc), "s"(st.soff)
+                 : "memory");
+  }
+  // Read R of half stage `Half` into f (K-outer: two reads make one block).
+  template <int R, int Half>
+  __device__ __forceinline__ void read(bf16x8* f, const unsigned char* lds) const {
+    if constexpr (kOuter) {
+      constexpr int i = R / 2;
+      // the read goes out as the pair's first half, its second 4 rows of K further
+      union {
+        s16x4 h[2];
+        bf16x8 v;
+      } u;
+      u.v = f[i];
+      u.h[R & 1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(lds + ((rd[Half] ^ (i << 5)) + (R & 1) * 4 * (kTile * 2))));
+      f[i] = u.v;
+    } else {
+      f[R] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(lds + rd[Half] + R * 16 * (kRowK * 2)));
+    }
+  }
+};
+
+// Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, part); a wave
+// has kWaveLds bytes of LDS to itself.  Lane l's accumulator [i][j][r] is
+// C(tm 32 BM + (wm BM + i) 16 + (l / 16) 4 + r, tn 32 BN + (wn BN + j) 16 + l % 16).
+// Five wait states between whatever wrote the descriptors and the loads that read them.
+template <class SA, class SB>
+__device__ __forceinline__ void settle(SA& a, SB& b) {
+  asm volatile("s_nop 4" : "+s"(a.rsrc), "+s"(a.soff), "+s"(b.rsrc), "+s"(b.soff));
+}
+
+// stage_barrier whose wait for the asm loads is asm too.
+template <int Vm>
+__device__ __forceinline__ void row_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(Vm) : "memory");
+  stage_barrier<63>();
+}
+
+template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
+void row_gemm_kernel(RowShape g, Epi epi) {
+  using A = RowSide<BM, kOuterA, kPairA>;
+  using B = RowSide<BN, kOuterB, false>;
+  constexpr int kStage = A::kBytes + B::kBytes;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStage];
+
+  int tm, tn;
+  if (!row_tile(g, blockIdx.x, tm, tn)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  A sa;
+  B sb;
+  sa.init(g.a, tm, g.K, wave, wm, lane);
+  sb.init(g.b, tn, g.K, wave, wn, lane);
+
+  const int per_seg = (g.K + kRowK - 1) / kRowK, nk_all = per_seg * g.segs;
+  const int part = blockIdx.y;
+  const int kb = (int)((int64_t)part * nk_all / g.parts), ke = (int)((int64_t)(part + 1) * nk_all / g.parts);
+
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; ++i)
+#pragma unroll
+    for (int j = 0; j < BN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bf16x8 fa[2][BM] = {}, fb[2][BN] = {};   // operand registers of the two half stages
+
+  typename A::Stage ga;
+  typename B::Stage gb;
+  auto aim = [&](int s) {   // the next loads are those of stage s (none past the end)
+    const int seg = s >= per_seg ? 1 : 0;
+    ga = sa.stage(seg, s - seg * per_seg, g.K, s < ke);
+    gb = sb.stage(seg, s - seg * per_seg, g.K, s < ke);
+    settle(ga, gb);
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+#pragma unroll
+  for (int st = 0; st < 2; ++st) {
+    aim(kb + st);
+    repeat<A::kLoads>([&](auto q) { sa.template load<decltype(q)::value>(ga, lds0 + st * kStage, wave); });
+    repeat<B::kLoads>([&](auto q) { sb.template load<decltype(q)::value>(gb, lds0 + st * kStage + A::kBytes, wave); });
+  }
+  row_barrier<A::kLoads + B::kLoads>();
+  repeat<A::kReads>([&](auto r) { sa.template read<decltype(r)::value, 0>(fa[0], lds); });
+  repeat<B::kReads>([&](auto r) { sb.template read<decltype(r)::value, 0>(fb[0], lds + A::kBytes); });
+
+  constexpr int kMfma = BM * BN, kReads = A::kReads + B::kReads, kLoads = A::kLoads + B::kLoads;
+  static_assert(kReads <= kMfma && kLoads <= kMfma, "one read and one load at most after each MFMA");
+  uint32_t cur = 0;
+  for (int t = kb; t < ke; ++t) {
+    const uint32_t nxt = kStage - cur;
+    // first half: K 0 .. 31 of this stage; its other half is read
+    repeat<kMfma>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
+      mfma_agpr(acc[m][n], fa[0][m], fb[0][n]);
+      if constexpr (i < kReads) {
+        if constexpr (i < B::kReads) sb.template read<i, 1>(fb[1], lds + cur + A::kBytes);
+        else sa.template read<i - B::kReads, 1>(fa[1], lds + cur);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    // every wave is done with this stage's buffer, and the next stage has landed
+    row_barrier<0>();
+    aim(t + 2);
+    repeat<kMfma>([&](auto ic) {
+      constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
+      mfma_agpr(acc[m][n], fa[1][m], fb[1][n]);
+      if constexpr (i < kReads) {
+        if constexpr (i < B::kReads) sb.template read<i, 0>(fb[0], lds + nxt + A::kBytes);
+        else sa.template read<i - B::kReads, 0>(fa[0], lds + nxt);
+      }
+      if constexpr (i < kLoads) {
+        if constexpr (i < A::kLoads) sa.template load<i>(ga, lds0 + cur, wave);
+        else sb.template load<i - A::kLoads>(gb, lds0 + cur + A::kBytes, wave);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    cur = nxt;
+  }
+
+  mfma_drain();
+#pragma unroll
+  for (int i = 0; i < BM; ++i)
+#pragma unroll
+    for (int j = 0; j < BN; ++j) asm volatile("" : "+a"(acc[i][j]));
+  row_barrier<0>();   // the last (empty) loads have landed, every wave is done with the buffers
+  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kStage / 2), part);
+}
+
+// A wave's own LDS: what its lanes wrote before is seen by its lanes' reads after.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Rows of kRow bytes in LDS (pitch kRow + 16) -> rows of memory `pitch` bytes apart, 16
+// bytes a lane: row r < rows_have, bytes < bytes_have (a multiple of 16).
+template <int kRow, int kRows>
+__device__ __forceinline__ void put_rows(const unsigned char* lds, unsigned char* out, int64_t pitch, int rows_have,
+                                         int bytes_have, int lane) {
+  constexpr int kPer = kRow / 16;
+#pragma unroll
+  for (int x = 0; x < kRows * kPer; x += 64) {
+    const int r = (x + lane) / kPer, c = (x + lane) % kPer * 16;
+    if (r < rows_have && c < bytes_have)
+      *reinterpret_cast<u32x4*>(out + r * pitch + c) = *reinterpret_cast<const u32x4*>(lds + r * (kRow + 16) + c);
+  }
+}
+
+}  // namespace pspo

@@ -19,6 +19,8 @@ from .pspo import _check, _dev, _ptr, _stream
 
 TYPE_BF16, TYPE_F32 = 0, 1
 ROPE_INTERLEAVED, QK_NO_NORM = 1, 2
+ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}
+FFN_DW_F32, FFN_BACKWARD, FFN_PREACT = 256, 512, 1024
 
 _P = ctypes.c_void_p
 _I32, _I64, _U32, _U64, _F32, _F64, _SZ = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32, ctypes.c_uint64,
@@ -31,6 +33,10 @@ _SIGNATURES = {
     "pspo_qk_norm_rope_bwd": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I32,
                                              _I32, _I32, _I32, _F32, _I32, _U32, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     "pspo_dropout_add_fwd": (ctypes.c_int, [_P, _P, _P, _I32, _I32, _F64, _U64, _U64, _I32, _P, _P]),
+    "pspo_gated_ffn_workspace_bytes": (_SZ, [_I32, _I32, _I32, _U32]),
+    "pspo_gated_ffn_fwd": (ctypes.c_int, [_P, _P, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]),
+    "pspo_gated_ffn_bwd": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _U32, _P, _P, _P, _P, _P,
+                                          _SZ, _P]),
     "pspo_dropout_bwd": (ctypes.c_int, [_P, _P, _I32, _I32, _F64, _U64, _U64, _I32, _I32, _P, _P]),
 }
 
@@ -299,3 +305,100 @@ def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optio
     _check(load().pspo_dropout_bwd(_ptr(dy), _ptr(row_ids), N, d, float(p), seed & _U64_MASK, offset & _U64_MASK, ty,
                                    _type(out, "out"), _ptr(out), _stream()))
     return out[:N]
+
+
+# ---------------------------------------------------------------------------
+# the gated feed-forward block
+# ---------------------------------------------------------------------------
+
+def _act(act: str) -> int:
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def _ffn_weights(w_gate, w_up, w_down):
+    if w_gate.dim() != 2:
+        raise ValueError("w_gate must be [f, d]")
+    f, d = w_gate.shape
+    _exact(w_up, (f, d), "w_up")
+    _exact(w_down, (d, f), "w_down")
+    for name, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
+        _dev(w, torch.bfloat16, name)
+    return d, f
+
+
+def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, preact: bool = False) -> int:
+    flags = (FFN_BACKWARD if backward else 0) | (FFN_PREACT if preact else 0)
+    return int(load().pspo_gated_ffn_workspace_bytes(N, d, f, flags))
+
+
+def _ffn_workspace(workspace, N, d, f, backward, preact, device):
+    if workspace is None:
+        workspace = torch.empty(max(gated_ffn_workspace_bytes(N, d, f, backward, preact), 256), dtype=torch.uint8,
+                                device=device)
+    return _dev(workspace, torch.uint8, "workspace")
+
+
+def gated_ffn(x, w_gate, w_up, w_down, N: int, act: str = "silu", keep: bool = False,
+              out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T of the first N rows of x [>=N, d], all bf16.
+
+    w_gate, w_up: [f, d]; w_down: [d, f]; act: "silu" or "gelu_tanh".  Returns y ([N, d]) and, with
+    keep, the float32 pre-activations [N, 2 f] that gated_ffn_bwd takes (else preact is None).
+    """
+    N = _count(N)
+    kind = _act(act)
+    d, f = _ffn_weights(w_gate, w_up, w_down)
+    _rows(x, N, (d,), "x")
+    _dev(x, torch.bfloat16, "x")
+    if out is None:
+        out = torch.empty((N, d), dtype=torch.bfloat16, device=x.device)
+    else:
+        _rows(out, N, (d,), "out")
+        _dev(out, torch.bfloat16, "out")
+        _apart(out, "out", x, w_gate, w_up, w_down)
+    pre = torch.empty((N, 2 * f), dtype=torch.float32, device=x.device) if keep else None
+    workspace = _ffn_workspace(workspace, N, d, f, False, False, x.device)
+    _check(load().pspo_gated_ffn_fwd(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), N, d, f, kind, _ptr(out),
+                                     _ptr(pre), _ptr(workspace), workspace.numel(), _stream()))
+    return dict(y=out[:N], preact=pre, workspace=workspace)
+
+
+def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact: Optional[torch.Tensor] = None,
+                  dw: Optional[tuple] = None, accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None) -> dict:
+    """Gradient of gated_ffn: dx [N, d] (bf16), dw_gate, dw_up [f, d], dw_down [d, f].
+
+    dy: bf16 [>=N, d]; preact: what gated_ffn kept (None: computed again).  dw: the three weight
+    gradients to write, all bf16 or all float32 (None: bf16); accumulate adds to them (float32).
+    """
+    N = _count(N)
+    kind = _act(act)
+    d, f = _ffn_weights(w_gate, w_up, w_down)
+    for name, t in (("dy", dy), ("x", x)):
+        _rows(t, N, (d,), name)
+        _dev(t, torch.bfloat16, name)
+    if preact is not None:
+        _rows(preact, N, (2 * f,), "preact")
+        _dev(preact, torch.float32, "preact")
+    shapes = ((f, d), (f, d), (d, f))
+    if dw is None:
+        if accumulate:
+            raise ValueError("accumulate needs dw")
+        dw = tuple(torch.empty(s, dtype=torch.bfloat16, device=x.device) for s in shapes)
+    else:
+        for i, (t, s, name) in enumerate(zip(dw, shapes, ("dw_gate", "dw_up", "dw_down"))):
+            ty = _type(t, name)
+            if ty != _type(dw[0], name):
+                raise TypeError("the weight gradients must have one dtype")
+            _exact(t, s, name)
+            _dev(t, t.dtype, name)
+            _apart(t, name, dy, x, w_gate, w_up, w_down, preact, *dw[:i])
+    flags = (FFN_DW_F32 if dw[0].dtype == torch.float32 else 0) | (pspo.PSPO_ACCUMULATE_DW if accumulate else 0)
+    dx = torch.empty((N, d), dtype=torch.bfloat16, device=x.device)
+    workspace = _ffn_workspace(workspace, N, d, f, True, preact is not None, x.device)
+    _check(load().pspo_gated_ffn_bwd(_ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(preact), N, d, f,
+                                     kind, flags, _ptr(dx), _ptr(dw[0]), _ptr(dw[1]), _ptr(dw[2]), _ptr(workspace),
+                                     workspace.numel(), _stream()))
+    return dict(dx=dx, dw_gate=dw[0], dw_up=dw[1], dw_down=dw[2], workspace=workspace)

@@ -1,0 +1,289 @@
+"""GPU: the gated feed-forward block against the float64 oracle, through the binding.
+
+Tolerances are worst-case bounds carried through the formulas, entry by entry (u = 2^-24, one
+float32 rounding; b = 2^-8, half a bf16 step): a sum of n products errs by at most (n + 2) u of the
+sum of their sizes, the activation and its derivative by 32 u of their parts' sizes (an
+exponential of up to 20 is good to 20 u + 2 u, the division and products 4 u), h, dg and du take b
+once, and so does each bf16 output.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_ops as ol
+from paper_2606_29758_amd import layer, pspo
+
+pytestmark = pytest.mark.gpu
+U, B = 2.0 ** -24, 2.0 ** -8
+BF, F4 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    layer.load()
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _inputs(N, d, f, seed, cap=None):
+    g = torch.Generator("cuda").manual_seed(seed)
+    new = lambda *s, k=1.0: (torch.randn(*s, device="cuda", generator=g) * k).to(BF)   # noqa: E731
+    n = N if cap is None else cap
+    return (new(n, d), new(f, d, k=1.5 / d ** 0.5), new(f, d, k=1 / d ** 0.5), new(d, f, k=1 / f ** 0.5),
+            new(n, d, k=0.1))
+
+
+def _poisoned(N, d, f, backward=False, preact=False):
+    """A workspace of the size asked for, filled with NaN."""
+    n = max(layer.gated_ffn_workspace_bytes(N, d, f, backward, preact), 256)
+    return torch.full((n // 4,), float("nan"), device="cuda").view(torch.uint8)
+
+
+class Ref:
+    """Values and entry-wise error bounds of everything the calls return."""
+
+    def __init__(self, x, wg, wu, wd, dy, act):
+        N, d = x.shape
+        f = wg.shape[0]
+        ab = np.abs
+        s = lambda n: (n + 2) * U                       # noqa: E731
+        g, u = x @ wg.T, x @ wu.T
+        eg, eu = s(d) * (ab(x) @ ab(wg).T), s(d) * (ab(x) @ ab(wu).T)
+        a, da = ol.activation(g, act)
+        # |act'| < 1.13 and |act''| < 0.8, so an error eg of g moves act by 1.13 eg and act' by 0.8 eg
+        ea = 1.13 * eg + 32 * U * ab(g)
+        eda = 0.8 * eg + 32 * U * (1 + ab(a) + ab(g))
+        h = a * u
+        eh = (ea * ab(u) + ab(a) * eu + ea * eu) * (1 + B) + B * ab(h)
+        self.pre, self.e_pre = np.concatenate([g, u], 1), np.concatenate([eg, eu], 1)
+        self.y = h @ wd.T
+        self.e_y = (eh @ ab(wd).T + s(f) * ((ab(h) + eh) @ ab(wd).T)) * (1 + B) + B * ab(self.y)
+        dh = dy @ wd
+        edh = s(d) * (ab(dy) @ ab(wd))
+        dg, du = dh * u * da, dh * a
+        edg = (edh * ab(u * da) + ab(dh) * (eu * ab(da) + ab(u) * eda) + 4 * U * ab(dg)) * (1 + 1e-3) * (1 + B) + B * ab(dg)
+        edu = (edh * ab(a) + ab(dh) * ea + 4 * U * ab(du)) * (1 + 1e-3) * (1 + B) + B * ab(du)
+
+        def product(p, ep, q, n):
+            v = p @ q
+            return v, ep @ ab(q) + s(n) * ((ab(p) + ep) @ ab(q))
+
+        v1, e1 = product(dg, edg, wg, 2 * f)
+        v2, e2 = product(du, edu, wu, 2 * f)
+        self.dx, self.e_dx = v1 + v2, e1 + e2
+        self.dw, self.e_dw = zip(product(dg.T, edg.T, x, N + 66), product(du.T, edu.T, x, N + 66),
+                                 (lambda v, e: (v.T, e.T))(*product(h.T, eh.T, dy, N + 66)))
+
+    @staticmethod
+    def close(got, want, err, bf16, what):
+        e = np.abs(_np(got) - want)
+        tol = err * (1 + B) + B * np.abs(want) if bf16 else err
+        tol = tol + 1e-30
+        assert (e <= tol).all(), (what, float((e / tol).max()))
+
+
+def _check(N, d, f, act, seed=0, f32=False):
+    x, wg, wu, wd, dy = _inputs(N, d, f, seed + 13 * N + d + f)
+    r = Ref(*(_np(t) for t in (x, wg, wu, wd, dy)), act)
+    plain = layer.gated_ffn(x, wg, wu, wd, N, act=act, workspace=_poisoned(N, d, f))
+    kept = layer.gated_ffn(x, wg, wu, wd, N, act=act, keep=True, workspace=_poisoned(N, d, f))
+    assert torch.equal(plain["y"], kept["y"]) and plain["preact"] is None
+    Ref.close(kept["preact"], r.pre, r.e_pre, False, "preact")
+    Ref.close(kept["y"], r.y, r.e_y, False, "y")   # e_y holds y's rounding
+    dw = None
+    if f32:
+        dw = tuple(torch.full(s, float("nan"), device="cuda") for s in ((f, d), (f, d), (d, f)))
+    for pre in (kept["preact"], None):
+        o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, act=act, preact=pre, dw=dw,
+                                workspace=_poisoned(N, d, f, True, pre is not None))
+        Ref.close(o["dx"], r.dx, r.e_dx, True, "dx")
+        for name, v, e in zip(("dw_gate", "dw_up", "dw_down"), r.dw, r.e_dw):
+            assert o[name].dtype == (F4 if f32 else BF)
+            Ref.close(o[name], v, e, not f32, name)
+
+
+SIZES = [(1, 8, 8), (2, 8, 64), (3, 64, 64), (5, 128, 128), (15, 16, 1000), (16, 72, 136), (17, 136, 72), (31, 64, 2048),
+         (33, 200, 328), (64, 328, 200), (65, 264, 520), (127, 128, 256), (129, 520, 264), (256, 256, 256),
+         (257, 1000, 392), (301, 392, 1032), (640, 64, 64), (1025, 72, 200)]
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("N,d,f", SIZES)
+def test_sizes(N, d, f, act):
+    _check(N, d, f, act)
+
+
+@pytest.mark.parametrize("N,d,f", [(1, 8, 8), (77, 200, 136), (600, 264, 520)])
+def test_float32_weight_gradients(N, d, f):
+    _check(N, d, f, "silu", f32=True)
+
+
+@pytest.mark.parametrize("N,d,f", [(2050, 1544, 3592), (4099, 3592, 2056)])
+def test_large_tiles(N, d, f):
+    _check(N, d, f, "silu")
+
+
+def test_accumulated_weight_gradients():
+    """Two micro-batches added up; the first call overwrites what was there."""
+    N, d, f = 150, 136, 264
+    x, wg, wu, wd, dy = _inputs(N, d, f, 5)
+    r = Ref(*(_np(t) for t in (x, wg, wu, wd, dy)), "silu")
+    dw = tuple(torch.full(s, 9.0, device="cuda") for s in ((f, d), (f, d), (d, f)))
+    layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, dw=dw)
+    once = [t.clone() for t in dw]
+    layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, dw=dw, accumulate=True)
+    for t, o, v, e in zip(dw, once, r.dw, r.e_dw):
+        Ref.close(o, v, e, False, "first")
+        assert (t - 2 * o).abs().max() <= 2.0 ** -23 * o.abs().max()   # one float32 rounding of each sum
+    layer.gated_ffn_bwd(dy, x, wg, wu, wd, 0, dw=dw, accumulate=True)
+    assert all(torch.equal(t, 2 * o) or (t - 2 * o).abs().max() <= 2.0 ** -23 * o.abs().max() for t, o in zip(dw, once))
+
+
+def test_gradient_is_the_difference():
+    """sum(y dy) along a direction of the gate weights, in the float64 oracle's forward on both sides of the point,
+    against the call's gradient: within the gradient's own bound and the difference's h^2."""
+    N, d, f, h = 40, 64, 72, 1e-4
+    x, wg, wu, wd, dy = _inputs(N, d, f, 6)
+    o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, act="gelu_tanh")
+    n = [_np(t) for t in (x, wg, wu, wd, dy)]
+    r = Ref(*n, "gelu_tanh")
+    v = np.random.default_rng(1).normal(size=(f, d))
+    up, down = (ol.gated_ffn(n[0], n[1] + s * h * v, n[2], n[3], "gelu_tanh")[0] for s in (1, -1))
+    diff = ((up - down) * n[4]).sum() / (2 * h)
+    tol = ((r.e_dw[0] * (1 + B) + B * np.abs(r.dw[0])) * np.abs(v)).sum()
+    assert abs((_np(o["dw_gate"]) * v).sum() - diff) <= tol + 1e-5 * abs(diff)
+
+
+def test_no_tokens():
+    x, wg, wu, wd, dy = _inputs(2, 64, 72, 1)
+    assert layer.gated_ffn(x, wg, wu, wd, 0)["y"].shape == (0, 64)
+    o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, 0)
+    assert o["dx"].shape == (0, 64) and all((o[k] == 0).all() for k in ("dw_gate", "dw_up", "dw_down"))
+
+
+@pytest.mark.parametrize("N,cap", [(5, 9), (70, 100), (300, 513)])
+def test_rows_behind_and_values_that_are_not_finite(N, cap):
+    """Rows behind the N-th are neither read nor written; a token's NaN stays in its own row (and the weights')."""
+    d, f = 136, 200
+    x, wg, wu, wd, dy = _inputs(N, d, f, 3, cap)
+    x0, dy0 = x[:N].clone(), dy[:N].clone()
+    ref, rb = layer.gated_ffn(x0, wg, wu, wd, N, keep=True), layer.gated_ffn_bwd(dy0, x0, wg, wu, wd, N)
+    x[N:] = float("nan")
+    dy[N:] = float("inf")
+    out = torch.full((cap, d), 5.0, dtype=BF, device="cuda")
+    layer.gated_ffn(x, wg, wu, wd, N, out=out)
+    assert torch.equal(out[:N], ref["y"]) and (out[N:] == 5).all()
+    o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N)
+    assert all(torch.equal(o[k], rb[k]) for k in ("dx", "dw_gate", "dw_up", "dw_down"))
+    x[2, 3] = float("inf")
+    y = layer.gated_ffn(x, wg, wu, wd, N)["y"]
+    keep = torch.arange(N, device="cuda") != 2
+    assert torch.equal(y[keep], ref["y"][keep]) and not torch.isfinite(y[2]).any()
+    o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N)
+    assert torch.equal(o["dx"][keep], rb["dx"][keep])
+
+
+def test_activation_far_out():
+    """Pre-activations of hundreds and thousands: no overflow of the exponential or the cube reaches a result."""
+    d = f = 8
+    eye = torch.eye(8, device="cuda").to(BF)
+    x = torch.tensor([[-1e4, -300.0, -88.0, -20.0, 20.0, 88.0, 300.0, 1e4]], device="cuda").to(BF)
+    dy = torch.ones(1, 8, dtype=BF, device="cuda")
+    wu = torch.zeros(8, 8, dtype=BF, device="cuda")
+    wu[:, 4] = 0.0625                                      # u = 20 / 16 everywhere
+    for act in ("silu", "gelu_tanh"):
+        y = layer.gated_ffn(x, eye, wu, eye, 1, act=act)["y"].double()
+        o = layer.gated_ffn_bwd(dy, x, eye, wu, eye, 1, act=act)
+        a, da = ol.activation(_np(x), act)
+        assert np.allclose(_np(y), 1.25 * a, rtol=2 * B, atol=1e-5)
+        assert np.allclose(np.diag(_np(o["dw_gate"])), 1.25 * da[0] * _np(x)[0], rtol=3 * B, atol=1e-3)
+
+
+def test_offsets_past_32_bits():
+    """A token count at which the intermediate and the pre-activations pass 2^32 bytes: rows at both ends equal
+    those of small calls."""
+    N, d, f = 140_001, 64, 16000
+    x, wg, wu, wd, dy = _inputs(N, d, f, 8)
+    y = layer.gated_ffn(x, wg, wu, wd, N, keep=True)
+    g = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, preact=y["preact"])
+    for at in (slice(0, 50), slice(67_090, 67_140), slice(N - 50, N)):
+        r = Ref(*(_np(t) for t in (x[at], wg, wu, wd, dy[at])), "silu")
+        Ref.close(y["y"][at], r.y, r.e_y, False, "y")
+        Ref.close(y["preact"][at], r.pre, r.e_pre, False, "preact")
+        Ref.close(g["dx"][at], r.dx, r.e_dx, True, "dx")
+    # the weight gradients of the halves add up to the whole's
+    parts = [layer.gated_ffn_bwd(dy[a], x[a], wg, wu, wd, x[a].shape[0],
+                                 dw=tuple(torch.empty(s, device="cuda") for s in ((f, d), (f, d), (d, f))))
+             for a in (slice(0, N // 2), slice(N // 2, N))]
+    for k in ("dw_gate", "dw_up", "dw_down"):
+        s = parts[0][k] + parts[1][k]
+        e = (g[k].float() - s).abs()
+        # bf16 output; sums of 140,001 float32 terms on both sides stay far below its step
+        assert (e <= B * s.abs() + 1e-3 * s.abs().max()).all()
+
+
+def test_refusals():
+    x, wg, wu, wd, dy = _inputs(8, 64, 72, 2)
+    with pytest.raises(ValueError, match="act must be"):
+        layer.gated_ffn(x, wg, wu, wd, 8, act="relu")
+    with pytest.raises(ValueError, match="w_up"):
+        layer.gated_ffn(x, wg, wu[:64], wd, 8)
+    with pytest.raises(ValueError, match="x must be"):
+        layer.gated_ffn(x, wg, wu, wd, 9)
+    with pytest.raises(TypeError, match="dtype"):
+        layer.gated_ffn(x.float(), wg, wu, wd, 8)
+    with pytest.raises(ValueError, match="contiguous"):
+        layer.gated_ffn(x, wg, wu, wd.t().contiguous().t(), 8)
+    with pytest.raises(ValueError, match="overlaps"):
+        layer.gated_ffn(x, wg, wu, wd, 8, out=x)
+    with pytest.raises(pspo.PspoError, match="workspace"):
+        layer.gated_ffn(x, wg, wu, wd, 8, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(pspo.PspoError, match="workspace"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(pspo.PspoError, match="d % 8"):
+        layer.gated_ffn(torch.zeros(8, 60, dtype=BF, device="cuda"), *(torch.zeros(s, dtype=BF, device="cuda")
+                                                                       for s in ((72, 60), (72, 60), (60, 72))), 8)
+    with pytest.raises(ValueError, match="accumulate needs"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, accumulate=True)
+    dw = tuple(torch.empty(s, dtype=BF, device="cuda") for s in ((72, 64), (72, 64), (64, 72)))
+    with pytest.raises(pspo.PspoError, match="float32"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, dw=dw, accumulate=True)
+    with pytest.raises(ValueError, match="overlaps"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, dw=(dw[0], dw[0], dw[2]))
+    with pytest.raises(ValueError, match="preact"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, preact=torch.empty(8, 72, device="cuda"))
+
+
+@pytest.mark.parametrize("N,d,f", [(1, 256, 512), (40, 256, 512), (700, 264, 1032)])
+def test_streams_and_graph_replays(N, d, f):
+    """On two streams at once, and captured and replayed on new inputs: the eager bits."""
+    x, wg, wu, wd, dy = _inputs(N, d, f, 4)
+
+    def calls(xx):
+        a = layer.gated_ffn(xx, wg, wu, wd, N, keep=True)
+        b = layer.gated_ffn_bwd(dy, xx, wg, wu, wd, N, preact=a["preact"])
+        return [a["y"], a["preact"], b["dx"], b["dw_gate"], b["dw_up"], b["dw_down"]]
+
+    x2 = (x.float() * 0.5).to(BF)
+    ref, ref2 = [[t.clone() for t in calls(v)] for v in (x, x2)]
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(s1):
+        a = calls(x)
+    with torch.cuda.stream(s2):
+        b = calls(x2)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(a + b, ref + ref2))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = calls(x)
+    for step in range(3):
+        x.mul_(-1.0 if step else 1.0)
+        want = [t.clone() for t in calls(x)]
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), step
