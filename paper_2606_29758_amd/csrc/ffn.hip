@@ -68,7 +68,7 @@ struct EpiBf16 {
       for (int i = 0; i < BM; ++i) {
         float v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
+        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
         *reinterpret_cast<u32x2*>(lds + (lane & 15) * (kRow + 16) + i * 32 + (lane >> 4) * 8) = pack4(v);
       }
       wave_lds_fence();
@@ -87,32 +87,58 @@ struct EpiBf16 {
   }
 };
 
-// C(m, n) -> out[part][n * ld + m] in float32, or added to it.
+// C(m, n) -> out[n * ld + m] in float32, or added to it.
 struct EpiF32 {
   float *out, *out2;
-  int64_t ld, part_stride;
+  int64_t ld;
   int M, N, split, add;
   template <int BM, int BN>
   __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char*, int part) const {
+                                        unsigned char*, int) const {
     const int m0 = (tm * 2 + wm) * BM * 16 + (lane >> 4) * 4;
     repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
       constexpr int j = decltype(jc)::value;
       const int n = ((tn * 2 + wn) * BN + j) * 16 + (lane & 15);
-      if (n >= N) return;
-      float* row = (n < split ? out + (int64_t)n * ld : out2 + (int64_t)(n - split) * ld) + part * part_stride;
+      float* row = n < split ? out + (int64_t)n * ld : out2 + (int64_t)(n - split) * ld;
 #pragma unroll
-      for (int i = 0; i < BM; ++i)
-        if (m0 + i * 16 < M) {   // M % 8 == 0
+      for (int i = 0; i < BM; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
+        if (n < N && m0 + i * 16 < M) {   // M % 8 == 0
           f32x4* p = reinterpret_cast<f32x4*>(row + m0 + i * 16);
-          f32x4 v;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r];
           *p = add ? *p + v : v;
         }
+      }
     });
   }
 };
+
+// A K part's whole tile in float32 to slab number `slab`: the 16 x 16 blocks one after
+// another (those of a column of blocks together), each as its lanes hold it, so that a store
+// writes 1 KB in one piece.  slab_piece says where four entries lie.
+struct EpiSlab {
+  float* base;
+  template <int BM, int BN>
+  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int, int, int wm, int wn, int lane, unsigned char*,
+                                        int slab) const {
+    float* to = base + (int64_t)slab * (1024 * BM * BN) + (wn * BN * 2 * BM + wm * BM) * 256 + lane * 4;
+    repeat<BN>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+#pragma unroll
+      for (int i = 0; i < BM; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
+        *reinterpret_cast<f32x4*>(to + (j * 2 * BM + i) * 256) = v;
+      }
+    });
+  }
+};
+// Offset of entries (m .. m + 3, n) of a tile of `tile` rows, m % 4 == 0.
+__device__ __forceinline__ int slab_piece(int tile, int m, int n) {
+  return ((n >> 4) * (tile >> 4) + (m >> 4)) * 256 + (((m >> 2) & 3) * 16 + (n & 15)) * 4;
+}
 
 // Row blocks in pairs (gate, up): h[n][j] = act(g) u, and the pre-activations if kept.
 struct EpiGateUp {
@@ -122,32 +148,38 @@ struct EpiGateUp {
   template <int BM, int BN>
   __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
                                         unsigned char* lds, int) const {
-    constexpr int kRow = BM * 16;   // BM * 8 entries of h a token
+    constexpr int kRow = BM * 16, kOne = kCols * (kRow + 16);   // BM * 8 entries of h a token
+    constexpr int kRow4 = 2 * kRow, kOne4 = kCols * (kRow4 + 16);
     const int m0 = (tm * 2 + wm) * BM * 8;
     repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
       constexpr int j = decltype(jc)::value;
-      const int n0 = ((tn * 2 + wn) * BN + j) * 16, n = n0 + (lane & 15);
+      const int n0 = ((tn * 2 + wn) * BN + j) * 16;
 #pragma unroll
       for (int i = 0; i < BM; i += 2) {
         f32x4 g, u;
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          g[r] = acc[i][j][r];
-          u[r] = acc[i + 1][j][r];
+          g[r] = acc_read(acc[i][j][r]);
+          u[r] = acc_read(acc[i + 1][j][r]);
           v[r] = act_value(g[r], act) * u[r];
         }
-        const int m = m0 + i * 8 + (lane >> 4) * 4;
-        if (pre != nullptr && n < N && m < f) {
-          float* row = pre + (int64_t)n * 2 * f + m;
-          *reinterpret_cast<f32x4*>(row) = g;
-          *reinterpret_cast<f32x4*>(row + f) = u;
+        const int at = i * 8 + (lane >> 4) * 4;   // entry of the token's row
+        *reinterpret_cast<u32x2*>(lds + (lane & 15) * (kRow + 16) + at * 2) = pack4(v);
+        if (pre != nullptr) {
+          unsigned char* p = lds + kOne + (lane & 15) * (kRow4 + 16) + at * 4;
+          *reinterpret_cast<f32x4*>(p) = g;
+          *reinterpret_cast<f32x4*>(p + kOne4) = u;
         }
-        *reinterpret_cast<u32x2*>(lds + (lane & 15) * (kRow + 16) + i * 16 + (lane >> 4) * 8) = pack4(v);
       }
       wave_lds_fence();
       put_rows<kRow, kCols>(lds, reinterpret_cast<unsigned char*>(h + (int64_t)n0 * f + m0), (int64_t)f * 2, N - n0,
                             (f - m0) * 2, lane);
+      if (pre != nullptr) {
+        unsigned char* to = reinterpret_cast<unsigned char*>(pre + (int64_t)n0 * 2 * f + m0);
+        put_rows<kRow4, kCols>(lds + kOne, to, (int64_t)f * 8, N - n0, (f - m0) * 4, lane);
+        put_rows<kRow4, kCols>(lds + kOne + kOne4, to + (int64_t)f * 4, (int64_t)f * 8, N - n0, (f - m0) * 4, lane);
+      }
       wave_lds_fence();
     });
   }
@@ -163,27 +195,35 @@ struct EpiDh {
                                         unsigned char* lds, int) const {
     constexpr int kRow = BM * 32, kOne = kCols * (kRow + 16);
     const int m0 = (tm * 2 + wm) * BM * 16;
-    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
-      constexpr int j = decltype(jc)::value;
-      const int n0 = ((tn * 2 + wn) * BN + j) * 16, n = n0 + (lane & 15);
+    f32x4 g[2][BM], u[2][BM];   // pre-activations of this column of blocks and of the next
+    auto fetch = [&](int j, f32x4* gj, f32x4* uj) {
+      const int n = ((tn * 2 + wn) * BN + j) * 16 + (lane & 15);
+      const float* row = pre + (int64_t)n * 2 * f + m0 + (lane >> 4) * 4;
 #pragma unroll
       for (int i = 0; i < BM; ++i) {
-        const int m = m0 + i * 16 + (lane >> 4) * 4;
-        f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
-        if (n < N && m < f) {
-          const float* row = pre + (int64_t)n * 2 * f + m;
-          g = *reinterpret_cast<const f32x4*>(row);
-          u = *reinterpret_cast<const f32x4*>(row + f);
+        gj[i] = uj[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (n < N && m0 + i * 16 + (lane >> 4) * 4 < f) {
+          gj[i] = *reinterpret_cast<const f32x4*>(row + i * 16);
+          uj[i] = *reinterpret_cast<const f32x4*>(row + f + i * 16);
         }
+      }
+    };
+    fetch(0, g[0], u[0]);
+    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
+      constexpr int j = decltype(jc)::value;
+      const int n0 = ((tn * 2 + wn) * BN + j) * 16;
+      if constexpr (j + 1 < BN) fetch(j + 1, g[(j + 1) & 1], u[(j + 1) & 1]);
+#pragma unroll
+      for (int i = 0; i < BM; ++i) {
         float dg[4], du[4], hv[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float a, da;
-          act_both(g[r], act, a, da);
-          const float dh = acc[i][j][r];
-          dg[r] = dh * u[r] * da;
+          act_both(g[j & 1][i][r], act, a, da);
+          const float dh = acc_read(acc[i][j][r]);
+          dg[r] = dh * u[j & 1][i][r] * da;
           du[r] = dh * a;
-          hv[r] = a * u[r];
+          hv[r] = a * u[j & 1][i][r];
         }
         unsigned char* at = lds + (lane & 15) * (kRow + 16) + i * 32 + (lane >> 4) * 8;
         *reinterpret_cast<u32x2*>(at) = pack4(dg);
@@ -202,77 +242,153 @@ struct EpiDh {
 };
 
 // ---- parts of K joined ------------------------------------------------------------
-// out = sum over parts of slab[part][i], in order, for 8 entries a thread; float32 or
-// bf16, or added to float32.  The entries from `split` on belong to a second matrix.
+// The slabs of a tile's parts added in order, then what the product's epilogue does with
+// the sum, eight entries of a column a thread.  `which`: the epilogue.
+enum : int { kJoinStore, kJoinGateUp, kJoinDh };
 struct JoinArgs {
   const float* slab;
-  int64_t total, split;
-  int parts;
-  unsigned char *out, *out2;
-  int f32, add;
+  RowShape g;
+  int tile, which;
+  EpiBf16 bf16;   // kJoinStore in bf16 ...
+  EpiF32 f32;     // ... or float32 (out set)
+  EpiGateUp gu;
+  EpiDh dh;
 };
-__global__ __launch_bounds__(256) void ffn_join_kernel(JoinArgs a) {
-  const int64_t v = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (v >= a.total) return;
+__device__ __forceinline__ Vec8 join8(const JoinArgs& a, int index, int m, int n) {
+  const int64_t size = (int64_t)a.tile * a.tile;
+  const int at = slab_piece(a.tile, m, n);   // entries m .. m + 3; the next four lie 64 floats on (m % 8 == 0)
   Vec8 s{};
-  for (int p = 0; p < a.parts; ++p) {
-    const Vec8 x = unpack8(load8<F32>(reinterpret_cast<const unsigned char*>(a.slab + p * a.total), v / 8));
+  for (int p = 0; p < a.g.parts; ++p) {
+    const float* from = a.slab + ((int64_t)p * a.g.count + index) * size + at;
+    const f32x4 x = *reinterpret_cast<const f32x4*>(from), y = *reinterpret_cast<const f32x4*>(from + 64);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s.v[i] += x.v[i];
-  }
-  const bool second = v >= a.split;   // split % 8 == 0
-  unsigned char* out = second ? a.out2 : a.out;
-  const int64_t at = (second ? v - a.split : v) / 8;
-  if (a.f32) {
-    if (a.add) {
-      const Vec8 x = unpack8(load8<F32>(out, at));
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s.v[i] += x.v[i];
+    for (int i = 0; i < 4; ++i) {
+      s.v[i] += x[i];
+      s.v[4 + i] += y[i];
     }
-    store8<F32>(out, at, s);
+  }
+  return s;
+}
+__global__ __launch_bounds__(256) void ffn_join_kernel(JoinArgs a) {
+  int tm, tn;
+  row_tile_at(a.g, a.g.tile0 + blockIdx.x, tm, tn);
+  // a wave takes 8 columns x 64 entries: whole lines of the output, 128-byte pieces of the slabs
+  const int width = a.which == kJoinGateUp ? a.tile / 2 : a.tile;
+  const int w = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int row = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
+  if (row >= a.tile) return;
+  const int64_t n = (int64_t)tn * a.tile + row;
+  if (a.which == kJoinStore) {
+    const int64_t m = (int64_t)tm * a.tile + m0;
+    if (n >= a.bf16.N || m >= a.bf16.M) return;
+    Vec8 s = join8(a, blockIdx.x, m0, row);
+    const bool second = n >= a.bf16.split;
+    const int64_t at = (second ? n - a.bf16.split : n) * a.bf16.ld + m;   // a multiple of 8
+    if (a.f32.out != nullptr) {
+      unsigned char* out = reinterpret_cast<unsigned char*>(second ? a.f32.out2 : a.f32.out);
+      if (a.f32.add) {
+        const Vec8 o = unpack8(load8<F32>(out, at / 8));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s.v[i] += o.v[i];
+      }
+      store8<F32>(out, at / 8, s);
+    } else {
+      store8<Bf16>(reinterpret_cast<unsigned char*>(second ? a.bf16.out2 : a.bf16.out), at / 8, s);
+    }
+  } else if (a.which == kJoinGateUp) {
+    const int64_t m = (int64_t)tm * (a.tile / 2) + m0;
+    if (n >= a.gu.N || m >= a.gu.f) return;
+    const int at = m0 / 16 * 32 + m0 % 16;   // gate and up in turn, 16 rows each
+    const Vec8 g = join8(a, blockIdx.x, at, row), u = join8(a, blockIdx.x, at + 16, row);
+    if (a.gu.pre != nullptr) {
+      unsigned char* pre = reinterpret_cast<unsigned char*>(a.gu.pre);
+      store8<F32>(pre, (n * 2 * a.gu.f + m) / 8, g);
+      store8<F32>(pre, (n * 2 * a.gu.f + a.gu.f + m) / 8, u);
+    }
+    Vec8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h.v[i] = act_value(g.v[i], a.gu.act) * u.v[i];
+    store8<Bf16>(reinterpret_cast<unsigned char*>(a.gu.h), (n * a.gu.f + m) / 8, h);
   } else {
-    store8<Bf16>(out, at, s);
+    const int64_t m = (int64_t)tm * a.tile + m0;
+    if (n >= a.dh.N || m >= a.dh.f) return;
+    const Vec8 dh = join8(a, blockIdx.x, m0, row);
+    const int64_t at = (n * 2 * a.dh.f + m) / 8;
+    const unsigned char* pre = reinterpret_cast<const unsigned char*>(a.dh.pre);
+    const Vec8 g = unpack8(load8<F32>(pre, at)), u = unpack8(load8<F32>(pre, at + a.dh.f / 8));
+    Vec8 dg, du, h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v, dv;
+      act_both(g.v[i], a.dh.act, v, dv);
+      dg.v[i] = dh.v[i] * u.v[i] * dv;
+      du.v[i] = dh.v[i] * v;
+      h.v[i] = v * u.v[i];
+    }
+    unsigned char* dgu = reinterpret_cast<unsigned char*>(a.dh.dgu);
+    store8<Bf16>(dgu, at, dg);
+    store8<Bf16>(dgu, at + a.dh.f / 8, du);
+    store8<Bf16>(reinterpret_cast<unsigned char*>(a.dh.h), (n * a.dh.f + m) / 8, h);
   }
 }
 
 // ---- plan ---------------------------------------------------------------------------
-// Tile and K parts of a product of M x N entries over nk stages.  fused: the epilogue
-// needs whole sums, so K is not split.
+// How a product of M x N entries over nk stages is covered: tiles of 256 x 256 (one
+// work-group to a CU) or 128 x 128 (two), the first `whole` of them launched as they are
+// and the rest in `parts` parts of K (parts = 1: all are whole).
 struct Plan {
-  int big;       // 256 x 256 tiles (one work-group to a CU), else 128 x 128 (two)
-  int tiles_m, tiles_n, parts;
+  int tile, tiles_m, tiles_n, whole, parts;
+  double us;
 };
 constexpr int64_t kSlabBytes = int64_t(256) << 20;   // most that the parts of one product take
 
-Plan plan_of(int64_t M, int64_t N, int nk, bool fused) {
-  auto tiles = [&](int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+// The cover of least estimated time: a stage of a round takes 1.45 us (256), 1.1 us (128, two
+// work-groups to a CU) or 0.7 us (one), each tile 20 us (10) beyond its stages, the parts'
+// slabs are written and read at 4.5 TB/s, and a further launch with its join takes 8 us.
+Plan plan_tile(int64_t M, int64_t N, int nk, int tile) {
   Plan p{};
-  p.big = tiles(256) >= 224;
-  const int t = p.big ? 256 : 128;
-  p.tiles_m = (int)((M + t - 1) / t);
-  p.tiles_n = (int)((N + t - 1) / t);
+  p.tile = tile;
+  p.tiles_m = (int)((M + tile - 1) / tile);
+  p.tiles_n = (int)((N + tile - 1) / tile);
+  const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : 512;
+  const double extra = tile == 256 ? 20 : 10;
+  auto time = [&](int64_t groups, int stages, double per_tile) {
+    const int64_t turns = (groups + slots - 1) / slots;
+    const bool alone = groups - (turns - 1) * slots <= 256;
+    const double stage = tile == 256 ? 1.45 : 1.1, last = tile == 128 && alone ? 0.7 : stage;
+    return (double)(turns - 1) * (stages * stage + per_tile) + stages * last + per_tile;
+  };
+  const int64_t before = (total - 1) / slots * slots, rest = total - before;   // the last round's tiles
+  p.whole = (int)total;
   p.parts = 1;
-  if (!fused) {
-    const int64_t have = tiles(t), slots = p.big ? 256 : 512;
-    int64_t s = slots / std::max<int64_t>(have, 1);
-    s = std::min<int64_t>(s, nk / 4);                          // four stages at least per part
-    s = std::min<int64_t>(s, kSlabBytes / std::max<int64_t>(M * N * 4, 1));
-    s = std::min<int64_t>(s, 64);
-    p.parts = (int)std::max<int64_t>(s, 1);
+  p.us = time(total, nk, extra);
+  const double start = before ? time(before, nk, extra) : 0.0;
+  const int64_t bytes = (int64_t)tile * tile * 4;
+  for (int s = 2; s <= 32 && s * 4 <= nk && rest * s * bytes <= kSlabBytes; ++s) {
+    const double us = start + time(rest * s, (nk + s - 1) / s, extra / 2) + 8 + (double)(rest * s * bytes) * 2 / 4.5e6;
+    if (us < p.us) {
+      p.us = us;
+      p.whole = (int)before;
+      p.parts = s;
+    }
   }
   return p;
 }
+Plan plan_of(int64_t M, int64_t N, int nk) {
+  const Plan big = plan_tile(M, N, nk, 256), small = plan_tile(M, N, nk, 128);
+  return big.us <= small.us ? big : small;
+}
+int64_t slab_bytes(int64_t M, int64_t N, int K, int segs) {
+  if (M == 0 || N == 0) return 0;
+  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK * segs);
+  if (p.parts == 1) return 0;
+  return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile * 4;
+}
 
 template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-int launch(RowShape g, const Plan& p, const Epi& epi, const char* name, hipStream_t stream) {
-  g.tiles_m = p.tiles_m;
-  g.tiles_n = p.tiles_n;
-  g.parts = p.parts;
-  const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
-  PSPO_REQUIRE(total < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
-  const dim3 grid((uint32_t)((total + kNumXcd - 1) / kNumXcd * kNumXcd), (uint32_t)p.parts);
-  if (total == 0) return PSPO_OK;
-  if (p.big)
+int launch(const RowShape& g, int tile, const Epi& epi, const char* name, hipStream_t stream) {
+  const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
+  if (tile == 256)
     hipLaunchKernelGGL((row_gemm_kernel<8, 8, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
   else
     hipLaunchKernelGGL((row_gemm_kernel<4, 4, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
@@ -280,37 +396,56 @@ int launch(RowShape g, const Plan& p, const Epi& epi, const char* name, hipStrea
   return PSPO_OK;
 }
 
+// One product with its epilogue: the whole tiles, then the rest in parts and their join
+// (`join` holds the same epilogue).
+template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, float* slab, const char* name,
+            hipStream_t stream) {
+  if (M == 0 || N == 0) return PSPO_OK;
+  const Plan p = plan_of(M, N, (g.K + kRowK - 1) / kRowK * g.segs);
+  const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+  PSPO_REQUIRE(total < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
+  g.tiles_m = p.tiles_m;
+  g.tiles_n = p.tiles_n;
+  g.tile0 = 0;
+  g.count = p.whole;
+  g.parts = 1;
+  if (g.count > 0)
+    if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p.tile, epi, name, stream)) return rc;
+  g.tile0 = p.whole;
+  g.count = (int)(total - p.whole);
+  if (g.count == 0) return PSPO_OK;
+  g.parts = p.parts;
+  if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p.tile, EpiSlab{slab}, name, stream)) return rc;
+  join.slab = slab;
+  join.g = g;
+  join.tile = p.tile;
+  const int chunks = (join.which == kJoinGateUp ? p.tile / 2 : p.tile) / 8;
+  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(p.tile * chunks / 256)), dim3(256), 0, stream,
+                     join);
+  PSPO_LAUNCHED("ffn_join_kernel", stream);
+  return PSPO_OK;
+}
+
 // A product whose output is stored as it is: out[n][m], bf16 or float32 (or added to
-// it); rows n >= split go to out2.  The slabs of K parts lie in `slab`.
+// it); rows n >= split go to out2.
 struct Out {
   void *out, *out2;
   int split;
   bool f32, add;
 };
 template <bool kOuterA, bool kOuterB>
-int product(RowShape g, int M, int N, const Out& o, float* slab, const char* name, hipStream_t stream) {
-  const int nk = (g.K + kRowK - 1) / kRowK * g.segs;
-  const Plan p = plan_of(M, N, nk, false);
-  if (p.parts > 1) {
-    EpiF32 e{slab, slab, M, (int64_t)M * N, M, N, N, 0};
-    if (int rc = launch<kOuterA, kOuterB, false>(g, p, e, name, stream)) return rc;
-    JoinArgs j{slab, (int64_t)M * N, (int64_t)M * o.split, p.parts, static_cast<unsigned char*>(o.out),
-               static_cast<unsigned char*>(o.out2), o.f32, o.add};
-    hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)((j.total / 8 + 255) / 256)), dim3(256), 0, stream, j);
-    PSPO_LAUNCHED("ffn_join_kernel", stream);
-    return PSPO_OK;
+int stored(const RowShape& g, int M, int N, const Out& o, float* slab, const char* name, hipStream_t stream) {
+  JoinArgs j{};
+  j.which = kJoinStore;
+  j.bf16 = EpiBf16{static_cast<uint16_t*>(o.out), static_cast<uint16_t*>(o.out2), M, M, N, o.split};
+  if constexpr (kOuterB) {   // weight gradients: also in float32
+    if (o.f32) {
+      j.f32 = EpiF32{static_cast<float*>(o.out), static_cast<float*>(o.out2), M, M, N, o.split, o.add};
+      return product<kOuterA, kOuterB, false>(g, M, N, j.f32, j, slab, name, stream);
+    }
   }
-  if (o.f32) {
-    EpiF32 e{static_cast<float*>(o.out), static_cast<float*>(o.out2), M, 0, M, N, o.split, o.add};
-    return launch<kOuterA, kOuterB, false>(g, p, e, name, stream);
-  }
-  EpiBf16 e{static_cast<uint16_t*>(o.out), static_cast<uint16_t*>(o.out2), M, M, N, o.split};
-  return launch<kOuterA, kOuterB, false>(g, p, e, name, stream);
-}
-
-int64_t slab_bytes(int64_t M, int64_t N, int K, int segs) {
-  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK * segs, false);
-  return p.parts > 1 ? p.parts * M * N * 4 : 0;
+  return product<kOuterA, kOuterB, false>(g, M, N, j.bf16, j, slab, name, stream);
 }
 
 // Workspace layout of one call.
@@ -327,12 +462,14 @@ Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
   };
   s.h = take(N * f * 2);
   int64_t slab = 0;
+  if (!backward || !kept) slab = slab_bytes(2 * f, N, (int)d, 1);
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab_bytes(d, N, (int)f, 2), slab_bytes(d, 2 * f, (int)N, 1), slab_bytes(f, d, (int)N, 1)});
+    slab = std::max({slab, slab_bytes(f, N, (int)d, 1), slab_bytes(d, N, (int)f, 2), slab_bytes(d, 2 * f, (int)N, 1),
+                     slab_bytes(f, d, (int)N, 1)});
   } else {
-    slab = slab_bytes(d, N, (int)f, 1);
+    slab = std::max(slab, slab_bytes(d, N, (int)f, 1));
   }
   s.slab = take(slab);
   s.total = at;
@@ -362,10 +499,12 @@ RowShape shape(const uint16_t* a, const uint16_t* a2, int64_t lda, int rows_a, c
 
 // h (and the pre-activations, if `pre`) of the first N tokens.
 int gate_up(const uint16_t* x, const uint16_t* wg, const uint16_t* wu, int N, int d, int f, int act, uint16_t* h,
-            float* pre, hipStream_t stream) {
-  const RowShape g = shape(wg, wu, d, f, x, d, N, d);
-  const Plan p = plan_of(2 * (int64_t)f, N, (d + kRowK - 1) / kRowK, true);
-  return launch<false, false, true>(g, p, EpiGateUp{h, pre, f, N, act}, "ffn_gate_up", stream);
+            float* pre, float* slab, hipStream_t stream) {
+  JoinArgs j{};
+  j.which = kJoinGateUp;
+  j.gu = EpiGateUp{h, pre, f, N, act};
+  return product<false, false, true>(shape(wg, wu, d, f, x, d, N, d), 2 * (int64_t)f, N, j.gu, j, slab, "ffn_gate_up",
+                                     stream);
 }
 
 }  // namespace
@@ -399,8 +538,8 @@ int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + s.h);
   float* slab = reinterpret_cast<float*>(ws + s.slab);
-  if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, preact, stream)) return rc;
-  return product<false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, Out{y, y, N, false, false}, slab,
+  if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, preact, slab, stream)) return rc;
+  return stored<false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, Out{y, y, N, false, false}, slab,
                                "ffn_down", stream);
 }
 
@@ -433,21 +572,23 @@ int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_
     const float* pre = preact;
     if (pre == nullptr) {
       float* own = reinterpret_cast<float*>(ws + s.pre);
-      if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, own, stream)) return rc;
+      if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, own, slab, stream)) return rc;
       pre = own;
     }
-    const Plan p = plan_of(f, N, (d + kRowK - 1) / kRowK, true);
-    if (int rc = launch<true, false, false>(shape(w_down, w_down, f, f, dy, d, N, d), p, EpiDh{pre, dgu, h, f, N, act},
-                                            "ffn_dh", stream))
+    JoinArgs j{};
+    j.which = kJoinDh;
+    j.dh = EpiDh{pre, dgu, h, f, N, act};
+    if (int rc = product<true, false, false>(shape(w_down, w_down, f, f, dy, d, N, d), f, N, j.dh, j, slab, "ffn_dh",
+                                             stream))
       return rc;
-    if (int rc = product<true, false>(shape(w_gate, w_up, d, d, dgu, 2 * (int64_t)f, N, f, 2, f), d, N,
+    if (int rc = stored<true, false>(shape(w_gate, w_up, d, d, dgu, 2 * (int64_t)f, N, f, 2, f), d, N,
                                       Out{dx, dx, N, false, false}, slab, "ffn_dx", stream))
       return rc;
   }
-  if (int rc = product<true, true>(shape(x, x, d, d, dgu, 2 * (int64_t)f, 2 * f, N), d, 2 * f,
+  if (int rc = stored<true, true>(shape(x, x, d, d, dgu, 2 * (int64_t)f, 2 * f, N), d, 2 * f,
                                    Out{dw_gate, dw_up, f, f32, add}, slab, "ffn_dw_gate_up", stream))
     return rc;
-  return product<true, true>(shape(h, h, f, f, dy, d, d, N), f, d, Out{dw_down, dw_down, d, f32, add}, slab,
+  return stored<true, true>(shape(h, h, f, f, dy, d, d, N), f, d, Out{dw_down, dw_down, d, f32, add}, slab,
                              "ffn_dw_down", stream);
 }
 

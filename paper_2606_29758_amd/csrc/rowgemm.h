@@ -48,24 +48,27 @@ struct RowShape {
   RowOperand a, b;
   int K, segs;             // K per segment, number of segments (1 or 2)
   int tiles_m, tiles_n;
+  int tile0, count;        // this launch's tiles: positions [tile0, tile0 + count) of the order below
   int parts;               // K parts (grid y)
 };
 
 constexpr int kGroupRows = 4;   // row tiles x all column tiles per group of the tile order
 
-// Work-group -> tile: work-groups b, b + 8, ... share an XCD and its L2; each XCD
-// takes a contiguous run of an order in which 4 x 8 neighbours run together.
-__device__ __forceinline__ bool row_tile(const RowShape& g, int bid, int& tm, int& tn) {
-  const int total = g.tiles_m * g.tiles_n, per = (total + kNumXcd - 1) / kNumXcd;
-  const int x = bid % kNumXcd, k = bid / kNumXcd;
-  const int t = x * per + k;
-  if (k >= per || t >= total) return false;
+// Position t of the tile order: groups of 4 row tiles x all column tiles, so that 4 x 8
+// neighbours run together.
+__device__ __forceinline__ void row_tile_at(const RowShape& g, int t, int& tm, int& tn) {
   const int width = kGroupRows * g.tiles_n;
   const int first = t / width * kGroupRows, rem = t % width;
   const int gs = min(g.tiles_m - first, kGroupRows);
   tm = first + rem % gs;
   tn = rem / gs;
-  return true;
+}
+// Work-group -> index among the launch's tiles (-1: none): work-groups b, b + 8, ... share an
+// XCD and its L2; each XCD takes a contiguous run of the order.
+__device__ __forceinline__ int row_index(const RowShape& g, int bid) {
+  const int per = (g.count + kNumXcd - 1) / kNumXcd;
+  const int x = bid % kNumXcd, k = bid / kNumXcd, t = x * per + k;
+  return k < per && t < g.count ? t : -1;
 }
 
 // One operand's side of the pipeline.  kOuter: K-outer layout.  kPair: K-inner
@@ -127,36 +130,44 @@ struct RowSide {
     }
   }
 
-  // Descriptor, scalar offset and lane addend of stage `s` (K entries from s * 64 of a segment).
+  // Descriptor, scalar offset and lane addend of the stage to load next.
   struct Stage {
     u32x4 rsrc;
     uint32_t soff, add;
+    uint64_t at;      // K-outer: address of the stage's first row
   };
-  // `live` false: an empty range, so the loads read nothing and write zeros.
-  __device__ __forceinline__ Stage stage(int seg, int s, int K, bool live) const {
-    Stage st;
-    const unsigned char* p;
-    uint32_t num;
-    if constexpr (kOuter) {
-      const int64_t left = ((int64_t)K - (int64_t)s * kRowK) * rows_bytes - col;
-      num = (uint32_t)max((int64_t)0, min(left, (int64_t)0x7FFFFFFF));
-      p = (seg ? base[1] : base[0]) + (int64_t)s * kRowK * rows_bytes;
-      st.soff = 0;
-      st.add = 0;
-    } else {
-      num = range;
-      p = base[0];
-      st.soff = (uint32_t)(seg * seg_bytes) + (uint32_t)s * (kRowK * 2);
-      st.add = (s + 1) * kRowK > K ? tail : 0u;
-    }
-    if (!live) num = st.soff = 0;
+  __device__ __forceinline__ void describe(Stage& st, uint64_t at, uint32_t num) const {
     // raw buffer descriptor: 48-bit base, no stride, bytes in range, 32-bit data format
-    const uint64_t at = reinterpret_cast<uint64_t>(p);
-    st.rsrc = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
-                    (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu)),
-                    (uint32_t)__builtin_amdgcn_readfirstlane((int)num), 0x00020000u};
-    st.soff = (uint32_t)__builtin_amdgcn_readfirstlane((int)st.soff);
-    return st;
+    st.rsrc = u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, num, 0x00020000u};
+  }
+  // `left`: K entries of the segment from the stage's first on; live false: an empty range,
+  // so the loads read nothing and write zeros.
+  __device__ __forceinline__ void set(Stage& st, int left, bool live) const {
+    if constexpr (kOuter) {
+      // rows of this stage; the last one ends with the matrix's row, not past it
+      const uint32_t num = (uint32_t)min(left, kRowK) * (uint32_t)rows_bytes - (uint32_t)col;
+      describe(st, st.at, live ? num : 0u);
+      st.soff = st.add = 0;
+    } else {
+      describe(st, reinterpret_cast<uint64_t>(base[0]), live ? range : 0u);
+      st.add = left < kRowK ? tail : 0u;
+    }
+  }
+  __device__ __forceinline__ void first(Stage& st, int seg, int s, int left, bool live) const {
+    if constexpr (kOuter) st.at = reinterpret_cast<uint64_t>((seg ? base[1] : base[0]) + (int64_t)s * kRowK * rows_bytes);
+    else st.soff = live ? (uint32_t)(seg * seg_bytes) + (uint32_t)s * (kRowK * 2) : 0u;
+    set(st, left, live);
+  }
+  // From one stage to the next; `over`: it is the second segment's first.
+  __device__ __forceinline__ void next(Stage& st, bool over, int left, bool live) const {
+    if constexpr (kOuter) {
+      st.at += (uint64_t)(kRowK * rows_bytes);
+      if (over) st.at = reinterpret_cast<uint64_t>(base[1]);
+    } else {
+      st.soff = over ? (uint32_t)seg_bytes : st.soff + kRowK * 2;
+      st.soff = live ? st.soff : 0u;
+    }
+    set(st, left, live);
   }
   // Load Q of the stage, to its 1 KB of the LDS buffer at byte offset `lds`.  Written as
   // asm, which has no output register: beside the builtin the compiler waits for every
@@ -190,8 +201,8 @@ struct RowSide {
   }
 };
 
-// Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, part); a wave
-// has kWaveLds bytes of LDS to itself.  Lane l's accumulator [i][j][r] is
+// Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, slab); a wave
+// has its own part of the LDS; slab = part * (tiles of the launch) + tile.  Lane l's accumulator [i][j][r] is
 // C(tm 32 BM + (wm BM + i) 16 + (l / 16) 4 + r, tn 32 BN + (wn BN + j) 16 + l % 16).
 // Five wait states between whatever wrote the descriptors and the loads that read them.
 template <class SA, class SB>
@@ -214,8 +225,10 @@ void row_gemm_kernel(RowShape g, Epi epi) {
   constexpr int kStage = A::kBytes + B::kBytes;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStage];
 
+  const int index = row_index(g, blockIdx.x);
+  if (index < 0) return;
   int tm, tn;
-  if (!row_tile(g, blockIdx.x, tm, tn)) return;
+  row_tile_at(g, g.tile0 + index, tm, tn);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   A sa;
@@ -234,26 +247,41 @@ void row_gemm_kernel(RowShape g, Epi epi) {
     for (int j = 0; j < BN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   bf16x8 fa[2][BM] = {}, fb[2][BN] = {};   // operand registers of the two half stages
 
+  // The loads run two stages ahead; past the end they are empty.
   typename A::Stage ga;
   typename B::Stage gb;
-  auto aim = [&](int s) {   // the next loads are those of stage s (none past the end)
-    const int seg = s >= per_seg ? 1 : 0;
-    ga = sa.stage(seg, s - seg * per_seg, g.K, s < ke);
-    gb = sb.stage(seg, s - seg * per_seg, g.K, s < ke);
-    settle(ga, gb);
+  int ahead = kb, left;
+  {
+    const int seg = kb >= per_seg ? 1 : 0;
+    left = g.K - (kb - seg * per_seg) * kRowK;
+    sa.first(ga, seg, kb - seg * per_seg, left, kb < ke);
+    sb.first(gb, seg, kb - seg * per_seg, left, kb < ke);
+  }
+  bool over = false;
+  auto step = [&] {   // the next stage's place; its two sides follow
+    ++ahead;
+    left -= kRowK;
+    over = left <= 0;
+    left = over ? g.K : left;
   };
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
 #pragma unroll
   for (int st = 0; st < 2; ++st) {
-    aim(kb + st);
+    settle(ga, gb);
     repeat<A::kLoads>([&](auto q) { sa.template load<decltype(q)::value>(ga, lds0 + st * kStage, wave); });
     repeat<B::kLoads>([&](auto q) { sb.template load<decltype(q)::value>(gb, lds0 + st * kStage + A::kBytes, wave); });
+    if (st == 0) {
+      step();
+      sa.next(ga, over, left, ahead < ke);
+      sb.next(gb, over, left, ahead < ke);
+    }
   }
   row_barrier<A::kLoads + B::kLoads>();
   repeat<A::kReads>([&](auto r) { sa.template read<decltype(r)::value, 0>(fa[0], lds); });
   repeat<B::kReads>([&](auto r) { sb.template read<decltype(r)::value, 0>(fb[0], lds + A::kBytes); });
 
   constexpr int kMfma = BM * BN, kReads = A::kReads + B::kReads, kLoads = A::kLoads + B::kLoads;
+  constexpr int kEvery = kMfma / kLoads, kApart = kMfma / kReads;   // MFMAs per load, per read
   static_assert(kReads <= kMfma && kLoads <= kMfma, "one read and one load at most after each MFMA");
   uint32_t cur = 0;
   for (int t = kb; t < ke; ++t) {
@@ -262,38 +290,54 @@ void row_gemm_kernel(RowShape g, Epi epi) {
     repeat<kMfma>([&](auto ic) {
       constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
       mfma_agpr(acc[m][n], fa[0][m], fb[0][n]);
-      if constexpr (i < kReads) {
-        if constexpr (i < B::kReads) sb.template read<i, 1>(fb[1], lds + cur + A::kBytes);
-        else sa.template read<i - B::kReads, 1>(fa[1], lds + cur);
+      if constexpr (i % kApart == 0 && i / kApart < kReads) {
+        constexpr int r = i / kApart;
+        if constexpr (r < B::kReads) sb.template read<r, 1>(fb[1], lds + cur + A::kBytes);
+        else sa.template read<r - B::kReads, 1>(fa[1], lds + cur);
       }
+      // where the stage after next lies, in slots without a read where there are such
+      if constexpr (i == kMfma - 6) step();
+      if constexpr (i == kMfma - 5) sa.next(ga, over, left, ahead < ke);
+      if constexpr (i == kMfma - 3) sb.next(gb, over, left, ahead < ke);
       __builtin_amdgcn_sched_barrier(0);
     });
     // every wave is done with this stage's buffer, and the next stage has landed
     row_barrier<0>();
-    aim(t + 2);
+    settle(ga, gb);
     repeat<kMfma>([&](auto ic) {
       constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
       mfma_agpr(acc[m][n], fa[1][m], fb[1][n]);
-      if constexpr (i < kReads) {
-        if constexpr (i < B::kReads) sb.template read<i, 0>(fb[0], lds + nxt + A::kBytes);
-        else sa.template read<i - B::kReads, 0>(fa[0], lds + nxt);
+      if constexpr (i % kApart == 0 && i / kApart < kReads) {
+        constexpr int r = i / kApart;
+        if constexpr (r < B::kReads) sb.template read<r, 0>(fb[0], lds + nxt + A::kBytes);
+        else sa.template read<r - B::kReads, 0>(fa[0], lds + nxt);
       }
-      if constexpr (i < kLoads) {
-        if constexpr (i < A::kLoads) sa.template load<i>(ga, lds0 + cur, wave);
-        else sb.template load<i - A::kLoads>(gb, lds0 + cur + A::kBytes, wave);
+      if constexpr (i % kEvery == kEvery - 1 && i / kEvery < kLoads) {
+        constexpr int q = i / kEvery;
+        if constexpr (q < A::kLoads) sa.template load<q>(ga, lds0 + cur, wave);
+        else sb.template load<q - A::kLoads>(gb, lds0 + cur + A::kBytes, wave);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
     cur = nxt;
+    // The accumulators are readable some passes after the last MFMA, which the compiler
+    // does not know of: the wait stands inside the loop, before any copy that it makes of
+    // them on the way out.
+    if (t + 1 == ke) mfma_drain();
+    __builtin_amdgcn_sched_barrier(0);
   }
 
-  mfma_drain();
-#pragma unroll
-  for (int i = 0; i < BM; ++i)
-#pragma unroll
-    for (int j = 0; j < BN; ++j) asm volatile("" : "+a"(acc[i][j]));
   row_barrier<0>();   // the last (empty) loads have landed, every wave is done with the buffers
-  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kStage / 2), part);
+  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kStage / 2),
+                              part * g.count + index);
+}
+
+// One accumulator, read where it is needed: as a plain value the compiler copies the
+// whole tile to vector registers at the loop's end, and spills.
+__device__ __forceinline__ float acc_read(float a) {
+  float x;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a));
+  return x;
 }
 
 // A wave's own LDS: what its lanes wrote before is seen by its lanes' reads after.
