@@ -347,7 +347,8 @@ __device__ __forceinline__ void wave_lds_fence() {
 }
 
 // Rows of kRow bytes in LDS (pitch kRow + 16) -> rows of memory `pitch` bytes apart, 16
-// bytes a lane: row r < rows_have, bytes < bytes_have (a multiple of 16).
+// bytes a lane: row r < rows_have, bytes < bytes_have (a multiple of 16).  Past the caches:
+// whole lines, far more of them than the caches hold until the next kernel reads them.
 template <int kRow, int kRows>
 __device__ __forceinline__ void put_rows(const unsigned char* lds, unsigned char* out, int64_t pitch, int rows_have,
                                          int bytes_have, int lane) {
@@ -356,7 +357,8 @@ __device__ __forceinline__ void put_rows(const unsigned char* lds, unsigned char
   for (int x = 0; x < kRows * kPer; x += 64) {
     const int r = (x + lane) / kPer, c = (x + lane) % kPer * 16;
     if (r < rows_have && c < bytes_have)
-      *reinterpret_cast<u32x4*>(out + r * pitch + c) = *reinterpret_cast<const u32x4*>(lds + r * (kRow + 16) + c);
+      __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(lds + r * (kRow + 16) + c),
+                                  reinterpret_cast<u32x4*>(out + r * pitch + c));
   }
 }
 
