@@ -140,6 +140,20 @@ __device__ __forceinline__ int slab_piece(int tile, int m, int n) {
   return ((n >> 4) * (tile >> 4) + (m >> 4)) * 256 + (((m >> 2) & 3) * 16 + (n & 15)) * 4;
 }
 
+// One of the three, by what the plan gave the product.
+struct EpiAny {
+  EpiBf16 bf16;
+  EpiF32 f32;     // used if out is set
+  EpiSlab slab;   // used if base is set
+  template <int BM, int BN>
+  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
+                                        unsigned char* lds, int slab_index) const {
+    if (slab.base != nullptr) slab.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
+    else if (f32.out != nullptr) f32.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
+    else bf16.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
+  }
+};
+
 // Row blocks in pairs (gate, up): h[n][j] = act(g) u, and the pre-activations if kept.
 struct EpiGateUp {
   uint16_t* h;
@@ -396,6 +410,8 @@ int launch(const RowShape& g, int tile, const Epi& epi, const char* name, hipStr
   return PSPO_OK;
 }
 
+int join_parts(JoinArgs join, const RowShape& g, int tile, const float* slab, hipStream_t stream);
+
 // One product with its epilogue: the whole tiles, then the rest in parts and their join
 // (`join` holds the same epilogue).
 template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
@@ -417,35 +433,118 @@ int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, flo
   if (g.count == 0) return PSPO_OK;
   g.parts = p.parts;
   if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p.tile, EpiSlab{slab}, name, stream)) return rc;
+  return join_parts(join, g, p.tile, slab, stream);
+}
+
+// The join of a product's slabs, after `launch`.
+int join_parts(JoinArgs join, const RowShape& g, int tile, const float* slab, hipStream_t stream) {
   join.slab = slab;
   join.g = g;
-  join.tile = p.tile;
-  const int chunks = (join.which == kJoinGateUp ? p.tile / 2 : p.tile) / 8;
-  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(p.tile * chunks / 256)), dim3(256), 0, stream,
+  join.tile = tile;
+  const int chunks = (join.which == kJoinGateUp ? tile / 2 : tile) / 8;
+  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(tile * chunks / 256)), dim3(256), 0, stream,
                      join);
   PSPO_LAUNCHED("ffn_join_kernel", stream);
   return PSPO_OK;
 }
 
-// A product whose output is stored as it is: out[n][m], bf16 or float32 (or added to
-// it); rows n >= split go to out2.
+// The three products behind dh, as one launch: dx, the two upper weights' gradients, the
+// lower one's.  All tiles of a size; a product whose tiles have more K stages than a
+// work-group's share of the whole is split along K.
+struct JobPlan {
+  int tile;
+  int tiles_m[3], tiles_n[3], parts[3];
+  int64_t slab[3], slab_bytes;   // bytes from the slabs' start; all of them
+  double us;
+};
+JobPlan plan_jobs(const int64_t (&M)[3], const int64_t (&N)[3], const int (&nk)[3], int tile) {
+  JobPlan p{};
+  p.tile = tile;
+  const int64_t slots = tile == 256 ? 256 : 512, bytes = (int64_t)tile * tile * 4;
+  int64_t units = 0, groups = 0;
+  for (int i = 0; i < 3; ++i) {
+    p.tiles_m[i] = (int)((M[i] + tile - 1) / tile);
+    p.tiles_n[i] = (int)((N[i] + tile - 1) / tile);
+    units += (int64_t)p.tiles_m[i] * p.tiles_n[i] * nk[i];
+  }
+  const int64_t share = std::max<int64_t>(units / slots, 4);
+  int longest = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
+    int64_t s = std::min<int64_t>((nk[i] + share - 1) / share, 32);
+    s = std::max<int64_t>(std::min<int64_t>(s, tiles ? kSlabBytes / 3 / (tiles * bytes) : 1), 1);
+    p.parts[i] = (int)s;
+    p.slab[i] = p.slab_bytes;
+    if (s > 1) p.slab_bytes += tiles * s * bytes;
+    groups += tiles * s;
+    if (tiles) longest = std::max(longest, (int)((nk[i] + s - 1) / s));
+  }
+  // a round's stages, half of the longest part idle at the end, the slabs out and in
+  const bool alone = tile == 128 && groups <= 256;
+  const double stage = tile == 256 ? 1.45 : alone ? 0.7 : 1.1;
+  const double rounds = (double)groups / (double)slots;
+  p.us = std::max((double)units / (double)slots + longest * 0.5, (double)longest) * stage +
+         std::max(rounds, 1.0) * (tile == 256 ? 10 : 5) + (double)p.slab_bytes * 2 / 4.5e6 + (p.slab_bytes ? 8 : 0);
+  return p;
+}
+JobPlan plan_backward(int64_t N, int64_t d, int64_t f) {
+  const int64_t M[3] = {N > 0 ? d : 0, d, f}, C[3] = {N, 2 * f, d};
+  const int kd = (int)((f + kRowK - 1) / kRowK * 2), kn = (int)((N + kRowK - 1) / kRowK);
+  const int nk[3] = {kd, kn, kn};
+  const JobPlan big = plan_jobs(M, C, nk, 256), small = plan_jobs(M, C, nk, 128);
+  return big.us <= small.us ? big : small;
+}
+
+// What a product stores: out[n][m], bf16 or float32 (or added to it); rows n >= split go to out2.
 struct Out {
   void *out, *out2;
-  int split;
+  int M, N, split;
   bool f32, add;
 };
-template <bool kOuterA, bool kOuterB>
-int stored(const RowShape& g, int M, int N, const Out& o, float* slab, const char* name, hipStream_t stream) {
+EpiBf16 bf16_of(const Out& o) {
+  return EpiBf16{static_cast<uint16_t*>(o.out), static_cast<uint16_t*>(o.out2), o.M, o.M, o.N, o.split};
+}
+EpiF32 f32_of(const Out& o) {
+  if (!o.f32) return EpiF32{};
+  return EpiF32{static_cast<float*>(o.out), static_cast<float*>(o.out2), o.M, o.M, o.N, o.split, o.add};
+}
+JoinArgs join_of(const Out& o) {
   JoinArgs j{};
   j.which = kJoinStore;
-  j.bf16 = EpiBf16{static_cast<uint16_t*>(o.out), static_cast<uint16_t*>(o.out2), M, M, N, o.split};
-  if constexpr (kOuterB) {   // weight gradients: also in float32
-    if (o.f32) {
-      j.f32 = EpiF32{static_cast<float*>(o.out), static_cast<float*>(o.out2), M, M, N, o.split, o.add};
-      return product<kOuterA, kOuterB, false>(g, M, N, j.f32, j, slab, name, stream);
-    }
+  j.bf16 = bf16_of(o);
+  j.f32 = f32_of(o);
+  return j;
+}
+
+int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsigned char* slabs, hipStream_t stream) {
+  RowJobs<EpiAny> jobs{};
+  int64_t blocks = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
+    PSPO_REQUIRE(tiles < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
+    RowShape& r = jobs.g[i];
+    r = g[i];
+    r.tiles_m = p.tiles_m[i];
+    r.tiles_n = p.tiles_n[i];
+    r.tile0 = 0;
+    r.count = (int)tiles;
+    r.parts = p.parts[i];
+    jobs.blocks[i] = (int)(round_up(tiles, kNumXcd) * p.parts[i]);
+    blocks += jobs.blocks[i];
+    jobs.epi[i] = EpiAny{bf16_of(o[i]), f32_of(o[i]),
+                         EpiSlab{p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr}};
   }
-  return product<kOuterA, kOuterB, false>(g, M, N, j.bf16, j, slab, name, stream);
+  PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
+  if (p.tile == 256)
+    hipLaunchKernelGGL((row_jobs_kernel<8, 8, EpiAny>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  else
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, EpiAny>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  PSPO_LAUNCHED("ffn_gradients", stream);
+  for (int i = 0; i < 3; ++i)
+    if (p.parts[i] > 1 && jobs.g[i].count > 0)
+      if (int rc = join_parts(join_of(o[i]), jobs.g[i], p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
+        return rc;
+  return PSPO_OK;
 }
 
 // Workspace layout of one call.
@@ -466,8 +565,7 @@ Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab, slab_bytes(f, N, (int)d, 1), slab_bytes(d, N, (int)f, 2), slab_bytes(d, 2 * f, (int)N, 1),
-                     slab_bytes(f, d, (int)N, 1)});
+    slab = std::max({slab, slab_bytes(f, N, (int)d, 1), plan_backward(N, d, f).slab_bytes});
   } else {
     slab = std::max(slab, slab_bytes(d, N, (int)f, 1));
   }
@@ -539,8 +637,9 @@ int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + s.h);
   float* slab = reinterpret_cast<float*>(ws + s.slab);
   if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, preact, slab, stream)) return rc;
-  return stored<false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, Out{y, y, N, false, false}, slab,
-                               "ffn_down", stream);
+  const Out o{y, y, d, N, N, false, false};
+  return product<false, false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, bf16_of(o), join_of(o), slab,
+                                      "ffn_down", stream);
 }
 
 int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up,
@@ -581,15 +680,13 @@ int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_
     if (int rc = product<true, false, false>(shape(w_down, w_down, f, f, dy, d, N, d), f, N, j.dh, j, slab, "ffn_dh",
                                              stream))
       return rc;
-    if (int rc = stored<true, false>(shape(w_gate, w_up, d, d, dgu, 2 * (int64_t)f, N, f, 2, f), d, N,
-                                      Out{dx, dx, N, false, false}, slab, "ffn_dx", stream))
-      return rc;
   }
-  if (int rc = stored<true, true>(shape(x, x, d, d, dgu, 2 * (int64_t)f, 2 * f, N), d, 2 * f,
-                                   Out{dw_gate, dw_up, f, f32, add}, slab, "ffn_dw_gate_up", stream))
-    return rc;
-  return stored<true, true>(shape(h, h, f, f, dy, d, d, N), f, d, Out{dw_down, dw_down, d, f32, add}, slab,
-                             "ffn_dw_down", stream);
+  const RowShape g[3] = {shape(w_gate, w_up, d, d, dgu, 2 * (int64_t)f, N, f, 2, f),
+                         shape(x, x, d, d, dgu, 2 * (int64_t)f, 2 * f, N), shape(h, h, f, f, dy, d, d, N)};
+  const Out o[3] = {{dx, dx, d, N, N, false, false},
+                    {dw_gate, dw_up, d, 2 * f, f, f32, add},
+                    {dw_down, dw_down, f, d, d, f32, add}};
+  return run_jobs(plan_backward(N, d, f), g, o, reinterpret_cast<unsigned char*>(slab), stream);
 }
 
 }  // extern "C"

@@ -217,15 +217,18 @@ __device__ __forceinline__ void row_barrier() {
   stage_barrier<63>();
 }
 
+template <int BM, int BN>
+constexpr int kRowLds = 2 * (32 * BM + 32 * BN) * kRowK * 2;
+
+// One tile of a product: work-group `bid` of the launch's tiles, K part `part`.
 template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
-void row_gemm_kernel(RowShape g, Epi epi) {
+__device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi, int bid, int part,
+                                              unsigned char* lds) {
   using A = RowSide<BM, kOuterA, kPairA>;
   using B = RowSide<BN, kOuterB, false>;
   constexpr int kStage = A::kBytes + B::kBytes;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStage];
 
-  const int index = row_index(g, blockIdx.x);
+  const int index = row_index(g, bid);
   if (index < 0) return;
   int tm, tn;
   row_tile_at(g, g.tile0 + index, tm, tn);
@@ -237,7 +240,6 @@ void row_gemm_kernel(RowShape g, Epi epi) {
   sb.init(g.b, tn, g.K, wave, wn, lane);
 
   const int per_seg = (g.K + kRowK - 1) / kRowK, nk_all = per_seg * g.segs;
-  const int part = blockIdx.y;
   const int kb = (int)((int64_t)part * nk_all / g.parts), ke = (int)((int64_t)(part + 1) * nk_all / g.parts);
 
   f32x4 acc[BM][BN];
@@ -330,6 +332,41 @@ void row_gemm_kernel(RowShape g, Epi epi) {
   row_barrier<0>();   // the last (empty) loads have landed, every wave is done with the buffers
   epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kStage / 2),
                               part * g.count + index);
+}
+
+template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
+void row_gemm_kernel(RowShape g, Epi epi) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
+  row_gemm_tile<BM, BN, kOuterA, kOuterB, kPairA>(g, epi, blockIdx.x, blockIdx.y, lds);
+}
+
+// Independent products in one launch, the first with A K-outer and B K-inner, the others with
+// both K-outer: their work-groups fill the chip together, so that only the last tiles of all
+// leave part of it idle.  A job's work-groups: its parts one after another, the tiles of a
+// part rounded up to whole rounds of the XCDs.
+template <class Epi>
+struct RowJobs {
+  static constexpr int kJobs = 3;
+  RowShape g[kJobs];
+  Epi epi[kJobs];
+  int blocks[kJobs];
+};
+template <int BM, int BN, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
+void row_jobs_kernel(RowJobs<Epi> jobs) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
+  int bid = blockIdx.x;
+  if (bid < jobs.blocks[0]) {
+    const int per = (jobs.g[0].count + kNumXcd - 1) / kNumXcd * kNumXcd;
+    row_gemm_tile<BM, BN, true, false, false>(jobs.g[0], jobs.epi[0], bid % per, bid / per, lds);
+    return;
+  }
+  bid -= jobs.blocks[0];
+  const int job = bid < jobs.blocks[1] ? 1 : 2;
+  if (job == 2) bid -= jobs.blocks[1];
+  const int per = (jobs.g[job].count + kNumXcd - 1) / kNumXcd * kNumXcd;
+  row_gemm_tile<BM, BN, true, true, false>(jobs.g[job], jobs.epi[job], bid % per, bid / per, lds);
 }
 
 // One accumulator, read where it is needed: as a plain value the compiler copies the
