@@ -15,7 +15,7 @@ from typing import Optional
 import torch
 
 from . import pspo
-from .pspo import _check, _dev, _ptr, _stream
+from .pspo import _dev
 
 TYPE_BF16, TYPE_F32 = 0, 1
 ROPE_INTERLEAVED, QK_NO_NORM = 1, 2
@@ -41,6 +41,28 @@ _SIGNATURES = {
 }
 
 _lib = None
+
+
+# The calls are short next to a Python call's own cost (5 us and up), so a tensor is looked at
+# with the cheap queries first, and pspo._dev runs for what they find wrong, to say what.
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _here(t, dtype, name: str, device: int) -> None:
+    """t: a contiguous tensor of `dtype` on the current device (`device`)."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        _dev(t, dtype, name)
+
+
+def _stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _check(rc: int) -> None:
+    if rc:
+        pspo._check(rc)
 
 
 def load() -> ctypes.CDLL:
@@ -72,12 +94,15 @@ def _type(t: torch.Tensor, name: str) -> int:
 
 def _rows(t: torch.Tensor, N: int, shape, name: str) -> None:
     """t must be [>= N, *shape]."""
-    if t.dim() != 1 + len(shape) or tuple(t.shape[1:]) != tuple(shape) or t.shape[0] < N:
+    have = t.shape if isinstance(t, torch.Tensor) else ()
+    if len(have) != 1 + len(shape) or have[1:] != shape or have[0] < N:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
         raise ValueError(f"{name} must be [>= {N}{''.join(', %d' % s for s in shape)}], got {list(t.shape)}")
 
 
 def _exact(t: torch.Tensor, shape, name: str) -> None:
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
@@ -94,10 +119,10 @@ def _apart(out: torch.Tensor, name: str, *ins) -> None:
             raise ValueError(f"{name} overlaps an input")
 
 
-def _ints(t: Optional[torch.Tensor], n: int, name: str) -> None:
+def _ints(t: Optional[torch.Tensor], n: int, name: str, device: int) -> None:
     if t is None:
         return
-    _dev(t, torch.int32, name)
+    _here(t, torch.int32, name, device)
     if t.dim() != 1 or t.shape[0] < n:
         raise ValueError(f"{name} must be [>= {n}], got {list(t.shape)}")
 
@@ -112,17 +137,16 @@ def _count(N: int) -> int:
 # norms of queries and keys with the position rotation
 # ---------------------------------------------------------------------------
 
-def _heads(t: torch.Tensor, N: int, name: str, like: Optional[torch.Tensor] = None) -> torch.Tensor:
+def _heads(t: torch.Tensor, N: int, name: str, device: int, like: Optional[torch.Tensor] = None) -> torch.Tensor:
     """[>= N, heads, D] on the current device, heads contiguous, any row stride."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{name} must be a tensor [>= N, heads, head_dim]")
     if t.shape[0] < N:
         raise ValueError(f"{name} has fewer than N rows")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, but the calls run on the current device "
-                         f"cuda:{torch.cuda.current_device()}")
+    if t.get_device() != device:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        raise ValueError(f"{name} is on {t.device}, but the calls run on the current device cuda:{device}")
     if like is not None and t.dtype != like.dtype:
         raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
     _, H, D = t.shape
@@ -140,35 +164,43 @@ def _row_stride(t: Optional[torch.Tensor]) -> int:
 
 def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos, interleaved, norm,
                err_flag):
-    _type(q, "q")
-    _heads(q, N, "q")
+    device = torch.cuda.current_device()
+    ty = _type(q, "q")
+    _heads(q, N, "q", device)
     D = q.shape[2]
     if k is not None:
-        _heads(k, N, "k", q)
+        _heads(k, N, "k", device, q)
         if k.shape[2] != D:
             raise ValueError("q and k disagree on the head dimension")
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
-            _dev(w, q.dtype, name)
+            _here(w, q.dtype, name, device)
             _exact(w, (D,), name)
     rot, R = 0, 0
     if inv_freq is not None:
-        _dev(inv_freq, torch.float32, "inv_freq")
+        _here(inv_freq, torch.float32, "inv_freq", device)
         if inv_freq.dim() != 1:
             raise ValueError("inv_freq must be [rot_dim / 2]")
         rot = 2 * inv_freq.shape[0]
-        _ints(positions, N, "positions")
-        if positions is None:
+        if positions is not None:
+            _ints(positions, N, "positions", device)
+            seq_id = cu_seqlens = first_pos = None
+        else:
             if seq_id is None or cu_seqlens is None:
                 raise ValueError("positions, or seq_id and cu_seqlens, must be given")
-            _ints(seq_id, N, "seq_id")
-            _ints(cu_seqlens, 1, "cu_seqlens")
+            _ints(seq_id, N, "seq_id", device)
+            _ints(cu_seqlens, 1, "cu_seqlens", device)
             R = cu_seqlens.shape[0] - 1
-            _ints(first_pos, R, "first_pos")
+            _ints(first_pos, R, "first_pos", device)
+    else:
+        positions = seq_id = cu_seqlens = first_pos = None
     if err_flag is not None:
-        _dev(err_flag, torch.int32, "err_flag")
+        _here(err_flag, torch.int32, "err_flag", device)
     flags = (ROPE_INTERLEAVED if interleaved else 0) | (0 if norm else QK_NO_NORM)
-    return D, rot, R, flags
+    heads = (N, R, q.shape[1], 0 if k is None else k.shape[1], D, rot)
+    ins = (q.data_ptr(), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
+           _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos))
+    return device, ty, D, flags, ins, heads
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq_id=None, cu_seqlens=None,
@@ -184,8 +216,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq
     Returns q and k ([N, H, D] contiguous; k None if there is none).
     """
     N = _count(N)
-    D, rot, R, flags = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos,
-                                  interleaved, norm, err_flag)
+    device, ty, D, flags, ins, heads = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens,
+                                                  first_pos, interleaved, norm, err_flag)
     outs = []
     for name, x, o in (("q_out", q, q_out), ("k_out", k, k_out)):
         if x is None:
@@ -195,15 +227,17 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq
             o = torch.empty((N, x.shape[1], D), dtype=x.dtype, device=x.device)
         else:
             _rows(o, N, (x.shape[1], D), name)
-            _dev(o, x.dtype, name)
-            _apart(o, name, q, k, q_weight, k_weight)
+            _here(o, x.dtype, name, device)
+            _apart(o, name, q, k, q_weight, k_weight, *outs)
         outs.append(o)
-    _check(load().pspo_qk_norm_rope_fwd(
-        _ptr(q), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
-        _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos), N, R, q.shape[1],
-        0 if k is None else k.shape[1], D, rot, float(eps), _type(q, "q"), flags, _ptr(outs[0]), _ptr(outs[1]),
-        _ptr(err_flag), _stream()))
-    return dict(q=outs[0][:N], k=None if outs[1] is None else outs[1][:N])
+    qo, ko = outs
+    _check((_lib or load()).pspo_qk_norm_rope_fwd(*ins, *heads, eps, ty, flags, qo.data_ptr(), _ptr(ko),
+                                                  _ptr(err_flag), _stream(device)))
+    if q_out is not None:
+        qo = qo[:N]
+    if k_out is not None:
+        ko = ko[:N]
+    return dict(q=qo, k=ko)
 
 
 def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq_id=None,
@@ -216,8 +250,8 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int,
     (unless want_weights is False), dq_weight and dk_weight (float32 [D]).
     """
     N = _count(N)
-    D, rot, R, flags = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens, first_pos,
-                                  interleaved, norm, err_flag)
+    device, ty, D, flags, ins, heads = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens,
+                                                  first_pos, interleaved, norm, err_flag)
     if (k is None) != (dk_out is None):
         raise ValueError("k and dk_out must be both given or both None")
     dx = []
@@ -226,22 +260,20 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int,
             dx.append(None)
             continue
         _rows(g, N, (x.shape[1], D), name)
-        _dev(g, x.dtype, name)
+        _here(g, x.dtype, name, device)
         dx.append(torch.empty((N, x.shape[1], D), dtype=x.dtype, device=x.device))
     dw = [torch.empty(D, dtype=torch.float32, device=q.device) if w is not None and want_weights else None
           for w in (q_weight, k_weight)]
-    lib = load()
-    if workspace is None and (dw[0] is not None or dw[1] is not None):
-        need = int(lib.pspo_qk_norm_rope_workspace_bytes(N, D))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    if workspace is not None:
-        _dev(workspace, torch.uint8, "workspace")
+    lib = _lib or load()
+    if workspace is None:
+        if dw[0] is not None or dw[1] is not None:
+            need = lib.pspo_qk_norm_rope_workspace_bytes(N, D)
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    else:
+        _here(workspace, torch.uint8, "workspace", device)
     _check(lib.pspo_qk_norm_rope_bwd(
-        _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight),
-        _ptr(inv_freq), _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos), N, R, q.shape[1],
-        0 if k is None else k.shape[1], D, rot, float(eps), _type(q, "q"), flags, _ptr(dx[0]), _ptr(dx[1]),
-        _ptr(dw[0]), _ptr(dw[1]), _ptr(err_flag), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-        _stream()))
+        dq_out.data_ptr(), _ptr(dk_out), *ins, *heads, eps, ty, flags, dx[0].data_ptr(), _ptr(dx[1]), _ptr(dw[0]),
+        _ptr(dw[1]), _ptr(err_flag), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(device)))
     return dict(dq=dx[0], dk=dx[1], dq_weight=dw[0], dk_weight=dw[1], workspace=workspace)
 
 
@@ -261,25 +293,26 @@ def dropout_add(x, N: int, p: float, seed: int, offset: int = 0, residual: Optio
     the packer's src_row it is the same for every draw of the cutoffs.  Returns [N, d].
     """
     N = _count(N)
+    device = torch.cuda.current_device()
     ty = _type(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be [>= N, d]")
     d = x.shape[1]
     _rows(x, N, (d,), "x")
-    _dev(x, x.dtype, "x")
+    _here(x, x.dtype, "x", device)
     if residual is not None:
         _rows(residual, N, (d,), "residual")
-        _dev(residual, x.dtype, "residual")
-    _ints(row_ids, N, "row_ids")
+        _here(residual, x.dtype, "residual", device)
+    _ints(row_ids, N, "row_ids", device)
     if out is None:
         out = torch.empty((N, d), dtype=x.dtype, device=x.device)
     else:
         _rows(out, N, (d,), "out")
-        _dev(out, x.dtype, "out")
+        _here(out, x.dtype, "out", device)
         _apart(out, "out", x, residual)
-    _check(load().pspo_dropout_add_fwd(_ptr(x), _ptr(residual), _ptr(row_ids), N, d, float(p), seed & _U64_MASK,
-                                       offset & _U64_MASK, ty, _ptr(out), _stream()))
-    return out[:N]
+    _check((_lib or load()).pspo_dropout_add_fwd(x.data_ptr(), _ptr(residual), _ptr(row_ids), N, d, p, seed & _U64_MASK,
+                                                 offset & _U64_MASK, ty, out.data_ptr(), _stream(device)))
+    return out if out.shape[0] == N else out[:N]
 
 
 def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optional[torch.Tensor] = None,
@@ -289,22 +322,24 @@ def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optio
     dy: [>=N, d] bf16 or float32 (e.g. the loss call's d_hidden); the result is of out_dtype (default: dy's).
     """
     N = _count(N)
+    device = torch.cuda.current_device()
     ty = _type(dy, "dy")
     if dy.dim() != 2:
         raise ValueError("dy must be [>= N, d]")
     d = dy.shape[1]
     _rows(dy, N, (d,), "dy")
-    _dev(dy, dy.dtype, "dy")
-    _ints(row_ids, N, "row_ids")
+    _here(dy, dy.dtype, "dy", device)
+    _ints(row_ids, N, "row_ids", device)
     if out is None:
         out = torch.empty((N, d), dtype=out_dtype or dy.dtype, device=dy.device)
     else:
         _rows(out, N, (d,), "out")
-        _dev(out, out_dtype or out.dtype, "out")
+        _here(out, out_dtype or out.dtype, "out", device)
         _apart(out, "out", dy)
-    _check(load().pspo_dropout_bwd(_ptr(dy), _ptr(row_ids), N, d, float(p), seed & _U64_MASK, offset & _U64_MASK, ty,
-                                   _type(out, "out"), _ptr(out), _stream()))
-    return out[:N]
+    _check((_lib or load()).pspo_dropout_bwd(dy.data_ptr(), _ptr(row_ids), N, d, p, seed & _U64_MASK,
+                                             offset & _U64_MASK, ty, _type(out, "out"), out.data_ptr(),
+                                             _stream(device)))
+    return out if out.shape[0] == N else out[:N]
 
 
 # ---------------------------------------------------------------------------
@@ -318,14 +353,15 @@ def _act(act: str) -> int:
 
 
 def _ffn_weights(w_gate, w_up, w_down):
+    device = torch.cuda.current_device()
     if w_gate.dim() != 2:
         raise ValueError("w_gate must be [f, d]")
     f, d = w_gate.shape
     _exact(w_up, (f, d), "w_up")
     _exact(w_down, (d, f), "w_down")
     for name, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
-        _dev(w, torch.bfloat16, name)
-    return d, f
+        _here(w, torch.bfloat16, name, device)
+    return device, d, f
 
 
 def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, preact: bool = False) -> int:
@@ -333,11 +369,12 @@ def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, pr
     return int(load().pspo_gated_ffn_workspace_bytes(N, d, f, flags))
 
 
-def _ffn_workspace(workspace, N, d, f, backward, preact, device):
+def _ffn_workspace(workspace, N, d, f, flags, like, device):
     if workspace is None:
-        workspace = torch.empty(max(gated_ffn_workspace_bytes(N, d, f, backward, preact), 256), dtype=torch.uint8,
-                                device=device)
-    return _dev(workspace, torch.uint8, "workspace")
+        need = (_lib or load()).pspo_gated_ffn_workspace_bytes(N, d, f, flags)
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
+    _here(workspace, torch.uint8, "workspace", device)
+    return workspace
 
 
 def gated_ffn(x, w_gate, w_up, w_down, N: int, act: str = "silu", keep: bool = False,
@@ -349,20 +386,21 @@ def gated_ffn(x, w_gate, w_up, w_down, N: int, act: str = "silu", keep: bool = F
     """
     N = _count(N)
     kind = _act(act)
-    d, f = _ffn_weights(w_gate, w_up, w_down)
+    device, d, f = _ffn_weights(w_gate, w_up, w_down)
     _rows(x, N, (d,), "x")
-    _dev(x, torch.bfloat16, "x")
+    _here(x, torch.bfloat16, "x", device)
     if out is None:
         out = torch.empty((N, d), dtype=torch.bfloat16, device=x.device)
     else:
         _rows(out, N, (d,), "out")
-        _dev(out, torch.bfloat16, "out")
+        _here(out, torch.bfloat16, "out", device)
         _apart(out, "out", x, w_gate, w_up, w_down)
     pre = torch.empty((N, 2 * f), dtype=torch.float32, device=x.device) if keep else None
-    workspace = _ffn_workspace(workspace, N, d, f, False, False, x.device)
-    _check(load().pspo_gated_ffn_fwd(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), N, d, f, kind, _ptr(out),
-                                     _ptr(pre), _ptr(workspace), workspace.numel(), _stream()))
-    return dict(y=out[:N], preact=pre, workspace=workspace)
+    workspace = _ffn_workspace(workspace, N, d, f, 0, x, device)
+    _check((_lib or load()).pspo_gated_ffn_fwd(
+        x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), N, d, f, kind, out.data_ptr(), _ptr(pre),
+        workspace.data_ptr(), workspace.numel(), _stream(device)))
+    return dict(y=out if out.shape[0] == N else out[:N], preact=pre, workspace=workspace)
 
 
 def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact: Optional[torch.Tensor] = None,
@@ -375,13 +413,13 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact
     """
     N = _count(N)
     kind = _act(act)
-    d, f = _ffn_weights(w_gate, w_up, w_down)
+    device, d, f = _ffn_weights(w_gate, w_up, w_down)
     for name, t in (("dy", dy), ("x", x)):
         _rows(t, N, (d,), name)
-        _dev(t, torch.bfloat16, name)
+        _here(t, torch.bfloat16, name, device)
     if preact is not None:
         _rows(preact, N, (2 * f,), "preact")
-        _dev(preact, torch.float32, "preact")
+        _here(preact, torch.float32, "preact", device)
     shapes = ((f, d), (f, d), (d, f))
     if dw is None:
         if accumulate:
@@ -393,12 +431,14 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact
             if ty != _type(dw[0], name):
                 raise TypeError("the weight gradients must have one dtype")
             _exact(t, s, name)
-            _dev(t, t.dtype, name)
+            _here(t, t.dtype, name, device)
             _apart(t, name, dy, x, w_gate, w_up, w_down, preact, *dw[:i])
     flags = (FFN_DW_F32 if dw[0].dtype == torch.float32 else 0) | (pspo.PSPO_ACCUMULATE_DW if accumulate else 0)
     dx = torch.empty((N, d), dtype=torch.bfloat16, device=x.device)
-    workspace = _ffn_workspace(workspace, N, d, f, True, preact is not None, x.device)
-    _check(load().pspo_gated_ffn_bwd(_ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(preact), N, d, f,
-                                     kind, flags, _ptr(dx), _ptr(dw[0]), _ptr(dw[1]), _ptr(dw[2]), _ptr(workspace),
-                                     workspace.numel(), _stream()))
+    need = FFN_BACKWARD | (FFN_PREACT if preact is not None else 0)
+    workspace = _ffn_workspace(workspace, N, d, f, need, x, device)
+    _check((_lib or load()).pspo_gated_ffn_bwd(
+        dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), _ptr(preact), N, d, f,
+        kind, flags, dx.data_ptr(), dw[0].data_ptr(), dw[1].data_ptr(), dw[2].data_ptr(), workspace.data_ptr(),
+        workspace.numel(), _stream(device)))
     return dict(dx=dx, dw_gate=dw[0], dw_up=dw[1], dw_down=dw[2], workspace=workspace)
