@@ -15,6 +15,7 @@
 
 #include "pspo_layer.h"
 #include "rowgemm.h"
+#include "skinny.h"
 #include "vec8.h"
 
 namespace pspo {
@@ -547,6 +548,57 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsign
   return PSPO_OK;
 }
 
+// ---- few tokens -----------------------------------------------------------------------
+struct SkinnyGateUp {
+  uint16_t* h;
+  float* pre;
+  int f, act;
+  __device__ __forceinline__ void operator()(int m, int n, const float (&s)[2]) const {
+    if (pre != nullptr) {
+      pre[(int64_t)n * 2 * f + m] = s[0];
+      pre[(int64_t)n * 2 * f + f + m] = s[1];
+    }
+    h[(int64_t)n * f + m] = (uint16_t)pack_bf16(act_value(s[0], act) * s[1], 0.f);
+  }
+};
+struct SkinnyStore {
+  uint16_t* y;
+  int ld;
+  __device__ __forceinline__ void operator()(int m, int n, const float (&s)[1]) const {
+    y[(int64_t)n * ld + m] = (uint16_t)pack_bf16(s[0], 0.f);
+  }
+};
+
+// Whether a forward of N tokens goes by these kernels.  They read every token's rows again for
+// each 16 rows of the weights, the 128 x 128 tiles write and join slabs instead: us a call, this
+// way / tiles, on 3 d f weights: d = 3584, f = 14336 (308 MB) N = 16 89 / 97, 24 105 / 97; 1536,
+// 6144 (57 MB) N = 32 34 / 38, 48 42 / 38; 512, 1344 (4 MB) N = 64 15 / 19.
+bool few_tokens(int64_t N, int64_t d, int64_t f) {
+  return N <= 16 || (N <= kSkinnyTokens && (N - 16) * (6 * d * f) <= int64_t(1200) << 20);
+}
+
+// Waves of a work-group: enough that the chip holds some 4,096, at most one for each
+// step of K and 64 KB of sums.
+template <int kMats, class Epi>
+int skinny(const SkinnyArgs& a, const Epi& epi, const char* name, hipStream_t stream) {
+  const int groups = (a.M + 15) / 16, blocks = (a.N + 15) / 16, steps = (a.K + kSkinnyK - 1) / kSkinnyK;
+  int waves = 1;
+  while (waves < (blocks > 1 ? 8 : 16) && waves * 2 <= steps && (int64_t)groups * waves < 4096 &&
+         waves * 2 * kMats * blocks * 1024 <= 65536)
+    waves *= 2;
+  const size_t lds = (size_t)waves * kMats * blocks * 1024;
+#define PSPO_SKINNY(NB, AHEAD)   hipLaunchKernelGGL((skinny_kernel<kMats, NB, AHEAD, Epi>), dim3(groups), dim3(64 * waves), lds, stream, a, epi)
+  switch (blocks) {
+    case 1: PSPO_SKINNY(1, 4); break;
+    case 2: PSPO_SKINNY(2, 2); break;
+    case 3: PSPO_SKINNY(3, 2); break;
+    default: PSPO_SKINNY(4, 1); break;
+  }
+#undef PSPO_SKINNY
+  PSPO_LAUNCHED(name, stream);
+  return PSPO_OK;
+}
+
 // Workspace layout of one call.
 struct Space {
   int64_t h, dgu, pre, slab, total;
@@ -561,12 +613,12 @@ Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
   };
   s.h = take(N * f * 2);
   int64_t slab = 0;
-  if (!backward || !kept) slab = slab_bytes(2 * f, N, (int)d, 1);
+  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, 1);
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
     slab = std::max({slab, slab_bytes(f, N, (int)d, 1), plan_backward(N, d, f).slab_bytes});
-  } else {
+  } else if (!few_tokens(N, d, f)) {
     slab = std::max(slab, slab_bytes(d, N, (int)f, 1));
   }
   s.slab = take(slab);
@@ -598,6 +650,8 @@ RowShape shape(const uint16_t* a, const uint16_t* a2, int64_t lda, int rows_a, c
 // h (and the pre-activations, if `pre`) of the first N tokens.
 int gate_up(const uint16_t* x, const uint16_t* wg, const uint16_t* wu, int N, int d, int f, int act, uint16_t* h,
             float* pre, float* slab, hipStream_t stream) {
+  if (few_tokens(N, d, f))
+    return skinny<2>(SkinnyArgs{{wg, wu}, x, f, N, d}, SkinnyGateUp{h, pre, f, act}, "ffn_gate_up", stream);
   JoinArgs j{};
   j.which = kJoinGateUp;
   j.gu = EpiGateUp{h, pre, f, N, act};
@@ -637,6 +691,8 @@ int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t
   uint16_t* h = reinterpret_cast<uint16_t*>(ws + s.h);
   float* slab = reinterpret_cast<float*>(ws + s.slab);
   if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, preact, slab, stream)) return rc;
+  if (few_tokens(N, d, f))
+    return skinny<1>(SkinnyArgs{{w_down, w_down}, h, d, N, f}, SkinnyStore{y, d}, "ffn_down", stream);
   const Out o{y, y, d, N, N, false, false};
   return product<false, false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, bf16_of(o), join_of(o), slab,
                                       "ffn_down", stream);
