@@ -120,12 +120,14 @@ struct EpiF32 {
 // writes 1 KB in one piece.  slab_piece says where four entries lie.
 struct EpiSlab {
   float* base;
+  int N;
   template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int, int, int wm, int wn, int lane, unsigned char*,
+  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int, int tn, int wm, int wn, int lane, unsigned char*,
                                         int slab) const {
     float* to = base + (int64_t)slab * (1024 * BM * BN) + (wn * BN * 2 * BM + wm * BM) * 256 + lane * 4;
     repeat<BN>([&](auto jc) {
       constexpr int j = decltype(jc)::value;
+      if (((tn * 2 + wn) * BN + j) * 16 >= N) return;   // nobody joins columns that do not exist
 #pragma unroll
       for (int i = 0; i < BM; ++i) {
         f32x4 v;
@@ -263,14 +265,14 @@ enum : int { kJoinStore, kJoinGateUp, kJoinDh };
 struct JoinArgs {
   const float* slab;
   RowShape g;
-  int tile, which;
+  int tile, tile_n, which;
   EpiBf16 bf16;   // kJoinStore in bf16 ...
   EpiF32 f32;     // ... or float32 (out set)
   EpiGateUp gu;
   EpiDh dh;
 };
 __device__ __forceinline__ Vec8 join8(const JoinArgs& a, int index, int m, int n) {
-  const int64_t size = (int64_t)a.tile * a.tile;
+  const int64_t size = (int64_t)a.tile * a.tile_n;
   const int at = slab_piece(a.tile, m, n);   // entries m .. m + 3; the next four lie 64 floats on (m % 8 == 0)
   Vec8 s{};
   for (int p = 0; p < a.g.parts; ++p) {
@@ -291,8 +293,8 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(JoinArgs a) {
   const int width = a.which == kJoinGateUp ? a.tile / 2 : a.tile;
   const int w = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
   const int row = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
-  if (row >= a.tile) return;
-  const int64_t n = (int64_t)tn * a.tile + row;
+  if (row >= a.tile_n) return;
+  const int64_t n = (int64_t)tn * a.tile_n + row;
   if (a.which == kJoinStore) {
     const int64_t m = (int64_t)tm * a.tile + m0;
     if (n >= a.bf16.N || m >= a.bf16.M) return;
@@ -349,28 +351,31 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(JoinArgs a) {
 
 // ---- plan ---------------------------------------------------------------------------
 // How a product of M x N entries over nk stages is covered: tiles of 256 x 256 (one
-// work-group to a CU) or 128 x 128 (two), the first `whole` of them launched as they are
-// and the rest in `parts` parts of K (parts = 1: all are whole).
+// work-group to a CU), 128 x 128 (two) or 128 x 64 (three), the first `whole` of them launched
+// as they are and the rest in `parts` parts of K (parts = 1: all are whole).
 struct Plan {
-  int tile, tiles_m, tiles_n, whole, parts;
+  int tile, tile_n, tiles_m, tiles_n, whole, parts;
   double us;
 };
 constexpr int64_t kSlabBytes = int64_t(256) << 20;   // most that the parts of one product take
 
-// The cover of least estimated time: a stage of a round takes 1.45 us (256), 1.1 us (128, two
-// work-groups to a CU) or 0.7 us (one), each tile 20 us (10) beyond its stages, the parts'
-// slabs are written and read at 4.5 TB/s, and a further launch with its join takes 8 us.
-Plan plan_tile(int64_t M, int64_t N, int nk, int tile) {
+// The cover of least estimated time: a stage of a full round takes 1.45, 1.1 or 0.9 us, one
+// with a work-group to a CU 0.7 us (128 x 128) or 0.5 us, each tile 20, 10 or 6 us beyond its
+// stages; the slabs of the parts are written and read at 4.5 TB/s, and a further launch with its
+// join takes 8 us.
+Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n) {
   Plan p{};
   p.tile = tile;
+  p.tile_n = tile_n;
   p.tiles_m = (int)((M + tile - 1) / tile);
-  p.tiles_n = (int)((N + tile - 1) / tile);
-  const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : 512;
-  const double extra = tile == 256 ? 20 : 10;
+  p.tiles_n = (int)((N + tile_n - 1) / tile_n);
+  const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : tile_n == 128 ? 512 : 768;
+  const double extra = tile == 256 ? 20 : tile_n == 128 ? 10 : 6;
+  const double stage = tile == 256 ? 1.45 : tile_n == 128 ? 1.1 : 0.9;
+  const double single = tile == 256 ? 1.45 : tile_n == 128 ? 0.7 : 0.5;
   auto time = [&](int64_t groups, int stages, double per_tile) {
-    const int64_t turns = (groups + slots - 1) / slots;
-    const bool alone = groups - (turns - 1) * slots <= 256;
-    const double stage = tile == 256 ? 1.45 : 1.1, last = tile == 128 && alone ? 0.7 : stage;
+    const int64_t turns = (groups + slots - 1) / slots, rest = groups - (turns - 1) * slots;
+    const double last = rest <= 256 ? single : stage;
     return (double)(turns - 1) * (stages * stage + per_tile) + stages * last + per_tile;
   };
   const int64_t before = (total - 1) / slots * slots, rest = total - before;   // the last round's tiles
@@ -378,9 +383,11 @@ Plan plan_tile(int64_t M, int64_t N, int nk, int tile) {
   p.parts = 1;
   p.us = time(total, nk, extra);
   const double start = before ? time(before, nk, extra) : 0.0;
-  const int64_t bytes = (int64_t)tile * tile * 4;
+  const int64_t bytes = (int64_t)tile * tile_n * 4;
+  // what a part writes: the columns that exist
+  const double written = (double)tile * (double)std::min<int64_t>(N, tile_n) * 4;
   for (int s = 2; s <= 32 && s * 4 <= nk && rest * s * bytes <= kSlabBytes; ++s) {
-    const double us = start + time(rest * s, (nk + s - 1) / s, extra / 2) + 8 + (double)(rest * s * bytes) * 2 / 4.5e6;
+    const double us = start + time(rest * s, (nk + s - 1) / s, extra / 2) + 8 + (double)(rest * s) * written * 2 / 4.5e6;
     if (us < p.us) {
       p.us = us;
       p.whole = (int)before;
@@ -389,21 +396,35 @@ Plan plan_tile(int64_t M, int64_t N, int nk, int tile) {
   }
   return p;
 }
-Plan plan_of(int64_t M, int64_t N, int nk) {
-  const Plan big = plan_tile(M, N, nk, 256), small = plan_tile(M, N, nk, 128);
-  return big.us <= small.us ? big : small;
+// narrow: 128 x 64 is to be had (A K-inner), for products of few columns.
+Plan plan_of(int64_t M, int64_t N, int nk, bool narrow) {
+  Plan best = plan_tile(M, N, nk, 128, 128);
+  const Plan big = plan_tile(M, N, nk, 256, 256);
+  if (big.us <= best.us) best = big;
+  if (narrow && N <= 64) {
+    const Plan thin = plan_tile(M, N, nk, 128, 64);
+    if (thin.us < best.us) best = thin;
+  }
+  return best;
 }
-int64_t slab_bytes(int64_t M, int64_t N, int K, int segs) {
+int64_t slab_bytes(int64_t M, int64_t N, int K, int segs, bool narrow) {
   if (M == 0 || N == 0) return 0;
-  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK * segs);
+  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK * segs, narrow);
   if (p.parts == 1) return 0;
-  return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile * 4;
+  return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile_n * 4;
 }
 
 template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-int launch(const RowShape& g, int tile, const Epi& epi, const char* name, hipStream_t stream) {
+int launch(const RowShape& g, const Plan& p, const Epi& epi, const char* name, hipStream_t stream) {
   const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
-  if (tile == 256)
+  if constexpr (!kOuterA) {
+    if (p.tile_n == 64) {
+      hipLaunchKernelGGL((row_gemm_kernel<4, 2, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
+      PSPO_LAUNCHED(name, stream);
+      return PSPO_OK;
+    }
+  }
+  if (p.tile == 256)
     hipLaunchKernelGGL((row_gemm_kernel<8, 8, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
   else
     hipLaunchKernelGGL((row_gemm_kernel<4, 4, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
@@ -411,7 +432,7 @@ int launch(const RowShape& g, int tile, const Epi& epi, const char* name, hipStr
   return PSPO_OK;
 }
 
-int join_parts(JoinArgs join, const RowShape& g, int tile, const float* slab, hipStream_t stream);
+int join_parts(JoinArgs join, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream);
 
 // One product with its epilogue: the whole tiles, then the rest in parts and their join
 // (`join` holds the same epilogue).
@@ -419,7 +440,7 @@ template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
 int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, float* slab, const char* name,
             hipStream_t stream) {
   if (M == 0 || N == 0) return PSPO_OK;
-  const Plan p = plan_of(M, N, (g.K + kRowK - 1) / kRowK * g.segs);
+  const Plan p = plan_of(M, N, (g.K + kRowK - 1) / kRowK * g.segs, !kOuterA);
   const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
   PSPO_REQUIRE(total < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
   g.tiles_m = p.tiles_m;
@@ -428,22 +449,23 @@ int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, flo
   g.count = p.whole;
   g.parts = 1;
   if (g.count > 0)
-    if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p.tile, epi, name, stream)) return rc;
+    if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p, epi, name, stream)) return rc;
   g.tile0 = p.whole;
   g.count = (int)(total - p.whole);
   if (g.count == 0) return PSPO_OK;
   g.parts = p.parts;
-  if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p.tile, EpiSlab{slab}, name, stream)) return rc;
-  return join_parts(join, g, p.tile, slab, stream);
+  if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p, EpiSlab{slab, (int)N}, name, stream)) return rc;
+  return join_parts(join, g, p.tile, p.tile_n, slab, stream);
 }
 
 // The join of a product's slabs, after `launch`.
-int join_parts(JoinArgs join, const RowShape& g, int tile, const float* slab, hipStream_t stream) {
+int join_parts(JoinArgs join, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
   join.slab = slab;
   join.g = g;
   join.tile = tile;
+  join.tile_n = tile_n;
   const int chunks = (join.which == kJoinGateUp ? tile / 2 : tile) / 8;
-  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(tile * chunks / 256)), dim3(256), 0, stream,
+  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(tile_n * chunks / 256)), dim3(256), 0, stream,
                      join);
   PSPO_LAUNCHED("ffn_join_kernel", stream);
   return PSPO_OK;
@@ -533,7 +555,7 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsign
     jobs.blocks[i] = (int)(round_up(tiles, kNumXcd) * p.parts[i]);
     blocks += jobs.blocks[i];
     jobs.epi[i] = EpiAny{bf16_of(o[i]), f32_of(o[i]),
-                         EpiSlab{p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr}};
+                         EpiSlab{p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
   }
   PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
   if (p.tile == 256)
@@ -543,7 +565,7 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsign
   PSPO_LAUNCHED("ffn_gradients", stream);
   for (int i = 0; i < 3; ++i)
     if (p.parts[i] > 1 && jobs.g[i].count > 0)
-      if (int rc = join_parts(join_of(o[i]), jobs.g[i], p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
+      if (int rc = join_parts(join_of(o[i]), jobs.g[i], p.tile, p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
         return rc;
   return PSPO_OK;
 }
@@ -570,11 +592,12 @@ struct SkinnyStore {
 };
 
 // Whether a forward of N tokens goes by these kernels.  They read every token's rows again for
-// each 16 rows of the weights, the 128 x 128 tiles write and join slabs instead: us a call, this
-// way / tiles, on 3 d f weights: d = 3584, f = 14336 (308 MB) N = 16 89 / 97, 24 105 / 97; 1536,
-// 6144 (57 MB) N = 32 34 / 38, 48 42 / 38; 512, 1344 (4 MB) N = 64 15 / 19.
+// each 16 rows of the weights, the 128 x 64 tiles write and join slabs instead: us a call, this
+// way / tiles, on 6 d f bytes of weights: d = 3584, f = 14336 (308 MB) N = 1 65 / 84, 16 90 / 84,
+// 24 105 / 84; 1536, 6144 (57 MB) N = 16 27 / 33, 32 33 / 34, 48 42 / 34; 512, 1344 (4 MB)
+// N = 64 15 / 19.
 bool few_tokens(int64_t N, int64_t d, int64_t f) {
-  return N <= 16 || (N <= kSkinnyTokens && (N - 16) * (6 * d * f) <= int64_t(1200) << 20);
+  return N <= kSkinnyTokens && (N - 12) * (6 * d * f) <= int64_t(900) << 20;
 }
 
 // Waves of a work-group: enough that the chip holds some 4,096, at most one for each
@@ -613,13 +636,13 @@ Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
   };
   s.h = take(N * f * 2);
   int64_t slab = 0;
-  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, 1);
+  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, 1, true);
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab, slab_bytes(f, N, (int)d, 1), plan_backward(N, d, f).slab_bytes});
+    slab = std::max({slab, slab_bytes(f, N, (int)d, 1, false), plan_backward(N, d, f).slab_bytes});
   } else if (!few_tokens(N, d, f)) {
-    slab = std::max(slab, slab_bytes(d, N, (int)f, 1));
+    slab = std::max(slab, slab_bytes(d, N, (int)f, 1, true));
   }
   s.slab = take(slab);
   s.total = at;

@@ -335,7 +335,7 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
 }
 
 template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : BM * BN > 8 ? 2 : 3)))
 void row_gemm_kernel(RowShape g, Epi epi) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
   row_gemm_tile<BM, BN, kOuterA, kOuterB, kPairA>(g, epi, blockIdx.x, blockIdx.y, lds);
@@ -353,7 +353,7 @@ struct RowJobs {
   int blocks[kJobs];
 };
 template <int BM, int BN, class Epi>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : 2)))
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : BM * BN > 8 ? 2 : 3)))
 void row_jobs_kernel(RowJobs<Epi> jobs) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
   int bid = blockIdx.x;
