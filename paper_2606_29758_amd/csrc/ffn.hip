@@ -12,6 +12,7 @@
 // enters the gradient twice (through act and act').
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "pspo_layer.h"
 #include "rowgemm.h"
@@ -23,7 +24,12 @@ namespace {
 
 // act(g) = g s(a(g)), s the logistic function: a(g) = g (silu), or
 // 2 sqrt(2/pi) (g + 0.044715 g^3) (gelu_tanh, as 1 + tanh(v) = 2 s(2 v)).
-__device__ __forceinline__ float logistic(float a) { return 1.f / (1.f + __expf(-a)); }
+// The exponential and the reciprocal are the instructions (both good to an ulp or so of
+// float32): with an IEEE division the dh product of 8192 tokens, one wave to a SIMD in its
+// epilogue, took 992 us instead of 956.
+__device__ __forceinline__ float logistic(float a) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f));
+}
 
 constexpr float kGelu = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 
@@ -46,307 +52,198 @@ __device__ __forceinline__ void act_both(float g, int kind, float& a, float& da)
   da = s + b * s * (1.f - s) * (kGelu * (1.f + 0.134145f * b * b));
 }
 
-__device__ __forceinline__ u32x2 pack4(const float* v) { return u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
-
 // ---- epilogues -----------------------------------------------------------------
-// The tile goes out in steps of kCols columns (tokens) through the wave's LDS, so
-// that every store writes whole lines of one row.
-constexpr int kCols = 16;
+// What becomes of eight entries (m .. m + 7, n) of a product; the same for a tile's
+// accumulators (apply) and for the joined sums of its K parts (ffn_join_kernel).  Stores go past
+// the caches: there are far more of them than the caches hold until the next kernel reads them
+// (dh product 1.06 -> 0.99 ms at 8192 tokens, d = 3584, f = 14336).
+struct Nothing {};
 
-// C(m, n) -> out[n * ld + m] in bf16; rows n >= split belong to a second matrix.
-struct EpiBf16 {
-  uint16_t *out, *out2;
+__device__ __forceinline__ void put_f32(float* to, const f32x4* v) {
+  // through the caches: the two stores of a lane fill the same lines in turn
+  reinterpret_cast<f32x4*>(to)[0] = v[0];
+  reinterpret_cast<f32x4*>(to)[1] = v[1];
+}
+__device__ __forceinline__ void put_bf16(uint16_t* to, const float* v) {
+  u32x4 p;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+  __builtin_nontemporal_store(p, reinterpret_cast<u32x4*>(to));
+}
+
+// C(m, n) -> out[n * ld + m], bf16 or float32 (or added to it); rows n >= split belong to a
+// second matrix.
+struct EpiStore {
+  static constexpr bool kPair = false;
+  void *out, *out2;
   int64_t ld;
-  int M, N, split;
-  template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char* lds, int) const {
-    constexpr int kRow = BM * 32;
-    const int m0 = (tm * 2 + wm) * BM * 16;
-    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
-      constexpr int j = decltype(jc)::value;
-#pragma unroll
-      for (int i = 0; i < BM; ++i) {
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
-        *reinterpret_cast<u32x2*>(lds + (lane & 15) * (kRow + 16) + i * 32 + (lane >> 4) * 8) = pack4(v);
+  int M, N, split, f32, add;
+  using Fetched = Nothing;
+  __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return {}; }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, Nothing) const {
+    if (n >= N || m >= M) return;   // M % 8 == 0
+    void* base = n < split ? out : out2;
+    const int64_t at = (n < split ? n : n - split) * ld + m;
+    if (f32) {
+      float* to = static_cast<float*>(base) + at;
+      f32x4 s[2] = {v[0], v[1]};
+      if (add) {
+        s[0] += reinterpret_cast<const f32x4*>(to)[0];
+        s[1] += reinterpret_cast<const f32x4*>(to)[1];
       }
-      wave_lds_fence();
-      constexpr int kPer = kRow / 16;
-#pragma unroll
-      for (int x = 0; x < kCols * kPer; x += 64) {
-        const int r = (x + lane) / kPer, c = (x + lane) % kPer * 8;
-        const int n = ((tn * 2 + wn) * BN + j) * 16 + r;
-        if (n < N && m0 + c < M) {
-          uint16_t* row = n < split ? out + (int64_t)n * ld : out2 + (int64_t)(n - split) * ld;
-          *reinterpret_cast<u32x4*>(row + m0 + c) = *reinterpret_cast<const u32x4*>(lds + r * (kRow + 16) + c * 2);
-        }
-      }
-      wave_lds_fence();
-    });
+      put_f32(to, s);
+    } else {
+      put_bf16(static_cast<uint16_t*>(base) + at, reinterpret_cast<const float*>(v));
+    }
   }
 };
 
-// C(m, n) -> out[n * ld + m] in float32, or added to it.
-struct EpiF32 {
-  float *out, *out2;
-  int64_t ld;
-  int M, N, split, add;
-  template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char*, int) const {
-    const int m0 = (tm * 2 + wm) * BM * 16 + (lane >> 4) * 4;
-    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
-      constexpr int j = decltype(jc)::value;
-      const int n = ((tn * 2 + wn) * BN + j) * 16 + (lane & 15);
-      float* row = n < split ? out + (int64_t)n * ld : out2 + (int64_t)(n - split) * ld;
+// Row blocks in pairs (gate, up): h[n][m] = act(g) u, and the pre-activations if kept.
+struct EpiGateUp {
+  static constexpr bool kPair = true;
+  uint16_t* h;
+  float* pre;     // [N][2 f] or NULL
+  int f, N, act;
+  using Fetched = Nothing;
+  __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return {}; }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, Nothing) const {
+    if (n >= N || m >= f) return;
+    if (pre != nullptr) {
+      float* row = pre + n * 2 * f + m;
+      put_f32(row, v);
+      put_f32(row + f, v + 2);
+    }
+    const float *g = reinterpret_cast<const float*>(v), *u = g + 8;
+    float o[8];
 #pragma unroll
-      for (int i = 0; i < BM; ++i) {
-        f32x4 v;
+    for (int k = 0; k < 8; ++k) o[k] = act_value(g[k], act) * u[k];
+    put_bf16(h + n * f + m, o);
+  }
+};
+
+// C(m, n) = dh: dgu[n] = (dh u act'(g), dh act(g)), h[n] = act(g) u.
+struct EpiDh {
+  static constexpr bool kPair = false;
+  const float* pre;   // [N][2 f]
+  uint16_t *dgu, *h;  // [N][2 f], [N][f]
+  int f, N, act;
+  struct Fetched {
+    f32x4 g[2], u[2];
+  };
+  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t m) const {
+    Fetched x{};
+    if (n < N && m < f) {
+      const f32x4* row = reinterpret_cast<const f32x4*>(pre + n * 2 * f + m);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
-        if (n < N && m0 + i * 16 < M) {   // M % 8 == 0
-          f32x4* p = reinterpret_cast<f32x4*>(row + m0 + i * 16);
-          *p = add ? *p + v : v;
-        }
+      for (int k = 0; k < 2; ++k) {
+        x.g[k] = __builtin_nontemporal_load(row + k);
+        x.u[k] = __builtin_nontemporal_load(row + f / 4 + k);
       }
-    });
+    }
+    return x;
+  }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, const Fetched& x) const {
+    if (n >= N || m >= f) return;
+    float dg[8], du[8], hv[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float a, da;
+      act_both(x.g[k / 4][k % 4], act, a, da);
+      const float dh = v[k / 4][k % 4], u = x.u[k / 4][k % 4];
+      dg[k] = dh * u * da;
+      du[k] = dh * a;
+      hv[k] = a * u;
+    }
+    uint16_t* row = dgu + n * 2 * f + m;
+    put_bf16(row, dg);
+    put_bf16(row + f, du);
+    put_bf16(h + n * f + m, hv);
   }
 };
 
 // A K part's whole tile in float32 to slab number `slab`: the 16 x 16 blocks one after
 // another (those of a column of blocks together), each as its lanes hold it, so that a store
 // writes 1 KB in one piece.  slab_piece says where four entries lie.
-struct EpiSlab {
+struct Slab {
   float* base;
   int N;
-  template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int, int tn, int wm, int wn, int lane, unsigned char*,
-                                        int slab) const {
-    float* to = base + (int64_t)slab * (1024 * BM * BN) + (wn * BN * 2 * BM + wm * BM) * 256 + lane * 4;
-    repeat<BN>([&](auto jc) {
-      constexpr int j = decltype(jc)::value;
-      if (((tn * 2 + wn) * BN + j) * 16 >= N) return;   // nobody joins columns that do not exist
-#pragma unroll
-      for (int i = 0; i < BM; ++i) {
-        f32x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
-        *reinterpret_cast<f32x4*>(to + (j * 2 * BM + i) * 256) = v;
-      }
-    });
-  }
 };
+template <int BM, int BN>
+__device__ __forceinline__ void put_slab(const f32x4 (&acc)[BM][BN], int tn, int wm, int wn, int lane, int slab,
+                                         const Slab& s) {
+  float* to = s.base + (int64_t)slab * (1024 * BM * BN) + (wn * BN * 2 * BM + wm * BM) * 256 + lane * 4;
+  repeat<BN>([&](auto jc) {
+    constexpr int j = decltype(jc)::value;
+    if (((tn * 2 + wn) * BN + j) * 16 >= s.N) return;   // nobody joins columns that do not exist
+#pragma unroll
+    for (int i = 0; i < BM; ++i) {
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
+      *reinterpret_cast<f32x4*>(to + (j * 2 * BM + i) * 256) = v;
+    }
+  });
+}
 // Offset of entries (m .. m + 3, n) of a tile of `tile` rows, m % 4 == 0.
 __device__ __forceinline__ int slab_piece(int tile, int m, int n) {
   return ((n >> 4) * (tile >> 4) + (m >> 4)) * 256 + (((m >> 2) & 3) * 16 + (n & 15)) * 4;
 }
 
-// One of the three, by what the plan gave the product.
-struct EpiAny {
-  EpiBf16 bf16;
-  EpiF32 f32;     // used if out is set
-  EpiSlab slab;   // used if base is set
+// The epilogue of a launch: slabs where the tiles are parts, else `op`.
+template <class Op>
+struct Epi {
+  Op op;
+  Slab slab;
   template <int BM, int BN>
   __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char* lds, int slab_index) const {
-    if (slab.base != nullptr) slab.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
-    else if (f32.out != nullptr) f32.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
-    else bf16.apply(acc, tm, tn, wm, wn, lane, lds, slab_index);
-  }
-};
-
-// Row blocks in pairs (gate, up): h[n][j] = act(g) u, and the pre-activations if kept.
-struct EpiGateUp {
-  uint16_t* h;
-  float* pre;     // [N][2 f] or NULL
-  int f, N, act;
-  template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char* lds, int) const {
-    constexpr int kRow = BM * 16, kOne = kCols * (kRow + 16);   // BM * 8 entries of h a token
-    constexpr int kRow4 = 2 * kRow, kOne4 = kCols * (kRow4 + 16);
-    const int m0 = (tm * 2 + wm) * BM * 8;
-    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
-      constexpr int j = decltype(jc)::value;
-      const int n0 = ((tn * 2 + wn) * BN + j) * 16;
-#pragma unroll
-      for (int i = 0; i < BM; i += 2) {
-        f32x4 g, u;
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          g[r] = acc_read(acc[i][j][r]);
-          u[r] = acc_read(acc[i + 1][j][r]);
-          v[r] = act_value(g[r], act) * u[r];
-        }
-        const int at = i * 8 + (lane >> 4) * 4;   // entry of the token's row
-        *reinterpret_cast<u32x2*>(lds + (lane & 15) * (kRow + 16) + at * 2) = pack4(v);
-        if (pre != nullptr) {
-          unsigned char* p = lds + kOne + (lane & 15) * (kRow4 + 16) + at * 4;
-          *reinterpret_cast<f32x4*>(p) = g;
-          *reinterpret_cast<f32x4*>(p + kOne4) = u;
-        }
-      }
-      wave_lds_fence();
-      put_rows<kRow, kCols>(lds, reinterpret_cast<unsigned char*>(h + (int64_t)n0 * f + m0), (int64_t)f * 2, N - n0,
-                            (f - m0) * 2, lane);
-      if (pre != nullptr) {
-        unsigned char* to = reinterpret_cast<unsigned char*>(pre + (int64_t)n0 * 2 * f + m0);
-        put_rows<kRow4, kCols>(lds + kOne, to, (int64_t)f * 8, N - n0, (f - m0) * 4, lane);
-        put_rows<kRow4, kCols>(lds + kOne + kOne4, to + (int64_t)f * 4, (int64_t)f * 8, N - n0, (f - m0) * 4, lane);
-      }
-      wave_lds_fence();
-    });
-  }
-};
-
-// C(j, n) = dh: dgu[n] = (dh u act'(g), dh act(g)), h[n] = act(g) u.
-struct EpiDh {
-  const float* pre;   // [N][2 f]
-  uint16_t *dgu, *h;  // [N][2 f], [N][f]
-  int f, N, act;
-  template <int BM, int BN>
-  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
-                                        unsigned char* lds, int) const {
-    constexpr int kRow = BM * 32, kOne = kCols * (kRow + 16);
-    const int m0 = (tm * 2 + wm) * BM * 16;
-    f32x4 g[2][BM], u[2][BM];   // pre-activations of this column of blocks and of the next
-    auto fetch = [&](int j, f32x4* gj, f32x4* uj) {
-      const int n = ((tn * 2 + wn) * BN + j) * 16 + (lane & 15);
-      const float* row = pre + (int64_t)n * 2 * f + m0 + (lane >> 4) * 4;
-#pragma unroll
-      for (int i = 0; i < BM; ++i) {
-        gj[i] = uj[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (n < N && m0 + i * 16 + (lane >> 4) * 4 < f) {
-          gj[i] = *reinterpret_cast<const f32x4*>(row + i * 16);
-          uj[i] = *reinterpret_cast<const f32x4*>(row + f + i * 16);
-        }
-      }
-    };
-    fetch(0, g[0], u[0]);
-    repeat<BN>([&](auto jc) {   // constant indices into the accumulators, whatever the unroller decides
-      constexpr int j = decltype(jc)::value;
-      const int n0 = ((tn * 2 + wn) * BN + j) * 16;
-      if constexpr (j + 1 < BN) fetch(j + 1, g[(j + 1) & 1], u[(j + 1) & 1]);
-#pragma unroll
-      for (int i = 0; i < BM; ++i) {
-        float dg[4], du[4], hv[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float a, da;
-          act_both(g[j & 1][i][r], act, a, da);
-          const float dh = acc_read(acc[i][j][r]);
-          dg[r] = dh * u[j & 1][i][r] * da;
-          du[r] = dh * a;
-          hv[r] = a * u[j & 1][i][r];
-        }
-        unsigned char* at = lds + (lane & 15) * (kRow + 16) + i * 32 + (lane >> 4) * 8;
-        *reinterpret_cast<u32x2*>(at) = pack4(dg);
-        *reinterpret_cast<u32x2*>(at + kOne) = pack4(du);
-        *reinterpret_cast<u32x2*>(at + 2 * kOne) = pack4(hv);
-      }
-      wave_lds_fence();
-      unsigned char* o = reinterpret_cast<unsigned char*>(dgu + (int64_t)n0 * 2 * f + m0);
-      put_rows<kRow, kCols>(lds, o, (int64_t)f * 4, N - n0, (f - m0) * 2, lane);
-      put_rows<kRow, kCols>(lds + kOne, o + (int64_t)f * 2, (int64_t)f * 4, N - n0, (f - m0) * 2, lane);
-      put_rows<kRow, kCols>(lds + 2 * kOne, reinterpret_cast<unsigned char*>(h + (int64_t)n0 * f + m0), (int64_t)f * 2,
-                            N - n0, (f - m0) * 2, lane);
-      wave_lds_fence();
-    });
+                                        unsigned char* lds, int index) const {
+    if (slab.base != nullptr) put_slab(acc, tn, wm, wn, lane, index, slab);
+    else row_pieces<BM, BN, Op::kPair>(acc, tm, tn, wm, wn, lane, lds, op);
   }
 };
 
 // ---- parts of K joined ------------------------------------------------------------
-// The slabs of a tile's parts added in order, then what the product's epilogue does with
-// the sum, eight entries of a column a thread.  `which`: the epilogue.
-enum : int { kJoinStore, kJoinGateUp, kJoinDh };
-struct JoinArgs {
+// The slabs of a tile's parts added in order and given to the product's epilogue.
+struct JoinShape {
   const float* slab;
   RowShape g;
-  int tile, tile_n, which;
-  EpiBf16 bf16;   // kJoinStore in bf16 ...
-  EpiF32 f32;     // ... or float32 (out set)
-  EpiGateUp gu;
-  EpiDh dh;
+  int tile, tile_n;
 };
-__device__ __forceinline__ Vec8 join8(const JoinArgs& a, int index, int m, int n) {
-  const int64_t size = (int64_t)a.tile * a.tile_n;
-  const int at = slab_piece(a.tile, m, n);   // entries m .. m + 3; the next four lie 64 floats on (m % 8 == 0)
-  Vec8 s{};
-  for (int p = 0; p < a.g.parts; ++p) {
-    const float* from = a.slab + ((int64_t)p * a.g.count + index) * size + at;
-    const f32x4 x = *reinterpret_cast<const f32x4*>(from), y = *reinterpret_cast<const f32x4*>(from + 64);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s.v[i] += x[i];
-      s.v[4 + i] += y[i];
-    }
-  }
-  return s;
-}
-__global__ __launch_bounds__(256) void ffn_join_kernel(JoinArgs a) {
+template <class Op>
+__global__ __launch_bounds__(256) void ffn_join_kernel(JoinShape a, Op op) {
   int tm, tn;
   row_tile_at(a.g, a.g.tile0 + blockIdx.x, tm, tn);
   // a wave takes 8 columns x 64 entries: whole lines of the output, 128-byte pieces of the slabs
-  const int width = a.which == kJoinGateUp ? a.tile / 2 : a.tile;
+  const int width = Op::kPair ? a.tile / 2 : a.tile;
   const int w = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int row = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
-  if (row >= a.tile_n) return;
-  const int64_t n = (int64_t)tn * a.tile_n + row;
-  if (a.which == kJoinStore) {
-    const int64_t m = (int64_t)tm * a.tile + m0;
-    if (n >= a.bf16.N || m >= a.bf16.M) return;
-    Vec8 s = join8(a, blockIdx.x, m0, row);
-    const bool second = n >= a.bf16.split;
-    const int64_t at = (second ? n - a.bf16.split : n) * a.bf16.ld + m;   // a multiple of 8
-    if (a.f32.out != nullptr) {
-      unsigned char* out = reinterpret_cast<unsigned char*>(second ? a.f32.out2 : a.f32.out);
-      if (a.f32.add) {
-        const Vec8 o = unpack8(load8<F32>(out, at / 8));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s.v[i] += o.v[i];
-      }
-      store8<F32>(out, at / 8, s);
-    } else {
-      store8<Bf16>(reinterpret_cast<unsigned char*>(second ? a.bf16.out2 : a.bf16.out), at / 8, s);
+  const int col = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
+  if (col >= a.tile_n) return;
+  const int64_t n = (int64_t)tn * a.tile_n + col, m = (int64_t)tm * width + m0;
+  if (n >= op.N) return;   // its slab columns are not written
+  // gate and up in turn, 16 rows each; the next four entries of a piece lie 64 floats on
+  const int row = Op::kPair ? m0 / 16 * 32 + m0 % 16 : m0;
+  const int64_t size = (int64_t)a.tile * a.tile_n;
+  const float* from = a.slab + blockIdx.x * size;
+  const int p0 = slab_piece(a.tile, row, col), p1 = Op::kPair ? slab_piece(a.tile, row + 16, col) : 0;
+  const typename Op::Fetched x = op.fetch(n, m);
+  f32x4 v[Op::kPair ? 4 : 2] = {};
+  for (int p = 0; p < a.g.parts; ++p, from += a.g.count * size) {
+    v[0] += *reinterpret_cast<const f32x4*>(from + p0);
+    v[1] += *reinterpret_cast<const f32x4*>(from + p0 + 64);
+    if constexpr (Op::kPair) {
+      v[2] += *reinterpret_cast<const f32x4*>(from + p1);
+      v[3] += *reinterpret_cast<const f32x4*>(from + p1 + 64);
     }
-  } else if (a.which == kJoinGateUp) {
-    const int64_t m = (int64_t)tm * (a.tile / 2) + m0;
-    if (n >= a.gu.N || m >= a.gu.f) return;
-    const int at = m0 / 16 * 32 + m0 % 16;   // gate and up in turn, 16 rows each
-    const Vec8 g = join8(a, blockIdx.x, at, row), u = join8(a, blockIdx.x, at + 16, row);
-    if (a.gu.pre != nullptr) {
-      unsigned char* pre = reinterpret_cast<unsigned char*>(a.gu.pre);
-      store8<F32>(pre, (n * 2 * a.gu.f + m) / 8, g);
-      store8<F32>(pre, (n * 2 * a.gu.f + a.gu.f + m) / 8, u);
-    }
-    Vec8 h;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h.v[i] = act_value(g.v[i], a.gu.act) * u.v[i];
-    store8<Bf16>(reinterpret_cast<unsigned char*>(a.gu.h), (n * a.gu.f + m) / 8, h);
-  } else {
-    const int64_t m = (int64_t)tm * a.tile + m0;
-    if (n >= a.dh.N || m >= a.dh.f) return;
-    const Vec8 dh = join8(a, blockIdx.x, m0, row);
-    const int64_t at = (n * 2 * a.dh.f + m) / 8;
-    const unsigned char* pre = reinterpret_cast<const unsigned char*>(a.dh.pre);
-    const Vec8 g = unpack8(load8<F32>(pre, at)), u = unpack8(load8<F32>(pre, at + a.dh.f / 8));
-    Vec8 dg, du, h;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v, dv;
-      act_both(g.v[i], a.dh.act, v, dv);
-      dg.v[i] = dh.v[i] * u.v[i] * dv;
-      du.v[i] = dh.v[i] * v;
-      h.v[i] = v * u.v[i];
-    }
-    unsigned char* dgu = reinterpret_cast<unsigned char*>(a.dh.dgu);
-    store8<Bf16>(dgu, at, dg);
-    store8<Bf16>(dgu, at + a.dh.f / 8, du);
-    store8<Bf16>(reinterpret_cast<unsigned char*>(a.dh.h), (n * a.dh.f + m) / 8, h);
   }
+  op.piece(n, m, v, x);
+}
+template <class Op>
+int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
+  const int waves = (Op::kPair ? tile / 2 : tile) / 64 * (tile_n / 8);
+  hipLaunchKernelGGL((ffn_join_kernel<Op>), dim3((uint32_t)g.count, (uint32_t)((waves + 3) / 4)), dim3(256), 0, stream,
+                     JoinShape{slab, g, tile, tile_n}, op);
+  PSPO_LAUNCHED("ffn_join_kernel", stream);
+  return PSPO_OK;
 }
 
 // ---- plan ---------------------------------------------------------------------------
@@ -361,16 +258,16 @@ constexpr int64_t kSlabBytes = int64_t(256) << 20;   // most that the parts of o
 
 // The cover of least estimated time: a stage of a full round takes 1.45, 1.1 or 0.9 us, one
 // with a work-group to a CU 0.7 us (128 x 128) or 0.5 us, each tile 20, 10 or 6 us beyond its
-// stages; the slabs of the parts are written and read at 4.5 TB/s, and a further launch with its
-// join takes 8 us.
-Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n) {
+// stages (dh, whose epilogue moves 14 bytes an entry: 55 or 16); the slabs of the parts are written
+// and read at 4.5 TB/s, and a further launch with its join takes 8 us.
+Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n, bool dh) {
   Plan p{};
   p.tile = tile;
   p.tile_n = tile_n;
   p.tiles_m = (int)((M + tile - 1) / tile);
   p.tiles_n = (int)((N + tile_n - 1) / tile_n);
   const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : tile_n == 128 ? 512 : 768;
-  const double extra = tile == 256 ? 20 : tile_n == 128 ? 10 : 6;
+  const double extra = tile == 256 ? (dh ? 55 : 20) : tile_n == 128 ? (dh ? 16 : 10) : 6;
   const double stage = tile == 256 ? 1.45 : tile_n == 128 ? 1.1 : 0.9;
   const double single = tile == 256 ? 1.45 : tile_n == 128 ? 0.7 : 0.5;
   auto time = [&](int64_t groups, int stages, double per_tile) {
@@ -387,7 +284,7 @@ Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n) {
   // what a part writes: the columns that exist
   const double written = (double)tile * (double)std::min<int64_t>(N, tile_n) * 4;
   for (int s = 2; s <= 32 && s * 4 <= nk && rest * s * bytes <= kSlabBytes; ++s) {
-    const double us = start + time(rest * s, (nk + s - 1) / s, extra / 2) + 8 + (double)(rest * s) * written * 2 / 4.5e6;
+    const double us = start + time(rest * s, (nk + s - 1) / s, tile == 256 ? 10 : 5) + 8 + (double)(rest * s) * written * 2 / 4.5e6;
     if (us < p.us) {
       p.us = us;
       p.whole = (int)before;
@@ -396,51 +293,55 @@ Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n) {
   }
   return p;
 }
-// narrow: 128 x 64 is to be had (A K-inner), for products of few columns.
-Plan plan_of(int64_t M, int64_t N, int nk, bool narrow) {
-  Plan best = plan_tile(M, N, nk, 128, 128);
-  const Plan big = plan_tile(M, N, nk, 256, 256);
+// dh: the product with that epilogue; the others may use 128 x 64, for few columns.
+Plan plan_of(int64_t M, int64_t N, int nk, bool dh) {
+  Plan best = plan_tile(M, N, nk, 128, 128, dh);
+  const Plan big = plan_tile(M, N, nk, 256, 256, dh);
   if (big.us <= best.us) best = big;
-  if (narrow && N <= 64) {
-    const Plan thin = plan_tile(M, N, nk, 128, 64);
+  if (!dh && N <= 64) {
+    const Plan thin = plan_tile(M, N, nk, 128, 64, dh);
     if (thin.us < best.us) best = thin;
   }
   return best;
 }
-int64_t slab_bytes(int64_t M, int64_t N, int K, int segs, bool narrow) {
+int64_t slab_bytes(int64_t M, int64_t N, int K, bool dh) {
   if (M == 0 || N == 0) return 0;
-  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK * segs, narrow);
+  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK, dh);
   if (p.parts == 1) return 0;
   return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile_n * 4;
 }
 
-template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-int launch(const RowShape& g, const Plan& p, const Epi& epi, const char* name, hipStream_t stream) {
+// A work-group alone on its CU has its stages' loads wait for memory, with one stage in flight:
+// launches of no more work-groups than CUs take a ring of four stages instead of two.
+constexpr int kDeep = 4;
+bool deep_ring(int64_t groups) { return groups <= 256; }
+
+template <bool kOuterA, bool kOuterB, class Op>
+int launch(const RowShape& g, const Plan& p, const Epi<Op>& epi, const char* name, hipStream_t stream) {
   const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
-  if constexpr (!kOuterA) {
-    if (p.tile_n == 64) {
-      hipLaunchKernelGGL((row_gemm_kernel<4, 2, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
-      PSPO_LAUNCHED(name, stream);
-      return PSPO_OK;
-    }
+  const bool deep = deep_ring((int64_t)g.count * g.parts);
+#define PSPO_ROW(BM, BN, RING)                                                                                    \
+  hipLaunchKernelGGL((row_gemm_kernel<BM, BN, RING, kOuterA, kOuterB, Op::kPair, Epi<Op>>), grid, dim3(256), 0, \
+                     stream, g, epi)
+  if (p.tile == 256) {
+    PSPO_ROW(8, 8, 2);
+  } else if (p.tile_n == 128) {
+    if (deep) PSPO_ROW(4, 4, kDeep);
+    else PSPO_ROW(4, 4, 2);
+  } else if constexpr (!kOuterA) {
+    if (deep) PSPO_ROW(4, 2, kDeep);
+    else PSPO_ROW(4, 2, 2);
   }
-  if (p.tile == 256)
-    hipLaunchKernelGGL((row_gemm_kernel<8, 8, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
-  else
-    hipLaunchKernelGGL((row_gemm_kernel<4, 4, kOuterA, kOuterB, kPairA, Epi>), grid, dim3(256), 0, stream, g, epi);
+#undef PSPO_ROW
   PSPO_LAUNCHED(name, stream);
   return PSPO_OK;
 }
 
-int join_parts(JoinArgs join, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream);
-
-// One product with its epilogue: the whole tiles, then the rest in parts and their join
-// (`join` holds the same epilogue).
-template <bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, float* slab, const char* name,
-            hipStream_t stream) {
+// One product with its epilogue: the whole tiles, then the rest in parts and their join.
+template <bool kOuterA, bool kOuterB, class Op>
+int product(RowShape g, int64_t M, int64_t N, const Op& op, float* slab, const char* name, hipStream_t stream) {
   if (M == 0 || N == 0) return PSPO_OK;
-  const Plan p = plan_of(M, N, (g.K + kRowK - 1) / kRowK * g.segs, !kOuterA);
+  const Plan p = plan_of(M, N, (g.K + kRowK - 1) / kRowK, std::is_same_v<Op, EpiDh>);
   const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
   PSPO_REQUIRE(total < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
   g.tiles_m = p.tiles_m;
@@ -449,26 +350,13 @@ int product(RowShape g, int64_t M, int64_t N, const Epi& epi, JoinArgs join, flo
   g.count = p.whole;
   g.parts = 1;
   if (g.count > 0)
-    if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p, epi, name, stream)) return rc;
+    if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {nullptr, 0}}, name, stream)) return rc;
   g.tile0 = p.whole;
   g.count = (int)(total - p.whole);
   if (g.count == 0) return PSPO_OK;
   g.parts = p.parts;
-  if (int rc = launch<kOuterA, kOuterB, kPairA>(g, p, EpiSlab{slab, (int)N}, name, stream)) return rc;
-  return join_parts(join, g, p.tile, p.tile_n, slab, stream);
-}
-
-// The join of a product's slabs, after `launch`.
-int join_parts(JoinArgs join, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
-  join.slab = slab;
-  join.g = g;
-  join.tile = tile;
-  join.tile_n = tile_n;
-  const int chunks = (join.which == kJoinGateUp ? tile / 2 : tile) / 8;
-  hipLaunchKernelGGL(ffn_join_kernel, dim3((uint32_t)g.count, (uint32_t)(tile_n * chunks / 256)), dim3(256), 0, stream,
-                     join);
-  PSPO_LAUNCHED("ffn_join_kernel", stream);
-  return PSPO_OK;
+  if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {slab, (int)N}}, name, stream)) return rc;
+  return join_parts(op, g, p.tile, p.tile_n, slab, stream);
 }
 
 // The three products behind dh, as one launch: dx, the two upper weights' gradients, the
@@ -518,29 +406,9 @@ JobPlan plan_backward(int64_t N, int64_t d, int64_t f) {
   return big.us <= small.us ? big : small;
 }
 
-// What a product stores: out[n][m], bf16 or float32 (or added to it); rows n >= split go to out2.
-struct Out {
-  void *out, *out2;
-  int M, N, split;
-  bool f32, add;
-};
-EpiBf16 bf16_of(const Out& o) {
-  return EpiBf16{static_cast<uint16_t*>(o.out), static_cast<uint16_t*>(o.out2), o.M, o.M, o.N, o.split};
-}
-EpiF32 f32_of(const Out& o) {
-  if (!o.f32) return EpiF32{};
-  return EpiF32{static_cast<float*>(o.out), static_cast<float*>(o.out2), o.M, o.M, o.N, o.split, o.add};
-}
-JoinArgs join_of(const Out& o) {
-  JoinArgs j{};
-  j.which = kJoinStore;
-  j.bf16 = bf16_of(o);
-  j.f32 = f32_of(o);
-  return j;
-}
-
-int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsigned char* slabs, hipStream_t stream) {
-  RowJobs<EpiAny> jobs{};
+int run_jobs(const JobPlan& p, const RowShape (&g)[3], const EpiStore (&o)[3], unsigned char* slabs,
+             hipStream_t stream) {
+  RowJobs<Epi<EpiStore>> jobs{};
   int64_t blocks = 0;
   for (int i = 0; i < 3; ++i) {
     const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
@@ -554,18 +422,19 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Out (&o)[3], unsign
     r.parts = p.parts[i];
     jobs.blocks[i] = (int)(round_up(tiles, kNumXcd) * p.parts[i]);
     blocks += jobs.blocks[i];
-    jobs.epi[i] = EpiAny{bf16_of(o[i]), f32_of(o[i]),
-                         EpiSlab{p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
+    jobs.epi[i] = {o[i], {p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
   }
   PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
   if (p.tile == 256)
-    hipLaunchKernelGGL((row_jobs_kernel<8, 8, EpiAny>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+    hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  else if (deep_ring(blocks))
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, kDeep, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
   else
-    hipLaunchKernelGGL((row_jobs_kernel<4, 4, EpiAny>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
   PSPO_LAUNCHED("ffn_gradients", stream);
   for (int i = 0; i < 3; ++i)
     if (p.parts[i] > 1 && jobs.g[i].count > 0)
-      if (int rc = join_parts(join_of(o[i]), jobs.g[i], p.tile, p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
+      if (int rc = join_parts(o[i], jobs.g[i], p.tile, p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
         return rc;
   return PSPO_OK;
 }
@@ -593,11 +462,11 @@ struct SkinnyStore {
 
 // Whether a forward of N tokens goes by these kernels.  They read every token's rows again for
 // each 16 rows of the weights, the 128 x 64 tiles write and join slabs instead: us a call, this
-// way / tiles, on 6 d f bytes of weights: d = 3584, f = 14336 (308 MB) N = 1 65 / 84, 16 90 / 84,
-// 24 105 / 84; 1536, 6144 (57 MB) N = 16 27 / 33, 32 33 / 34, 48 42 / 34; 512, 1344 (4 MB)
-// N = 64 15 / 19.
+// way / tiles, on 6 d f bytes of weights: d = 3584, f = 14336 (308 MB) N = 1 65 / 77, 16 90 / 82;
+// 1536, 6144 (57 MB) N = 16 26 / 28, 32 33 / 30; 2048, 800 (10 MB) N = 48 17 / 26; 512, 1344
+// (4 MB) N = 64 15 / 19.
 bool few_tokens(int64_t N, int64_t d, int64_t f) {
-  return N <= kSkinnyTokens && (N - 12) * (6 * d * f) <= int64_t(900) << 20;
+  return N <= kSkinnyTokens && (N - 12) * (6 * d * f) <= int64_t(300) << 20;
 }
 
 // Waves of a work-group: enough that the chip holds some 4,096, at most one for each
@@ -636,13 +505,13 @@ Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
   };
   s.h = take(N * f * 2);
   int64_t slab = 0;
-  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, 1, true);
+  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, false);
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab, slab_bytes(f, N, (int)d, 1, false), plan_backward(N, d, f).slab_bytes});
+    slab = std::max({slab, slab_bytes(f, N, (int)d, true), plan_backward(N, d, f).slab_bytes});
   } else if (!few_tokens(N, d, f)) {
-    slab = std::max(slab, slab_bytes(d, N, (int)f, 1, true));
+    slab = std::max(slab, slab_bytes(d, N, (int)f, false));
   }
   s.slab = take(slab);
   s.total = at;
@@ -675,11 +544,8 @@ int gate_up(const uint16_t* x, const uint16_t* wg, const uint16_t* wu, int N, in
             float* pre, float* slab, hipStream_t stream) {
   if (few_tokens(N, d, f))
     return skinny<2>(SkinnyArgs{{wg, wu}, x, f, N, d}, SkinnyGateUp{h, pre, f, act}, "ffn_gate_up", stream);
-  JoinArgs j{};
-  j.which = kJoinGateUp;
-  j.gu = EpiGateUp{h, pre, f, N, act};
-  return product<false, false, true>(shape(wg, wu, d, f, x, d, N, d), 2 * (int64_t)f, N, j.gu, j, slab, "ffn_gate_up",
-                                     stream);
+  return product<false, false>(shape(wg, wu, d, f, x, d, N, d), 2 * (int64_t)f, N, EpiGateUp{h, pre, f, N, act}, slab,
+                               "ffn_gate_up", stream);
 }
 
 }  // namespace
@@ -716,9 +582,8 @@ int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t
   if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, preact, slab, stream)) return rc;
   if (few_tokens(N, d, f))
     return skinny<1>(SkinnyArgs{{w_down, w_down}, h, d, N, f}, SkinnyStore{y, d}, "ffn_down", stream);
-  const Out o{y, y, d, N, N, false, false};
-  return product<false, false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, bf16_of(o), join_of(o), slab,
-                                      "ffn_down", stream);
+  return product<false, false>(shape(w_down, w_down, f, d, h, f, N, f), d, N, EpiStore{y, y, d, d, N, N, 0, 0}, slab,
+                               "ffn_down", stream);
 }
 
 int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up,
@@ -753,18 +618,15 @@ int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_
       if (int rc = gate_up(x, w_gate, w_up, N, d, f, act, h, own, slab, stream)) return rc;
       pre = own;
     }
-    JoinArgs j{};
-    j.which = kJoinDh;
-    j.dh = EpiDh{pre, dgu, h, f, N, act};
-    if (int rc = product<true, false, false>(shape(w_down, w_down, f, f, dy, d, N, d), f, N, j.dh, j, slab, "ffn_dh",
-                                             stream))
+    if (int rc = product<true, false>(shape(w_down, w_down, f, f, dy, d, N, d), f, N, EpiDh{pre, dgu, h, f, N, act}, slab,
+                                      "ffn_dh", stream))
       return rc;
   }
   const RowShape g[3] = {shape(w_gate, w_up, d, d, dgu, 2 * (int64_t)f, N, f, 2, f),
                          shape(x, x, d, d, dgu, 2 * (int64_t)f, 2 * f, N), shape(h, h, f, f, dy, d, d, N)};
-  const Out o[3] = {{dx, dx, d, N, N, false, false},
-                    {dw_gate, dw_up, d, 2 * f, f, f32, add},
-                    {dw_down, dw_down, f, d, d, f32, add}};
+  const EpiStore o[3] = {{dx, dx, d, d, N, N, 0, 0},
+                         {dw_gate, dw_up, d, d, 2 * f, f, f32, add},
+                         {dw_down, dw_down, f, f, d, d, f32, add}};
   return run_jobs(plan_backward(N, d, f), g, o, reinterpret_cast<unsigned char*>(slab), stream);
 }
 

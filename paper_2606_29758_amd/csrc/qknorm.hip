@@ -357,7 +357,7 @@ int check(const void* q, const void* k, int64_t q_stride, int64_t k_stride, cons
                  PSPO_ERR_INVALID_ARG, "misaligned pointer argument");
     if (rot > 0) {
       PSPO_REQUIRE(inv_freq, PSPO_ERR_INVALID_ARG, "inv_freq is NULL");
-      PSPO_REQUIRE(positions || (seq_id && (cu || R == 0)), PSPO_ERR_INVALID_ARG,
+      PSPO_REQUIRE(positions || (seq_id && cu), PSPO_ERR_INVALID_ARG,
                    "positions, or seq_id and cu_seqlens, must be given");
     }
   }

@@ -217,11 +217,11 @@ __device__ __forceinline__ void row_barrier() {
   stage_barrier<63>();
 }
 
-template <int BM, int BN>
-constexpr int kRowLds = 2 * (32 * BM + 32 * BN) * kRowK * 2;
+template <int BM, int BN, int kRing>
+constexpr int kRowLds = kRing * (32 * BM + 32 * BN) * kRowK * 2;
 
 // One tile of a product: work-group `bid` of the launch's tiles, K part `part`.
-template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
 __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi, int bid, int part,
                                               unsigned char* lds) {
   using A = RowSide<BM, kOuterA, kPairA>;
@@ -249,7 +249,7 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
     for (int j = 0; j < BN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   bf16x8 fa[2][BM] = {}, fb[2][BN] = {};   // operand registers of the two half stages
 
-  // The loads run two stages ahead; past the end they are empty.
+  // The loads run kRing stages ahead; past the end they are empty.
   typename A::Stage ga;
   typename B::Stage gb;
   int ahead = kb, left;
@@ -268,17 +268,17 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
   };
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
 #pragma unroll
-  for (int st = 0; st < 2; ++st) {
+  for (int st = 0; st < kRing; ++st) {
     settle(ga, gb);
     repeat<A::kLoads>([&](auto q) { sa.template load<decltype(q)::value>(ga, lds0 + st * kStage, wave); });
     repeat<B::kLoads>([&](auto q) { sb.template load<decltype(q)::value>(gb, lds0 + st * kStage + A::kBytes, wave); });
-    if (st == 0) {
+    if (st + 1 < kRing) {
       step();
       sa.next(ga, over, left, ahead < ke);
       sb.next(gb, over, left, ahead < ke);
     }
   }
-  row_barrier<A::kLoads + B::kLoads>();
+  row_barrier<(kRing - 1) * (A::kLoads + B::kLoads)>();
   repeat<A::kReads>([&](auto r) { sa.template read<decltype(r)::value, 0>(fa[0], lds); });
   repeat<B::kReads>([&](auto r) { sb.template read<decltype(r)::value, 0>(fb[0], lds + A::kBytes); });
 
@@ -287,7 +287,7 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
   static_assert(kReads <= kMfma && kLoads <= kMfma, "one read and one load at most after each MFMA");
   uint32_t cur = 0;
   for (int t = kb; t < ke; ++t) {
-    const uint32_t nxt = kStage - cur;
+    const uint32_t nxt = cur == (kRing - 1) * kStage ? 0u : cur + kStage;
     // first half: K 0 .. 31 of this stage; its other half is read
     repeat<kMfma>([&](auto ic) {
       constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
@@ -297,14 +297,14 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
         if constexpr (r < B::kReads) sb.template read<r, 1>(fb[1], lds + cur + A::kBytes);
         else sa.template read<r - B::kReads, 1>(fa[1], lds + cur);
       }
-      // where the stage after next lies, in slots without a read where there are such
+      // where the next stage to load lies
       if constexpr (i == kMfma - 6) step();
       if constexpr (i == kMfma - 5) sa.next(ga, over, left, ahead < ke);
       if constexpr (i == kMfma - 3) sb.next(gb, over, left, ahead < ke);
       __builtin_amdgcn_sched_barrier(0);
     });
     // every wave is done with this stage's buffer, and the next stage has landed
-    row_barrier<0>();
+    row_barrier<(kRing - 2) * kLoads>();
     settle(ga, gb);
     repeat<kMfma>([&](auto ic) {
       constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
@@ -330,15 +330,19 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
   }
 
   row_barrier<0>();   // the last (empty) loads have landed, every wave is done with the buffers
-  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kStage / 2),
+  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kRing * kStage / 4),
                               part * g.count + index);
 }
 
-template <int BM, int BN, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : BM * BN > 8 ? 2 : 3)))
+// Work-groups of a CU (waves of a SIMD): what the LDS holds.
+template <int BM, int BN, int kRing>
+constexpr int kRowGroups = 163840 / kRowLds<BM, BN, kRing> < 3 ? 163840 / kRowLds<BM, BN, kRing> : 3;
+
+template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kRowGroups<BM, BN, kRing>)))
 void row_gemm_kernel(RowShape g, Epi epi) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
-  row_gemm_tile<BM, BN, kOuterA, kOuterB, kPairA>(g, epi, blockIdx.x, blockIdx.y, lds);
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
+  row_gemm_tile<BM, BN, kRing, kOuterA, kOuterB, kPairA>(g, epi, blockIdx.x, blockIdx.y, lds);
 }
 
 // Independent products in one launch, the first with A K-outer and B K-inner, the others with
@@ -352,21 +356,21 @@ struct RowJobs {
   Epi epi[kJobs];
   int blocks[kJobs];
 };
-template <int BM, int BN, class Epi>
-__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(BM * BN > 32 ? 1 : BM * BN > 8 ? 2 : 3)))
+template <int BM, int BN, int kRing, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kRowGroups<BM, BN, kRing>)))
 void row_jobs_kernel(RowJobs<Epi> jobs) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN>];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
   int bid = blockIdx.x;
   if (bid < jobs.blocks[0]) {
     const int per = (jobs.g[0].count + kNumXcd - 1) / kNumXcd * kNumXcd;
-    row_gemm_tile<BM, BN, true, false, false>(jobs.g[0], jobs.epi[0], bid % per, bid / per, lds);
+    row_gemm_tile<BM, BN, kRing, true, false, false>(jobs.g[0], jobs.epi[0], bid % per, bid / per, lds);
     return;
   }
   bid -= jobs.blocks[0];
   const int job = bid < jobs.blocks[1] ? 1 : 2;
   if (job == 2) bid -= jobs.blocks[1];
   const int per = (jobs.g[job].count + kNumXcd - 1) / kNumXcd * kNumXcd;
-  row_gemm_tile<BM, BN, true, true, false>(jobs.g[job], jobs.epi[job], bid % per, bid / per, lds);
+  row_gemm_tile<BM, BN, kRing, true, true, false>(jobs.g[job], jobs.epi[job], bid % per, bid / per, lds);
 }
 
 // One accumulator, read where it is needed: as a plain value the compiler copies the
@@ -383,20 +387,62 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Rows of kRow bytes in LDS (pitch kRow + 16) -> rows of memory `pitch` bytes apart, 16
-// bytes a lane: row r < rows_have, bytes < bytes_have (a multiple of 16).  Past the caches:
-// whole lines, far more of them than the caches hold until the next kernel reads them.
-template <int kRow, int kRows>
-__device__ __forceinline__ void put_rows(const unsigned char* lds, unsigned char* out, int64_t pitch, int rows_have,
-                                         int bytes_have, int lane) {
-  constexpr int kPer = kRow / 16;
+// Hands a wave's accumulators to `op` eight entries of a column at a time, whole lines of a
+// row of the output together: op.fetch(n, m) for kAhead pieces (what they need from memory),
+// then op.piece(n, m, values, fetched) for each.  With kPair the row blocks come in pairs (even:
+// first matrix, odd: second) and a piece is eight entries of both.  The accumulators go through
+// the wave's LDS, up to 64 columns at once, 16-byte chunk c of column n at place c ^ (n & 15);
+// the work on them is a loop over whole lines of the output (against straight-line code with
+// three staged stores per block column: dh product of 8192 tokens 956 -> 918 us).
+template <int BM, int BN, bool kPair, class Op>
+__device__ __forceinline__ void row_pieces(const f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
+                                           unsigned char* lds, const Op& op) {
+  constexpr int kM = BM * 16, kPasses = BN > 4 ? BN / 4 : 1, kB = BN / kPasses;   // column blocks per pass
+  constexpr int kWidth = kPair ? kM / 2 : kM, kPer = kWidth / 8;                  // entries, pieces of a column
+  constexpr int kSteps = kB * 16 * kPer / 64, kAhead = kSteps < 4 ? kSteps : 4;
+  static_assert(kSteps % kAhead == 0 && 64 % kPer == 0, "whole steps");
+  const int g = lane >> 4, c0 = lane & 15;
+  repeat<kPasses>([&](auto pc) {   // constant indices into the accumulators, whatever the unroller decides
+    constexpr int pass = decltype(pc)::value;
+    wave_lds_fence();
+    repeat<kB>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
 #pragma unroll
-  for (int x = 0; x < kRows * kPer; x += 64) {
-    const int r = (x + lane) / kPer, c = (x + lane) % kPer * 16;
-    if (r < rows_have && c < bytes_have)
-      __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(lds + r * (kRow + 16) + c),
-                                  reinterpret_cast<u32x4*>(out + r * pitch + c));
-  }
+      for (int i = 0; i < BM; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][pass * kB + j][r]);
+        *reinterpret_cast<f32x4*>(lds + (j * 16 + c0) * (kM * 4) + (((i * 4 + g) ^ c0) << 4)) = v;
+      }
+    });
+    wave_lds_fence();
+    const int64_t n0 = ((int64_t)(tn * 2 + wn) * BN + pass * kB) * 16;
+    const int64_t m0 = (int64_t)(tm * 2 + wm) * kWidth + lane % kPer * 8;
+    const int k = lane % kPer;
+    // chunk of the piece's first four entries: of the row, or of the first of a pair of blocks
+    const int at = kPair ? k / 2 * 8 + k % 2 * 2 : k * 2;
+    auto four = [&](int col, int chunk) -> f32x4 {
+      return *reinterpret_cast<const f32x4*>(lds + col * (kM * 4) + ((chunk ^ (col & 15)) << 4));
+    };
+#pragma unroll 1
+    for (int s = 0; s < kSteps; s += kAhead) {
+      typename Op::Fetched f[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) f[u] = op.fetch(n0 + (s + u) * (64 / kPer) + lane / kPer, m0);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int col = (s + u) * (64 / kPer) + lane / kPer;
+        f32x4 v[kPair ? 4 : 2];
+        v[0] = four(col, at);
+        v[1] = four(col, at + 1);
+        if constexpr (kPair) {
+          v[2] = four(col, at + 4);
+          v[3] = four(col, at + 5);
+        }
+        op.piece(n0 + col, m0, v, f[u]);
+      }
+    }
+  });
 }
 
 }  // namespace pspo
