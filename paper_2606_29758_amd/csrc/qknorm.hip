@@ -64,12 +64,14 @@ __device__ __forceinline__ void angles(const QkArgs& a, int n, int lane, float* 
 struct LaneTurn {
   float c[8], s[8];
   int partner;      // lane offset to the partner's lane
+  bool half_row;    // the same in every lane: the partner sits across the row of 16 lanes
 };
 
 // dir: +1 forward, -1 back (the transpose).
 __device__ __forceinline__ LaneTurn lane_turn(const QkArgs& a, int chunk, const float* cs, const float* sn, float dir) {
   LaneTurn t;
   t.partner = 0;
+  t.half_row = a.D == 128 && a.rot == 128;
   const int e0 = chunk * 8;
   if (e0 >= a.rot) {   // not turned (rot is a multiple of 16, so a lane's entries agree)
 #pragma unroll
@@ -99,24 +101,38 @@ __device__ __forceinline__ LaneTurn lane_turn(const QkArgs& a, int chunk, const 
   return t;
 }
 
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), kCtrl, 0xF, 0xF, true));
+}
+
+// Sum over the head's L lanes, in each of them: up to 16 lanes by moves within a row of 16
+// (quads, then mirrored halves), which go at the vector rate, beyond by exchanges through LDS.
+template <int L>
+__device__ __forceinline__ float head_sum(float x) {
+  if constexpr (L >= 2) x += dpp<0xB1>(x);    // quad_perm 1, 0, 3, 2
+  if constexpr (L >= 4) x += dpp<0x4E>(x);    // quad_perm 2, 3, 0, 1
+  if constexpr (L >= 8) x += dpp<0x141>(x);   // row_half_mirror: the other quad of eight
+  if constexpr (L >= 16) x += dpp<0x140>(x);  // row_mirror: the other half of sixteen
+#pragma unroll
+  for (int m = 16; m < L; m <<= 1) x += __shfl_xor(x, m);
+  return x;
+}
+
 __device__ __forceinline__ Vec8 turn(const Vec8& z, const LaneTurn& t, int interleaved, int lane) {
   Vec8 o;
   if (interleaved) {   // uniform over the call
 #pragma unroll
     for (int j = 0; j < 8; ++j) o.v[j] = z.v[j] * t.c[j] + z.v[j ^ 1] * t.s[j];
+  } else if (t.half_row) {   // uniform: heads of 16 lanes turned whole, the partner 8 lanes on
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o.v[j] = z.v[j] * t.c[j] + dpp<0x128>(z.v[j]) * t.s[j];   // row_ror:8
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o.v[j] = z.v[j] * t.c[j] + __shfl(z.v[j], lane + t.partner) * t.s[j];
   }
   // an entry that is not turned is passed on as it is (0 * Inf would make a NaN of it)
   return o;
-}
-
-template <int L>
-__device__ __forceinline__ float head_sum(float x) {
-#pragma unroll
-  for (int m = 1; m < L; m <<= 1) x += __shfl_xor(x, m);
-  return x;
 }
 
 template <class T>
@@ -130,7 +146,7 @@ __device__ __forceinline__ Vec8 weight8(const unsigned char* w, int chunk, bool 
 
 // One wave per token (and per grid row, a span of its passes), heads in the
 // order queries, keys; a pass takes 64 / L heads.
-template <class T, int L>
+template <class T, int L, bool kPast>
 __global__ __launch_bounds__(64 * kWaves) void qk_fwd_kernel(QkArgs a) {
   constexpr int kHeads = 64 / L;
   __shared__ float cs[kWaves][kMaxDim / 2], sn[kWaves][kMaxDim / 2];
@@ -177,7 +193,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_fwd_kernel(QkArgs a) {
       }
       const Vec8 o = turn(z, t, a.interleaved, lane);
       if (inside && h < (is_q ? a.Hq : a.Hk))
-        store8<T>((is_q ? a.q_out + n * a.Hq * head_bytes : a.k_out + n * a.Hk * head_bytes) + h * head_bytes, chunk,
+        store8<T, kPast>((is_q ? a.q_out + n * a.Hq * head_bytes : a.k_out + n * a.Hk * head_bytes) + h * head_bytes, chunk,
                   turned ? o : z);
     }
   }
@@ -186,7 +202,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_fwd_kernel(QkArgs a) {
 // Waves walk the tokens in steps of the grid and keep their sums of dz * xhat in
 // registers (one set for queries, one for keys); a work-group's sums are joined
 // in LDS, in wave order, and left in `partials`.
-template <class T, int L>
+template <class T, int L, bool kPast>
 __global__ __launch_bounds__(64 * kWaves) void qk_bwd_kernel(QkArgs a) {
   constexpr int kHeads = 64 / L;
   __shared__ float cs[kWaves][kMaxDim / 2], sn[kWaves][kMaxDim / 2];
@@ -222,8 +238,8 @@ __global__ __launch_bounds__(64 * kWaves) void qk_bwd_kernel(QkArgs a) {
           xr[s] = Raw8<T>{};
           dr[s] = Raw8<T>{};
           if (inside && h < H) {
-            xr[s] = load8<T>(xin + h * head_bytes, chunk);
-            dr[s] = load8<T>(din + h * head_bytes, chunk);
+            xr[s] = load8<T, kPast>(xin + h * head_bytes, chunk);
+            dr[s] = load8<T, kPast>(din + h * head_bytes, chunk);
           }
         }
 #pragma unroll
@@ -248,7 +264,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_bwd_kernel(QkArgs a) {
               dz.v[j] = rstd * (dz.v[j] * w.v[j] - x.v[j] * m);
             }
           }
-          if (inside && h < H) store8<T>(dst + h * head_bytes, chunk, dz);
+          if (inside && h < H) store8<T, kPast>(dst + h * head_bytes, chunk, dz);
         }
       }
     }
@@ -309,19 +325,31 @@ int lanes_of(int D) {
   return L;
 }
 
-template <class T>
+// The forward stores past the caches, the backward loads and stores (28,481 tokens of 32 heads of
+// 128: 89 -> 73 us, 171 -> 162 us; the forward's loads too 84).
+bool past(const QkArgs& a, int bytes, int times) {
+  return (int64_t)a.N * (a.Hq + a.Hk) * a.D * bytes * times >= kPastBytes;
+}
+
+template <class T, bool kPast>
 void launch_fwd(const QkArgs& a, int L, dim3 grid, hipStream_t stream) {
 #define PSPO_QK(W) \
-  case W: hipLaunchKernelGGL((qk_fwd_kernel<T, W>), grid, dim3(64 * kWaves), 0, stream, a); break
+  case W: hipLaunchKernelGGL((qk_fwd_kernel<T, W, kPast>), grid, dim3(64 * kWaves), 0, stream, a); break
+  switch (L) { PSPO_QK(1); PSPO_QK(2); PSPO_QK(4); PSPO_QK(8); PSPO_QK(16); PSPO_QK(32); PSPO_QK(64); }
+#undef PSPO_QK
+}
+template <class T, bool kPast>
+void launch_bwd(const QkArgs& a, int L, dim3 grid, hipStream_t stream) {
+#define PSPO_QK(W) \
+  case W: hipLaunchKernelGGL((qk_bwd_kernel<T, W, kPast>), grid, dim3(64 * kWaves), 0, stream, a); break
   switch (L) { PSPO_QK(1); PSPO_QK(2); PSPO_QK(4); PSPO_QK(8); PSPO_QK(16); PSPO_QK(32); PSPO_QK(64); }
 #undef PSPO_QK
 }
 template <class T>
-void launch_bwd(const QkArgs& a, int L, dim3 grid, hipStream_t stream) {
-#define PSPO_QK(W) \
-  case W: hipLaunchKernelGGL((qk_bwd_kernel<T, W>), grid, dim3(64 * kWaves), 0, stream, a); break
-  switch (L) { PSPO_QK(1); PSPO_QK(2); PSPO_QK(4); PSPO_QK(8); PSPO_QK(16); PSPO_QK(32); PSPO_QK(64); }
-#undef PSPO_QK
+void launch(const QkArgs& a, int L, dim3 grid, bool backward, hipStream_t stream) {
+  const bool p = past(a, T::kBytes, backward ? 3 : 2);
+  if (backward) p ? launch_bwd<T, true>(a, L, grid, stream) : launch_bwd<T, false>(a, L, grid, stream);
+  else p ? launch_fwd<T, true>(a, L, grid, stream) : launch_fwd<T, false>(a, L, grid, stream);
 }
 
 // Checks shared by both directions; fills the common arguments.
@@ -420,8 +448,8 @@ int pspo_qk_norm_rope_fwd(const void* q, const void* k, int64_t q_stride, int64_
   a.per_part = (passes + parts - 1) / parts;
   parts = (passes + a.per_part - 1) / a.per_part;
   const dim3 grid((uint32_t)gx, (uint32_t)parts);
-  if (type == PSPO_TYPE_F32) launch_fwd<F32>(a, L, grid, stream);
-  else launch_fwd<Bf16>(a, L, grid, stream);
+  if (type == PSPO_TYPE_F32) launch<F32>(a, L, grid, false, stream);
+  else launch<Bf16>(a, L, grid, false, stream);
   PSPO_LAUNCHED("qk_fwd_kernel", stream);
   return PSPO_OK;
 }
@@ -469,8 +497,8 @@ int pspo_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
     a.k_out = static_cast<unsigned char*>(dk);
     a.partials = want ? static_cast<float*>(workspace) : nullptr;
     const int L = lanes_of(head_dim);
-    if (type == PSPO_TYPE_F32) launch_bwd<F32>(a, L, dim3(groups), stream);
-    else launch_bwd<Bf16>(a, L, dim3(groups), stream);
+    if (type == PSPO_TYPE_F32) launch<F32>(a, L, dim3(groups), true, stream);
+    else launch<Bf16>(a, L, dim3(groups), true, stream);
     PSPO_LAUNCHED("qk_bwd_kernel", stream);
   }
   if (want) {

@@ -31,13 +31,18 @@ struct Raw8<F32> {
   u32x4 a, b;
 };
 
-// p: the row's bytes; i: index of the group of eight in the row.
-template <class T>
+// p: the row's bytes; i: index of the group of eight in the row; kPast: past the caches.
+template <class T, bool kPast = false>
 __device__ __forceinline__ Raw8<T> load8(const unsigned char* p, int64_t i) {
   Raw8<T> r;
   const u32x4* q = reinterpret_cast<const u32x4*>(p + i * (8 * T::kBytes));
-  r.a = q[0];
-  if constexpr (T::kBytes == 4) r.b = q[1];
+  if constexpr (kPast) {
+    r.a = __builtin_nontemporal_load(q);
+    if constexpr (T::kBytes == 4) r.b = __builtin_nontemporal_load(q + 1);
+  } else {
+    r.a = q[0];
+    if constexpr (T::kBytes == 4) r.b = q[1];
+  }
   return r;
 }
 
@@ -65,14 +70,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, b);
 }
 
-template <class T>
+template <bool kPast>
+__device__ __forceinline__ void put16(u32x4* q, const u32x4& a) {
+  if constexpr (kPast) __builtin_nontemporal_store(a, q);
+  else *q = a;
+}
+
+template <class T, bool kPast = false>
 __device__ __forceinline__ void store8(unsigned char* p, int64_t i, const Vec8& x) {
   u32x4* q = reinterpret_cast<u32x4*>(p + i * (8 * T::kBytes));
   if constexpr (T::kBytes == 2) {
     u32x4 a;
 #pragma unroll
     for (int k = 0; k < 4; ++k) a[k] = pack_bf16(x.v[2 * k], x.v[2 * k + 1]);
-    q[0] = a;
+    put16<kPast>(q, a);
   } else {
     u32x4 a, b;
 #pragma unroll
@@ -80,9 +91,13 @@ __device__ __forceinline__ void store8(unsigned char* p, int64_t i, const Vec8& 
       a[k] = __float_as_uint(x.v[k]);
       b[k] = __float_as_uint(x.v[4 + k]);
     }
-    q[0] = a;
-    q[1] = b;
+    put16<kPast>(q, a);
+    put16<kPast>(q + 1, b);
   }
 }
+
+// Calls that move this much go past the caches, which would not hold their outputs until the
+// next call reads them; smaller ones leave them there.
+constexpr int64_t kPastBytes = int64_t(160) << 20;
 
 }  // namespace pspo
