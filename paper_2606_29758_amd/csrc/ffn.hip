@@ -33,10 +33,12 @@ __device__ __forceinline__ float logistic(float a) {
 
 constexpr float kGelu = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 
+// Beyond 16 the logistic is 0 or 1; the bound keeps the cube finite (and a NaN a NaN).
+__device__ __forceinline__ float gelu_bound(float g) { return g > 16.f ? 16.f : (g < -16.f ? -16.f : g); }
+
 __device__ __forceinline__ float act_value(float g, int kind) {
   if (kind == PSPO_ACT_SILU) return g * logistic(g);
-  // beyond 16 the logistic is 0 or 1; the bound keeps the cube finite
-  const float b = fminf(fmaxf(g, -16.f), 16.f);
+  const float b = gelu_bound(g);
   return g * logistic(kGelu * (b + 0.044715f * b * b * b));
 }
 __device__ __forceinline__ void act_both(float g, int kind, float& a, float& da) {
@@ -46,7 +48,7 @@ __device__ __forceinline__ void act_both(float g, int kind, float& a, float& da)
     da = s + a * (1.f - s);
     return;
   }
-  const float b = fminf(fmaxf(g, -16.f), 16.f);
+  const float b = gelu_bound(g);
   const float s = logistic(kGelu * (b + 0.044715f * b * b * b));
   a = g * s;
   da = s + b * s * (1.f - s) * (kGelu * (1.f + 0.134145f * b * b));

@@ -288,7 +288,7 @@ def dropout_add(x, N: int, p: float, seed: int, offset: int = 0, residual: Optio
                 row_ids: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x) of the first N rows of x [>=N, d] (bf16 or float32); no mask is stored.
 
-    An entry is kept with probability T / 2^16, T = round((1 - p) 2^16), and scaled by its inverse.
+    An entry is kept with probability T / 2^16, T = floor((1 - p) 2^16 + 1/2), and scaled by its inverse.
     The mask depends on (seed, offset, column, row_ids[n]) only (row_ids None: the row itself); with
     the packer's src_row it is the same for every draw of the cutoffs.  Returns [N, d].
     """
@@ -426,6 +426,8 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact
             raise ValueError("accumulate needs dw")
         dw = tuple(torch.empty(s, dtype=torch.bfloat16, device=x.device) for s in shapes)
     else:
+        if len(dw) != 3:
+            raise ValueError("dw must hold the three weight gradients")
         for i, (t, s, name) in enumerate(zip(dw, shapes, ("dw_gate", "dw_up", "dw_down"))):
             ty = _type(t, name)
             if ty != _type(dw[0], name):

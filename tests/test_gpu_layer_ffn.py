@@ -202,6 +202,24 @@ def test_activation_far_out():
         assert np.allclose(np.diag(_np(o["dw_gate"])), 1.25 * da[0] * _np(x)[0], rtol=3 * B, atol=1e-3)
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("N", [3, 200])
+def test_a_nan_of_a_weight_reaches_every_gradient_it_enters(act, N):
+    """One NaN in a gate row: that pre-activation is NaN for every token, so are y, dx, and the rows of the three
+    weight gradients that it enters; the others are not."""
+    d, f, j = 64, 136, 70
+    x, wg, wu, wd, dy = _inputs(N, d, f, 9)
+    ref = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, act=act)
+    wg[j, 5] = float("nan")
+    assert torch.isnan(layer.gated_ffn(x, wg, wu, wd, N, act=act)["y"]).all()
+    o = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, act=act)
+    rest = torch.arange(f, device="cuda") != j
+    assert torch.isnan(o["dx"]).all()
+    assert torch.isnan(o["dw_gate"][j]).all() and torch.equal(o["dw_gate"][rest], ref["dw_gate"][rest])
+    assert torch.isnan(o["dw_up"][j]).all() and torch.equal(o["dw_up"][rest], ref["dw_up"][rest])
+    assert torch.isnan(o["dw_down"][:, j]).all() and torch.equal(o["dw_down"][:, rest], ref["dw_down"][:, rest])
+
+
 def test_offsets_past_32_bits():
     """A token count at which the intermediate and the pre-activations pass 2^32 bytes: rows at both ends equal
     those of small calls."""
@@ -253,6 +271,8 @@ def test_refusals():
         layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, dw=dw, accumulate=True)
     with pytest.raises(ValueError, match="overlaps"):
         layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, dw=(dw[0], dw[0], dw[2]))
+    with pytest.raises(ValueError, match="three weight"):
+        layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, dw=dw[:2])
     with pytest.raises(ValueError, match="preact"):
         layer.gated_ffn_bwd(dy, x, wg, wu, wd, 8, preact=torch.empty(8, 72, device="cuda"))
 
