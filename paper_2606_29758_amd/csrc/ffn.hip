@@ -212,12 +212,12 @@ struct JoinShape {
   int tile, tile_n;
 };
 template <class Op>
-__global__ __launch_bounds__(256) void ffn_join_kernel(JoinShape a, Op op) {
+__device__ __forceinline__ void join_tile(const JoinShape& a, const Op& op, int index, int block) {
   int tm, tn;
-  row_tile_at(a.g, a.g.tile0 + blockIdx.x, tm, tn);
+  row_tile_at(a.g, a.g.tile0 + index, tm, tn);
   // a wave takes 8 columns x 64 entries: whole lines of the output, 128-byte pieces of the slabs
   const int width = Op::kPair ? a.tile / 2 : a.tile;
-  const int w = blockIdx.y * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int w = block * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
   const int col = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
   if (col >= a.tile_n) return;
   const int64_t n = (int64_t)tn * a.tile_n + col, m = (int64_t)tm * width + m0;
@@ -225,25 +225,56 @@ __global__ __launch_bounds__(256) void ffn_join_kernel(JoinShape a, Op op) {
   // gate and up in turn, 16 rows each; the next four entries of a piece lie 64 floats on
   const int row = Op::kPair ? m0 / 16 * 32 + m0 % 16 : m0;
   const int64_t size = (int64_t)a.tile * a.tile_n;
-  const float* from = a.slab + blockIdx.x * size;
+  const float* from = a.slab + index * size;
   const int p0 = slab_piece(a.tile, row, col), p1 = Op::kPair ? slab_piece(a.tile, row + 16, col) : 0;
   const typename Op::Fetched x = op.fetch(n, m);
   f32x4 v[Op::kPair ? 4 : 2] = {};
-  for (int p = 0; p < a.g.parts; ++p, from += a.g.count * size) {
-    v[0] += *reinterpret_cast<const f32x4*>(from + p0);
-    v[1] += *reinterpret_cast<const f32x4*>(from + p0 + 64);
-    if constexpr (Op::kPair) {
-      v[2] += *reinterpret_cast<const f32x4*>(from + p1);
-      v[3] += *reinterpret_cast<const f32x4*>(from + p1 + 64);
-    }
+  // four parts' loads out before the first is added; the sums in the parts' order
+  const int64_t next = a.g.count * size;
+  constexpr int kV = Op::kPair ? 4 : 2;
+  for (int p = 0; p < a.g.parts; p += 4) {
+    f32x4 t[4][kV];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (p + q < a.g.parts) {
+        const float* at = from + (p + q) * next;
+        t[q][0] = *reinterpret_cast<const f32x4*>(at + p0);
+        t[q][1] = *reinterpret_cast<const f32x4*>(at + p0 + 64);
+        if constexpr (Op::kPair) {
+          t[q][2] = *reinterpret_cast<const f32x4*>(at + p1);
+          t[q][3] = *reinterpret_cast<const f32x4*>(at + p1 + 64);
+        }
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (p + q < a.g.parts)
+#pragma unroll
+        for (int k = 0; k < kV; ++k) v[k] += t[q][k];
   }
   op.piece(n, m, v, x);
 }
+// Work-groups for a tile's join: a wave for 8 columns x 64 entries.
+inline int join_blocks(int width, int tile_n) { return (width / 64 * (tile_n / 8) + 3) / 4; }
+
+template <class Op>
+__global__ __launch_bounds__(256) void ffn_join_kernel(JoinShape a, Op op) {
+  join_tile(a, op, blockIdx.x, blockIdx.y);
+}
+// The joins of several products in one launch (grid x: their tiles one after another).
+struct JoinJobs {
+  JoinShape a[3];
+  EpiStore op[3];
+};
+__global__ __launch_bounds__(256) void ffn_join_jobs_kernel(JoinJobs j) {
+  int index = blockIdx.x, job = 0;
+  while (index >= j.a[job].g.count) index -= j.a[job++].g.count;   // the counts add up to the grid
+  join_tile(j.a[job], j.op[job], index, blockIdx.y);
+}
 template <class Op>
 int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
-  const int waves = (Op::kPair ? tile / 2 : tile) / 64 * (tile_n / 8);
-  hipLaunchKernelGGL((ffn_join_kernel<Op>), dim3((uint32_t)g.count, (uint32_t)((waves + 3) / 4)), dim3(256), 0, stream,
-                     JoinShape{slab, g, tile, tile_n}, op);
+  hipLaunchKernelGGL((ffn_join_kernel<Op>),
+                     dim3((uint32_t)g.count, (uint32_t)join_blocks(Op::kPair ? tile / 2 : tile, tile_n)), dim3(256), 0,
+                     stream, JoinShape{slab, g, tile, tile_n}, op);
   PSPO_LAUNCHED("ffn_join_kernel", stream);
   return PSPO_OK;
 }
@@ -434,10 +465,20 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const EpiStore (&o)[3], u
   else
     hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
   PSPO_LAUNCHED("ffn_gradients", stream);
+  JoinJobs join{};
+  int split = 0;
+  int64_t tiles = 0;
   for (int i = 0; i < 3; ++i)
-    if (p.parts[i] > 1 && jobs.g[i].count > 0)
-      if (int rc = join_parts(o[i], jobs.g[i], p.tile, p.tile, reinterpret_cast<float*>(slabs + p.slab[i]), stream))
-        return rc;
+    if (p.parts[i] > 1 && jobs.g[i].count > 0) {
+      join.a[split] = JoinShape{reinterpret_cast<float*>(slabs + p.slab[i]), jobs.g[i], p.tile, p.tile};
+      join.op[split++] = o[i];
+      tiles += jobs.g[i].count;
+    }
+  if (split > 0) {
+    hipLaunchKernelGGL(ffn_join_jobs_kernel, dim3((uint32_t)tiles, (uint32_t)join_blocks(p.tile, p.tile)), dim3(256), 0,
+                       stream, join);
+    PSPO_LAUNCHED("ffn_join_jobs_kernel", stream);
+  }
   return PSPO_OK;
 }
 
