@@ -199,22 +199,27 @@ __global__ __launch_bounds__(64 * kWaves) void qk_fwd_kernel(QkArgs a) {
   }
 }
 
-// Waves walk the tokens in steps of the grid and keep their sums of dz * xhat in
-// registers (one set for queries, one for keys); a work-group's sums are joined
-// in LDS, in wave order, and left in `partials`.
+// Grid y: queries, keys.  Waves walk the tokens in steps of grid x and keep their sums of
+// dz * xhat in registers; a work-group's sums are joined in LDS, in wave order, and left in
+// `partials`.  (One work-group for both sides held two sets of sums and weights: 196 registers,
+// two waves to a SIMD: 138 us against 131 at 28,481 tokens of 28 + 4 heads of 128.)
 template <class T, int L, bool kPast>
 __global__ __launch_bounds__(64 * kWaves) void qk_bwd_kernel(QkArgs a) {
   constexpr int kHeads = 64 / L;
   __shared__ float cs[kWaves][kMaxDim / 2], sn[kWaves][kMaxDim / 2];
-  __shared__ float sums[kWaves][2][kMaxDim];
+  __shared__ float sums[kWaves][kMaxDim];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int chunk = lane % L, sub = lane / L;
   const bool inside = chunk * 8 < a.D, turned = chunk * 8 < a.rot;
-  const Vec8 qw = weight8<T>(a.qw, chunk, inside), kw = weight8<T>(a.kw, chunk, inside);
-  const int64_t head_bytes = (int64_t)a.D * T::kBytes;
-  float acc[2][8] = {};
+  const bool keys = blockIdx.y != 0;
+  const Vec8 w = weight8<T>(keys ? a.kw : a.qw, chunk, inside);
+  const int H = keys ? a.Hk : a.Hq;
+  const int64_t head_bytes = (int64_t)a.D * T::kBytes, row_in = keys ? a.k_row : a.q_row, row_out = H * head_bytes;
+  const unsigned char *in = keys ? a.k : a.q, *grad = keys ? a.dk_out : a.dq_out;
+  unsigned char* out = keys ? a.k_out : a.q_out;
+  float acc[8] = {};
   // every wave of a work-group runs the same count of steps (the barriers)
-  for (int64_t n0 = (int64_t)blockIdx.x * kWaves; n0 < a.N; n0 += (int64_t)gridDim.x * kWaves) {
+  for (int64_t n0 = (int64_t)blockIdx.x * kWaves; H > 0 && n0 < a.N; n0 += (int64_t)gridDim.x * kWaves) {
     const int64_t n = n0 + wave;
     const bool live = n < a.N;
     __syncthreads();
@@ -222,70 +227,61 @@ __global__ __launch_bounds__(64 * kWaves) void qk_bwd_kernel(QkArgs a) {
     __syncthreads();
     if (!live) continue;
     const LaneTurn t = lane_turn(a, chunk, cs[wave], sn[wave], -1.f);
+    const unsigned char *xin = in + n * row_in, *din = grad + n * row_out;
+    unsigned char* dst = out + n * row_out;
+    constexpr int kAhead = 2;
+    for (int hb = 0; hb < H; hb += kAhead * kHeads) {
+      Raw8<T> xr[kAhead], dr[kAhead];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const int H = side ? a.Hk : a.Hq;
-      const unsigned char* xin = side ? a.k + n * a.k_row : a.q + n * a.q_row;
-      const unsigned char* din = (side ? a.dk_out : a.dq_out) + n * H * head_bytes;
-      unsigned char* dst = (side ? a.k_out : a.q_out) + n * H * head_bytes;
-      const Vec8& w = side ? kw : qw;
-      constexpr int kAhead = 4;
-      for (int hb = 0; hb < H; hb += kAhead * kHeads) {
-        Raw8<T> xr[kAhead], dr[kAhead];
+      for (int s = 0; s < kAhead; ++s) {
+        const int h = hb + s * kHeads + sub;
+        xr[s] = Raw8<T>{};
+        dr[s] = Raw8<T>{};
+        if (inside && h < H) {
+          xr[s] = load8<T, kPast>(xin + h * head_bytes, chunk);
+          dr[s] = load8<T, kPast>(din + h * head_bytes, chunk);
+        }
+      }
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) {
-          const int h = hb + s * kHeads + sub;
-          xr[s] = Raw8<T>{};
-          dr[s] = Raw8<T>{};
-          if (inside && h < H) {
-            xr[s] = load8<T, kPast>(xin + h * head_bytes, chunk);
-            dr[s] = load8<T, kPast>(din + h * head_bytes, chunk);
+      for (int s = 0; s < kAhead; ++s) {
+        if (hb + s * kHeads >= H) break;
+        const int h = hb + s * kHeads + sub;
+        const Vec8 x = unpack8(xr[s]), d = unpack8(dr[s]);
+        Vec8 dz = turn(d, t, a.interleaved, lane);
+        if (!turned) dz = d;
+        if (a.norm) {
+          float ss = 0.f, dot = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            ss += x.v[j] * x.v[j];
+            dot += dz.v[j] * w.v[j] * x.v[j];
+          }
+          const float rstd = 1.f / sqrtf(head_sum<L>(ss) * a.inv_d + a.eps);
+          const float m = head_sum<L>(dot) * a.inv_d * rstd * rstd;   // mean(dz w xhat) / rms
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            acc[j] += dz.v[j] * (x.v[j] * rstd);
+            dz.v[j] = rstd * (dz.v[j] * w.v[j] - x.v[j] * m);
           }
         }
-#pragma unroll
-        for (int s = 0; s < kAhead; ++s) {
-          if (hb + s * kHeads >= H) break;
-          const int h = hb + s * kHeads + sub;
-          const Vec8 x = unpack8(xr[s]), d = unpack8(dr[s]);
-          Vec8 dz = turn(d, t, a.interleaved, lane);
-          if (!turned) dz = d;
-          if (a.norm) {
-            float ss = 0.f, dot = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              ss += x.v[j] * x.v[j];
-              dot += dz.v[j] * w.v[j] * x.v[j];
-            }
-            const float rstd = 1.f / sqrtf(head_sum<L>(ss) * a.inv_d + a.eps);
-            const float m = head_sum<L>(dot) * a.inv_d * rstd * rstd;   // mean(dz w xhat) / rms
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              acc[side][j] += dz.v[j] * (x.v[j] * rstd);
-              dz.v[j] = rstd * (dz.v[j] * w.v[j] - x.v[j] * m);
-            }
-          }
-          if (inside && h < H) store8<T, kPast>(dst + h * head_bytes, chunk, dz);
-        }
+        if (inside && h < H) store8<T, kPast>(dst + h * head_bytes, chunk, dz);
       }
     }
   }
   if (a.partials == nullptr) return;   // uniform: no weight gradient is wanted
 #pragma unroll
-  for (int side = 0; side < 2; ++side)
+  for (int j = 0; j < 8; ++j) {
+    float x = acc[j];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float x = acc[side][j];
-#pragma unroll
-      for (int m = L; m < 64; m <<= 1) x += __shfl_xor(x, m);
-      if (sub == 0 && inside) sums[wave][side][chunk * 8 + j] = x;
-    }
+    for (int m = L; m < 64; m <<= 1) x += __shfl_xor(x, m);
+    if (sub == 0 && inside) sums[wave][chunk * 8 + j] = x;
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * a.D; i += 64 * kWaves) {
-    const int side = i / a.D, e = i % a.D;
+  for (int e = threadIdx.x; e < a.D; e += 64 * kWaves) {
     float x = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) x += sums[w][side][e];
-    a.partials[(int64_t)blockIdx.x * 2 * a.D + i] = x;
+    for (int w4 = 0; w4 < kWaves; ++w4) x += sums[w4][e];
+    a.partials[((int64_t)blockIdx.x * 2 + (keys ? 1 : 0)) * a.D + e] = x;
   }
 }
 
@@ -310,8 +306,8 @@ __global__ __launch_bounds__(1024) void qk_dweight_kernel(const float* partials,
   }
 }
 
-// Work-groups of the backward: four to a CU keep some 16 waves with their loads
-// in flight.
+// Work-groups of the backward and side: four to a CU keep some 16 waves with their
+// loads in flight.
 constexpr int kBwdGroups = 1024;
 
 int bwd_groups(int32_t N) {
@@ -326,7 +322,7 @@ int lanes_of(int D) {
 }
 
 // The forward stores past the caches, the backward loads and stores (28,481 tokens of 32 heads of
-// 128: 89 -> 73 us, 171 -> 162 us; the forward's loads too 84).
+// 128: 89 -> 73 us, 171 -> 162 us, before the later steps; the forward's loads too 84).
 bool past(const QkArgs& a, int bytes, int times) {
   return (int64_t)a.N * (a.Hq + a.Hk) * a.D * bytes * times >= kPastBytes;
 }
@@ -497,8 +493,8 @@ int pspo_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
     a.k_out = static_cast<unsigned char*>(dk);
     a.partials = want ? static_cast<float*>(workspace) : nullptr;
     const int L = lanes_of(head_dim);
-    if (type == PSPO_TYPE_F32) launch<F32>(a, L, dim3(groups), true, stream);
-    else launch<Bf16>(a, L, dim3(groups), true, stream);
+    if (type == PSPO_TYPE_F32) launch<F32>(a, L, dim3(groups, 2), true, stream);
+    else launch<Bf16>(a, L, dim3(groups, 2), true, stream);
     PSPO_LAUNCHED("qk_bwd_kernel", stream);
   }
   if (want) {

@@ -137,7 +137,7 @@ def _reference(s, pk, N, qkv):
     sur = torch.minimum(rho * adv, rho.clamp(1 - f32(0.1), 1 + f32(0.1)) * adv)
     loss = -(f32(1.0 / (P * K)) * d(pk["weight"][:N]) * sur).sum()
     loss.backward()
-    return float(loss), dict({n: t.grad for n, t in leaf.items()}, dq=q.grad, dk=k.grad, h0=h0.grad), rho.detach()
+    return float(loss.detach()), dict({n: t.grad for n, t in leaf.items()}, dq=q.grad, dk=k.grad, h0=h0.grad), rho.detach()
 
 
 def test_layer_run_against_autograd():
