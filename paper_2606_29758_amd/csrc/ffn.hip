@@ -10,13 +10,11 @@
 // operand type; each adds 2^-9 relative rms or less to a sum of f or N terms), the
 // outputs once; the pre-activations stay float32, because an error of theirs
 // enters the gradient twice (through act and act').
-#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
+#include "ffn_plan.h"
 #include "pspo_layer.h"
-#include "rowgemm.h"
-#include "skinny.h"
 #include "vec8.h"
 
 namespace pspo {
@@ -280,76 +278,6 @@ int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const floa
   return PSPO_OK;
 }
 
-// ---- plan ---------------------------------------------------------------------------
-// How a product of M x N entries over nk stages is covered: tiles of 256 x 256 (one
-// work-group to a CU), 128 x 128 (two) or 128 x 64 (three), the first `whole` of them launched
-// as they are and the rest in `parts` parts of K (parts = 1: all are whole).
-struct Plan {
-  int tile, tile_n, tiles_m, tiles_n, whole, parts;
-  double us;
-};
-constexpr int64_t kSlabBytes = int64_t(256) << 20;   // most that the parts of one product take
-
-// The cover of least estimated time: a stage of a full round takes 1.45, 1.1 or 0.9 us, one
-// with a work-group to a CU 0.7 us (128 x 128) or 0.5 us, each tile 20, 10 or 6 us beyond its
-// stages (dh, whose epilogue moves 14 bytes an entry: 55 or 16); the slabs of the parts are written
-// and read at 4.5 TB/s, and a further launch with its join takes 8 us.
-Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n, bool dh) {
-  Plan p{};
-  p.tile = tile;
-  p.tile_n = tile_n;
-  p.tiles_m = (int)((M + tile - 1) / tile);
-  p.tiles_n = (int)((N + tile_n - 1) / tile_n);
-  const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : tile_n == 128 ? 512 : 768;
-  const double extra = tile == 256 ? (dh ? 55 : 20) : tile_n == 128 ? (dh ? 16 : 10) : 6;
-  const double stage = tile == 256 ? 1.45 : tile_n == 128 ? 1.1 : 0.9;
-  const double single = tile == 256 ? 1.45 : tile_n == 128 ? 0.7 : 0.5;
-  auto time = [&](int64_t groups, int stages, double per_tile) {
-    const int64_t turns = (groups + slots - 1) / slots, rest = groups - (turns - 1) * slots;
-    const double last = rest <= 256 ? single : stage;
-    return (double)(turns - 1) * (stages * stage + per_tile) + stages * last + per_tile;
-  };
-  const int64_t before = (total - 1) / slots * slots, rest = total - before;   // the last round's tiles
-  p.whole = (int)total;
-  p.parts = 1;
-  p.us = time(total, nk, extra);
-  const double start = before ? time(before, nk, extra) : 0.0;
-  const int64_t bytes = (int64_t)tile * tile_n * 4;
-  // what a part writes: the columns that exist
-  const double written = (double)tile * (double)std::min<int64_t>(N, tile_n) * 4;
-  for (int s = 2; s <= 32 && s * 4 <= nk && rest * s * bytes <= kSlabBytes; ++s) {
-    const double us = start + time(rest * s, (nk + s - 1) / s, tile == 256 ? 10 : 5) + 8 + (double)(rest * s) * written * 2 / 4.5e6;
-    if (us < p.us) {
-      p.us = us;
-      p.whole = (int)before;
-      p.parts = s;
-    }
-  }
-  return p;
-}
-// dh: the product with that epilogue; the others may use 128 x 64, for few columns.
-Plan plan_of(int64_t M, int64_t N, int nk, bool dh) {
-  Plan best = plan_tile(M, N, nk, 128, 128, dh);
-  const Plan big = plan_tile(M, N, nk, 256, 256, dh);
-  if (big.us <= best.us) best = big;
-  if (!dh && N <= 64) {
-    const Plan thin = plan_tile(M, N, nk, 128, 64, dh);
-    if (thin.us < best.us) best = thin;
-  }
-  return best;
-}
-int64_t slab_bytes(int64_t M, int64_t N, int K, bool dh) {
-  if (M == 0 || N == 0) return 0;
-  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK, dh);
-  if (p.parts == 1) return 0;
-  return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile_n * 4;
-}
-
-// A work-group alone on its CU has its stages' loads wait for memory, with one stage in flight:
-// launches of no more work-groups than CUs take a ring of four stages instead of two.
-constexpr int kDeep = 4;
-bool deep_ring(int64_t groups) { return groups <= 256; }
-
 template <bool kOuterA, bool kOuterB, class Op>
 int launch(const RowShape& g, const Plan& p, const Epi<Op>& epi, const char* name, hipStream_t stream) {
   const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
@@ -391,56 +319,6 @@ int product(RowShape g, int64_t M, int64_t N, const Op& op, float* slab, const c
   g.parts = p.parts;
   if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {slab, (int)N}}, name, stream)) return rc;
   return join_parts(op, g, p.tile, p.tile_n, slab, stream);
-}
-
-// The three products behind dh, as one launch: dx, the two upper weights' gradients, the
-// lower one's.  All tiles of a size; a product whose tiles have more K stages than a
-// work-group's share of the whole is split along K.
-struct JobPlan {
-  int tile;
-  int tiles_m[3], tiles_n[3], parts[3];
-  int64_t slab[3], slab_bytes;   // bytes from the slabs' start; all of them
-  double us;
-};
-JobPlan plan_jobs(const int64_t (&M)[3], const int64_t (&N)[3], const int (&nk)[3], int tile) {
-  JobPlan p{};
-  p.tile = tile;
-  const int64_t slots = tile == 256 ? 256 : 512, bytes = (int64_t)tile * tile * 4;
-  int64_t units = 0, groups = 0;
-  for (int i = 0; i < 3; ++i) {
-    p.tiles_m[i] = (int)((M[i] + tile - 1) / tile);
-    p.tiles_n[i] = (int)((N[i] + tile - 1) / tile);
-    units += (int64_t)p.tiles_m[i] * p.tiles_n[i] * nk[i];
-  }
-  const int64_t share = std::max<int64_t>(units / slots, 4);
-  int longest = 0;
-  for (int i = 0; i < 3; ++i) {
-    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
-    int64_t s = std::min<int64_t>((nk[i] + share - 1) / share, 32);
-    s = std::max<int64_t>(std::min<int64_t>(s, tiles ? kSlabBytes / 3 / (tiles * bytes) : 1), 1);
-    p.parts[i] = (int)s;
-    p.slab[i] = p.slab_bytes;
-    if (s > 1) p.slab_bytes += tiles * s * bytes;
-    groups += tiles * s;
-    if (tiles) longest = std::max(longest, (int)((nk[i] + s - 1) / s));
-  }
-  // A round's stages, half of the longest part idle at the end, the slabs out and in.  A stage of
-  // the small tiles takes 0.85 us here (stages of different products meet on a CU; with 1.1 as for
-  // one product, 777 tokens, d = 1000, f = 4104 would take the large tiles: 72 us with its join
-  // against 61; 300 tokens, d = 2048, f = 8192: 116 against 98).
-  const bool alone = tile == 128 && groups <= 256;
-  const double stage = tile == 256 ? 1.45 : alone ? 0.7 : 0.85;
-  const double rounds = (double)groups / (double)slots;
-  p.us = std::max((double)units / (double)slots + longest * 0.5, (double)longest) * stage +
-         std::max(rounds, 1.0) * (tile == 256 ? 10 : 5) + (double)p.slab_bytes * 2 / 4.5e6 + (p.slab_bytes ? 8 : 0);
-  return p;
-}
-JobPlan plan_backward(int64_t N, int64_t d, int64_t f) {
-  const int64_t M[3] = {N > 0 ? d : 0, d, f}, C[3] = {N, 2 * f, d};
-  const int kd = (int)((f + kRowK - 1) / kRowK * 2), kn = (int)((N + kRowK - 1) / kRowK);
-  const int nk[3] = {kd, kn, kn};
-  const JobPlan big = plan_jobs(M, C, nk, 256), small = plan_jobs(M, C, nk, 128);
-  return big.us <= small.us ? big : small;
 }
 
 int run_jobs(const JobPlan& p, const RowShape (&g)[3], const EpiStore (&o)[3], unsigned char* slabs,
@@ -507,15 +385,6 @@ struct SkinnyStore {
   }
 };
 
-// Whether a forward of N tokens goes by these kernels.  They read every token's rows again for
-// each 16 rows of the weights, the 128 x 64 tiles write and join slabs instead: us a call, this
-// way / tiles, on 6 d f bytes of weights: d = 3584, f = 14336 (308 MB) N = 1 65 / 77, 16 90 / 82;
-// 1536, 6144 (57 MB) N = 16 26 / 28, 32 33 / 30; 2048, 800 (10 MB) N = 48 17 / 26; 512, 1344
-// (4 MB) N = 64 15 / 19.
-bool few_tokens(int64_t N, int64_t d, int64_t f) {
-  return N <= kSkinnyTokens && (N - 12) * (6 * d * f) <= int64_t(300) << 20;
-}
-
 // Waves of a work-group: enough that the chip holds some 4,096, at most one for each
 // step of K and 64 KB of sums.
 template <int kMats, class Epi>
@@ -536,33 +405,6 @@ int skinny(const SkinnyArgs& a, const Epi& epi, const char* name, hipStream_t st
 #undef PSPO_SKINNY
   PSPO_LAUNCHED(name, stream);
   return PSPO_OK;
-}
-
-// Workspace layout of one call.
-struct Space {
-  int64_t h, dgu, pre, slab, total;
-};
-Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept) {
-  Space s{};
-  int64_t at = 0;
-  auto take = [&](int64_t bytes) {
-    const int64_t a = at;
-    at = round_up(at + bytes, 256);
-    return a;
-  };
-  s.h = take(N * f * 2);
-  int64_t slab = 0;
-  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, false);
-  if (backward) {
-    s.dgu = take(N * 2 * f * 2);
-    if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab, slab_bytes(f, N, (int)d, true), plan_backward(N, d, f).slab_bytes});
-  } else if (!few_tokens(N, d, f)) {
-    slab = std::max(slab, slab_bytes(d, N, (int)f, false));
-  }
-  s.slab = take(slab);
-  s.total = at;
-  return s;
 }
 
 constexpr int kMaxWidth = 1 << 20;   // d and f: a tile's rows stay below 2^31 bytes
