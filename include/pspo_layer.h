@@ -128,7 +128,9 @@ int pspo_dropout_bwd(const void* dy, const int32_t* row_ids, int32_t N, int32_t 
 #define PSPO_FFN_BACKWARD 512u /* the backward call's workspace instead of the forward's */
 #define PSPO_FFN_PREACT  1024u /* ... with the forward's pre-activations given */
 
-/* Bytes of device workspace the calls below need for N tokens (host-only); 0 for sizes they refuse. */
+/* Bytes of device workspace the calls below need for N tokens (host-only); 0 for sizes they refuse.
+ * The size for N tokens serves every call of fewer (same d, f and flags).  Up to 256 MB of it hold
+ * the sums of products that are split along K. */
 size_t pspo_gated_ffn_workspace_bytes(int32_t N, int32_t d, int32_t f, uint32_t flags);
 
 /*

@@ -67,13 +67,6 @@ inline Plan plan_of(int64_t M, int64_t N, int nk, bool dh) {
   }
   return best;
 }
-inline int64_t slab_bytes(int64_t M, int64_t N, int K, bool dh) {
-  if (M == 0 || N == 0) return 0;
-  const Plan p = plan_of(M, N, (K + kRowK - 1) / kRowK, dh);
-  if (p.parts == 1) return 0;
-  return ((int64_t)p.tiles_m * p.tiles_n - p.whole) * p.parts * p.tile * p.tile_n * 4;
-}
-
 // A work-group alone on its CU has its stages' loads wait for memory, with one stage in flight:
 // launches of no more work-groups than CUs take a ring of four stages instead of two.
 constexpr int kDeep = 4;
@@ -138,7 +131,40 @@ inline bool few_tokens(int64_t N, int64_t d, int64_t f) {
   return N <= kSkinnyTokens && (N - 12) * (6 * d * f) <= int64_t(300) << 20;
 }
 
-// Workspace layout of one call.
+// Most that the parts of any N' <= N take: the plans' own need goes up and down with N (a last
+// round of few tiles is cut finer than one of many), and a workspace asked for N has to serve
+// fewer tokens too.  Tiles of 128 x 64 take no more than the 128 x 128 ones stand for here; up to
+// 128 columns those have as many rounds as the 256 x 256 ones, shorter, and are taken.
+inline int64_t slab_reserve(int64_t M, int64_t N, int K) {
+  const int64_t most = std::min<int64_t>((K + kRowK - 1) / kRowK / 4, 32);   // parts, plan_tile's limits
+  if (most < 2) return 0;
+  int64_t bytes = 0;
+  for (const int64_t tile : {128, 256}) {
+    if (tile == 256 && N <= 128) break;
+    const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile), slots = tile == 256 ? 256 : 512;
+    bytes = std::max(bytes, std::min(tiles, slots) * most * tile * tile * 4);
+  }
+  return std::min(bytes, kSlabBytes);
+}
+inline int64_t jobs_reserve(int64_t N, int64_t d, int64_t f) {
+  const int64_t M[3] = {N > 0 ? d : 0, d, f}, C[3] = {N, 2 * f, d};
+  const int64_t nk[3] = {(f + kRowK - 1) / kRowK * 2, (N + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK};
+  int64_t bytes = 0;
+  for (const int64_t tile : {128, 256}) {
+    int64_t sum = 0;
+    for (int i = 0; i < 3; ++i) {
+      const int64_t most = std::min<int64_t>((nk[i] + 3) / 4, 32);   // plan_jobs: a share is 4 stages at least
+      // a product of as many tiles as there are slots has more stages in its share than a tile holds
+      const int64_t tiles = std::min<int64_t>(((M[i] + tile - 1) / tile) * ((C[i] + tile - 1) / tile),
+                                              tile == 256 ? 256 : 512);
+      if (most >= 2) sum += std::min(tiles * most * tile * tile * 4, kSlabBytes / 3);
+    }
+    bytes = std::max(bytes, sum);
+  }
+  return bytes;
+}
+
+// Workspace layout of one call; no part of it shrinks with more tokens.
 struct Space {
   int64_t h, dgu, pre, slab, total;
 };
@@ -152,13 +178,13 @@ inline Space space_of(int64_t N, int64_t d, int64_t f, bool backward, bool kept)
   };
   s.h = take(N * f * 2);
   int64_t slab = 0;
-  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_bytes(2 * f, N, (int)d, false);
+  if ((!backward || !kept) && !few_tokens(N, d, f)) slab = slab_reserve(2 * f, N, (int)d);
   if (backward) {
     s.dgu = take(N * 2 * f * 2);
     if (!kept) s.pre = take(N * 2 * f * 4);
-    slab = std::max({slab, slab_bytes(f, N, (int)d, true), plan_backward(N, d, f).slab_bytes});
+    slab = std::max({slab, slab_reserve(f, N, (int)d), jobs_reserve(N, d, f)});
   } else if (!few_tokens(N, d, f)) {
-    slab = std::max(slab, slab_bytes(d, N, (int)f, false));
+    slab = std::max(slab, slab_reserve(d, N, (int)f));
   }
   s.slab = take(slab);
   s.total = at;

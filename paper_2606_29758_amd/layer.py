@@ -365,6 +365,7 @@ def _ffn_weights(w_gate, w_up, w_down):
 
 
 def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, preact: bool = False) -> int:
+    """Bytes of workspace that gated_ffn (gated_ffn_bwd; with kept pre-activations) takes for up to N tokens."""
     flags = (FFN_BACKWARD if backward else 0) | (FFN_PREACT if preact else 0)
     return int(load().pspo_gated_ffn_workspace_bytes(N, d, f, flags))
 

@@ -1,0 +1,37 @@
+"""GPU: calls of the layer operators that a program makes beside the plain ones: one workspace for changing
+token counts, empty calls, refused arguments."""
+import pytest
+import torch
+
+from paper_2606_29758_amd import layer
+
+pytestmark = pytest.mark.gpu
+BF, F4 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    layer.load()
+
+
+def _ffn(N, d, f, seed=0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    new = lambda *s, k=1.0: (torch.randn(*s, device="cuda", generator=g) * k).to(BF)   # noqa: E731
+    return (new(N, d), new(f, d, k=1 / d ** 0.5), new(f, d, k=1 / d ** 0.5), new(d, f, k=1 / f ** 0.5),
+            new(N, d, k=0.1))
+
+
+def test_one_workspace_for_fewer_tokens():
+    """A workspace asked for the largest count serves every smaller one, with the same bits as one of its own."""
+    cap, d, f = 1025, 1000, 4104
+    x, wg, wu, wd, dy = _ffn(cap, d, f)
+    fwd = torch.empty(layer.gated_ffn_workspace_bytes(cap, d, f), dtype=torch.uint8, device="cuda")
+    bwd = torch.empty(layer.gated_ffn_workspace_bytes(cap, d, f, True, True), dtype=torch.uint8, device="cuda")
+    for N in (1, 20, 64, 65, 128, 129, 200, 257, 400, 513, 777, 1000, 1024, 1025):
+        a = layer.gated_ffn(x, wg, wu, wd, N, keep=True, workspace=fwd)
+        b = layer.gated_ffn(x, wg, wu, wd, N, keep=True)
+        assert torch.equal(a["y"], b["y"]) and torch.equal(a["preact"], b["preact"]), N
+        p = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, preact=a["preact"], workspace=bwd)
+        q = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, preact=a["preact"])
+        assert all(torch.equal(p[k], q[k]) for k in ("dx", "dw_gate", "dw_up", "dw_down")), N

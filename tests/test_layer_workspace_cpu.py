@@ -1,0 +1,43 @@
+"""Workspace sizes of the layer operators (host functions, no GPU): a size asked for N tokens serves every
+call of fewer, since the count of kept tokens changes with each draw of the cutoffs."""
+import subprocess
+
+import pytest
+
+import ffn_plan
+from paper_2606_29758_amd import layer
+
+WIDTHS = [(3584, 14336), (1536, 6144), (1000, 4104), (64, 72), (8, 8), (8, 4096), (4096, 8), (2048, 800), (512, 1344),
+          (568, 7952)]
+
+
+def _counts():
+    """Every count up to 300 tokens, then steps that meet every remainder of a tile, then around powers of two."""
+    return sorted({*range(300), *range(300, 9000, 7), *range(9000, 70000, 131),
+                   *(2 ** b + e for b in range(10, 20) for e in (-1, 1, 129))})
+
+
+@pytest.mark.parametrize("d,f", WIDTHS)
+@pytest.mark.parametrize("way", [dict(), dict(backward=True), dict(backward=True, preact=True)])
+def test_ffn_workspace_never_falls(d, f, way):
+    last, at = 0, 0
+    for N in _counts():
+        n = layer.gated_ffn_workspace_bytes(N, d, f, **way)
+        assert n >= last, (at, N, last, n)
+        last, at = n, N
+
+
+def test_head_norm_workspace_never_falls():
+    lib = layer.load()
+    last = 0
+    for N in _counts():
+        n = lib.pspo_qk_norm_rope_workspace_bytes(N, 128)
+        assert n >= last, N
+        last = n
+
+
+def test_plans_fit_the_workspace(tmp_path):
+    """The slabs that the plans take, over many sizes, against the workspace's layout (host build of ffn_plan.h)."""
+    exe = ffn_plan.build(tmp_path)
+    run = subprocess.run([exe, "need"], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and run.stdout.strip() == "ok", run.stdout + run.stderr
