@@ -67,7 +67,8 @@ int pspo_qk_norm_rope_fwd(const void* q, const void* k, int64_t q_stride, int64_
                           int32_t head_dim, int32_t rot_dim, float eps, int32_t type, uint32_t flags,
                           void* q_out, void* k_out, int32_t* err_flag, hipStream_t stream);
 
-/* Bytes of device workspace pspo_qk_norm_rope_bwd needs (host-only). */
+/* Bytes of device workspace pspo_qk_norm_rope_bwd needs for N tokens (host-only), enough for fewer too;
+ * 0 for sizes it refuses. */
 size_t pspo_qk_norm_rope_workspace_bytes(int32_t N, int32_t head_dim);
 
 /*

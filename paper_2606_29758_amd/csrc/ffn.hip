@@ -444,7 +444,7 @@ extern "C" {
 
 size_t pspo_gated_ffn_workspace_bytes(int32_t N, int32_t d, int32_t f, uint32_t flags) {
   using namespace pspo;
-  if (N < 0 || d <= 0 || f <= 0 || d > kMaxWidth || f > kMaxWidth) return 0;
+  if (N < 0 || d <= 0 || f <= 0 || d % 8 != 0 || f % 8 != 0 || d > kMaxWidth || f > kMaxWidth) return 0;
   const bool bwd = (flags & PSPO_FFN_BACKWARD) != 0;
   return (size_t)space_of(N, d, f, bwd, (flags & PSPO_FFN_PREACT) != 0).total;
 }

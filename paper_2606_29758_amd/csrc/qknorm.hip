@@ -348,6 +348,10 @@ void launch(const QkArgs& a, int L, dim3 grid, bool backward, hipStream_t stream
   else p ? launch_fwd<T, true>(a, L, grid, stream) : launch_fwd<T, false>(a, L, grid, stream);
 }
 
+bool head_dim_fits(int32_t D) { return D >= 8 && D % 8 == 0 && D <= kMaxDim; }
+// A launch holds less than 2^32 threads along x.
+bool tokens_fit(int32_t N) { return ((int64_t)N + kWaves - 1) / kWaves < (int64_t(1) << 24); }
+
 // Checks shared by both directions; fills the common arguments.
 int check(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const void* qw, const void* kw,
           const float* inv_freq, const int32_t* positions, const int32_t* seq_id, const int32_t* cu,
@@ -356,7 +360,7 @@ int check(const void* q, const void* k, int64_t q_stride, int64_t k_stride, cons
   PSPO_REQUIRE(N >= 0 && R >= 0, PSPO_ERR_INVALID_ARG, "N and R must be >= 0");
   PSPO_REQUIRE(Hq >= 1 && Hk >= 0, PSPO_ERR_INVALID_ARG, "heads_q must be >= 1 and heads_k >= 0");
   PSPO_REQUIRE(Hq <= 65536 && Hk <= 65536, PSPO_ERR_UNSUPPORTED, "at most 65536 heads");
-  PSPO_REQUIRE(D >= 8 && D % 8 == 0 && D <= kMaxDim, PSPO_ERR_UNSUPPORTED,
+  PSPO_REQUIRE(head_dim_fits(D), PSPO_ERR_UNSUPPORTED,
                "head_dim must be a multiple of 8, at most 512");
   PSPO_REQUIRE(rot >= 0 && rot % 16 == 0 && rot <= D, PSPO_ERR_UNSUPPORTED,
                "rot_dim must be a multiple of 16, at most head_dim");
@@ -372,8 +376,7 @@ int check(const void* q, const void* k, int64_t q_stride, int64_t k_stride, cons
                "rows must be 16-byte aligned");
   PSPO_REQUIRE(q_stride < (int64_t(1) << 40) && (Hk == 0 || k_stride < (int64_t(1) << 40)), PSPO_ERR_INVALID_ARG,
                "row stride out of range");
-  PSPO_REQUIRE(((int64_t)N + kWaves - 1) / kWaves < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED,
-               "at most 2^26 tokens per call");
+  PSPO_REQUIRE(tokens_fit(N), PSPO_ERR_UNSUPPORTED, "at most 2^26 tokens per call");
   if (N > 0) {
     PSPO_REQUIRE(q && (k || Hk == 0), PSPO_ERR_INVALID_ARG, "null input pointer");
     PSPO_REQUIRE(aligned(q, 16) && aligned(k, 16) && aligned(qw, 16) && aligned(kw, 16) && aligned(inv_freq, 4) &&
@@ -451,7 +454,7 @@ int pspo_qk_norm_rope_fwd(const void* q, const void* k, int64_t q_stride, int64_
 }
 
 size_t pspo_qk_norm_rope_workspace_bytes(int32_t N, int32_t head_dim) {
-  if (N < 0 || head_dim < 0) return 0;
+  if (N < 0 || !pspo::tokens_fit(N) || !pspo::head_dim_fits(head_dim)) return 0;
   return (size_t)pspo::bwd_groups(N) * 2 * (size_t)head_dim * sizeof(float);
 }
 

@@ -41,3 +41,13 @@ def test_plans_fit_the_workspace(tmp_path):
     exe = ffn_plan.build(tmp_path)
     run = subprocess.run([exe, "need"], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and run.stdout.strip() == "ok", run.stdout + run.stderr
+
+
+def test_no_size_for_widths_that_the_calls_refuse():
+    for d, f in ((60, 72), (64, 70), (1, 8), (8, 4)):
+        for way in (dict(), dict(backward=True), dict(backward=True, preact=True)):
+            assert layer.gated_ffn_workspace_bytes(4, d, f, **way) == 0, (d, f, way)
+    lib = layer.load()
+    for D in (-8, 0, 4, 12, 520):
+        assert lib.pspo_qk_norm_rope_workspace_bytes(4, D) == 0, D
+    assert lib.pspo_qk_norm_rope_workspace_bytes(1 << 27, 128) == 0   # more tokens than a call takes
