@@ -160,7 +160,7 @@ int pspo_gated_ffn_fwd(const uint16_t* x, const uint16_t* w_gate, const uint16_t
  *  preact        what the forward wrote, or NULL: computed again (in the workspace).
  *  dx            device, bf16 bits [N, d] out.
  *  dw_gate, dw_up, dw_down   device, of the weights' shapes, out: bf16, or float32
- *                with PSPO_FFN_DW_F32; N = 0 writes (or adds) zeros.
+ *                with PSPO_FFN_DW_F32; N = 0 writes (or adds) zeros and takes workspace NULL.
  */
 int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_gate, const uint16_t* w_up,
                        const uint16_t* w_down, const float* preact, int32_t N, int32_t d, int32_t f,

@@ -486,9 +486,9 @@ int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_
   PSPO_REQUIRE((flags & ~(PSPO_FFN_DW_F32 | PSPO_ACCUMULATE_DW)) == 0, PSPO_ERR_INVALID_ARG, "unknown flag bits");
   const bool f32 = (flags & PSPO_FFN_DW_F32) != 0, add = (flags & PSPO_ACCUMULATE_DW) != 0;
   PSPO_REQUIRE(f32 || !add, PSPO_ERR_INVALID_ARG, "accumulating needs float32 weight gradients");
-  PSPO_REQUIRE(w_gate && w_up && w_down && dw_gate && dw_up && dw_down && workspace, PSPO_ERR_INVALID_ARG,
+  PSPO_REQUIRE(w_gate && w_up && w_down && dw_gate && dw_up && dw_down, PSPO_ERR_INVALID_ARG,
                "null pointer argument");
-  PSPO_REQUIRE(N == 0 || (dy && x && dx), PSPO_ERR_INVALID_ARG, "null pointer argument");
+  PSPO_REQUIRE(N == 0 || (dy && x && dx && workspace), PSPO_ERR_INVALID_ARG, "null pointer argument");
   PSPO_REQUIRE(aligned(dy, 16) && aligned(x, 16) && aligned(w_gate, 16) && aligned(w_up, 16) && aligned(w_down, 16) &&
                    aligned(preact, 16) && aligned(dx, 16) && aligned(dw_gate, 16) && aligned(dw_up, 16) &&
                    aligned(dw_down, 16) && aligned(workspace, 256),

@@ -35,3 +35,16 @@ def test_one_workspace_for_fewer_tokens():
         p = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, preact=a["preact"], workspace=bwd)
         q = layer.gated_ffn_bwd(dy, x, wg, wu, wd, N, preact=a["preact"])
         assert all(torch.equal(p[k], q[k]) for k in ("dx", "dw_gate", "dw_up", "dw_down")), N
+
+
+def test_an_empty_backward_without_a_workspace():
+    """No tokens ask for 0 bytes: the C call takes NULL and writes (or adds) zeros."""
+    lib, d, f = layer.load(), 64, 72
+    _, wg, wu, wd, _ = _ffn(1, d, f)
+    assert layer.gated_ffn_workspace_bytes(0, d, f, True) == 0
+    dw = [torch.full(s, 3.0, device="cuda") for s in ((f, d), (f, d), (d, f))]
+    for flags, want in ((256 + 1, 3.0), (256, 0.0)):   # float32 gradients: added to, then written
+        rc = lib.pspo_gated_ffn_bwd(None, None, wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), None, 0, d, f, 0, flags, None,
+                                    *(t.data_ptr() for t in dw), None, 0, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0, lib.pspo_last_error()
+        assert all((t == want).all() for t in dw)

@@ -3,6 +3,7 @@ call of fewer, since the count of kept tokens changes with each draw of the cuto
 import subprocess
 
 import pytest
+import torch
 
 import ffn_plan
 from paper_2606_29758_amd import layer
@@ -51,3 +52,17 @@ def test_no_size_for_widths_that_the_calls_refuse():
     for D in (-8, 0, 4, 12, 520):
         assert lib.pspo_qk_norm_rope_workspace_bytes(4, D) == 0, D
     assert lib.pspo_qk_norm_rope_workspace_bytes(1 << 27, 128) == 0   # more tokens than a call takes
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="addresses that no device call may touch")
+def test_an_empty_call_takes_the_workspace_it_asked_for():
+    """No tokens: 0 bytes are asked for, and the backward takes NULL for them (here up to the device check)."""
+    lib = layer.load()
+    A = 0x10000
+    for flags, pre in ((512, None), (512 + 1024, A)):
+        assert lib.pspo_gated_ffn_workspace_bytes(0, 64, 72, flags) == 0
+        rc = lib.pspo_gated_ffn_bwd(None, None, A, A, A, pre, 0, 64, 72, 0, 0, None, A, A, A, None, 0, None)
+        assert "null pointer" not in lib.pspo_last_error().decode(), (rc, lib.pspo_last_error())
+    # with tokens it is asked for
+    assert lib.pspo_gated_ffn_bwd(A, A, A, A, A, None, 4, 64, 72, 0, 0, A, A, A, A, None, 0, None) == 1
+    assert "null pointer" in lib.pspo_last_error().decode()
