@@ -127,10 +127,19 @@ def _ints(t: Optional[torch.Tensor], n: int, name: str, device: int) -> None:
         raise ValueError(f"{name} must be [>= {n}], got {list(t.shape)}")
 
 
+_MOST = 2 ** 31 - 1   # the C calls take 32-bit counts, and ctypes passes the low bits of a larger number
+
+
+def _fits(n: int, name: str) -> int:
+    if n > _MOST:
+        raise ValueError(f"{name} must be at most {_MOST}, got {n}")
+    return n
+
+
 def _count(N: int) -> int:
     if N < 0:
         raise ValueError("N must be >= 0")
-    return int(N)
+    return _fits(int(N), "N")
 
 
 # ---------------------------------------------------------------------------
@@ -150,6 +159,7 @@ def _heads(t: torch.Tensor, N: int, name: str, device: int, like: Optional[torch
     if like is not None and t.dtype != like.dtype:
         raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
     _, H, D = t.shape
+    _fits(max(H, D), f"heads and head_dim of {name}")
     if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
         raise ValueError(f"the heads of {name} must be contiguous within a row")
     return t
@@ -181,7 +191,7 @@ def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seql
         _here(inv_freq, torch.float32, "inv_freq", device)
         if inv_freq.dim() != 1:
             raise ValueError("inv_freq must be [rot_dim / 2]")
-        rot = 2 * inv_freq.shape[0]
+        rot = _fits(2 * inv_freq.shape[0], "rot_dim")
         if positions is not None:
             _ints(positions, N, "positions", device)
             seq_id = cu_seqlens = first_pos = None
@@ -190,7 +200,7 @@ def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seql
                 raise ValueError("positions, or seq_id and cu_seqlens, must be given")
             _ints(seq_id, N, "seq_id", device)
             _ints(cu_seqlens, 1, "cu_seqlens", device)
-            R = cu_seqlens.shape[0] - 1
+            R = _fits(cu_seqlens.shape[0] - 1, "R")
             _ints(first_pos, R, "first_pos", device)
     else:
         positions = seq_id = cu_seqlens = first_pos = None
@@ -297,7 +307,7 @@ def dropout_add(x, N: int, p: float, seed: int, offset: int = 0, residual: Optio
     ty = _type(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be [>= N, d]")
-    d = x.shape[1]
+    d = _fits(x.shape[1], "d")
     _rows(x, N, (d,), "x")
     _here(x, x.dtype, "x", device)
     if residual is not None:
@@ -326,7 +336,7 @@ def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optio
     ty = _type(dy, "dy")
     if dy.dim() != 2:
         raise ValueError("dy must be [>= N, d]")
-    d = dy.shape[1]
+    d = _fits(dy.shape[1], "d")
     _rows(dy, N, (d,), "dy")
     _here(dy, dy.dtype, "dy", device)
     _ints(row_ids, N, "row_ids", device)
@@ -357,6 +367,7 @@ def _ffn_weights(w_gate, w_up, w_down):
     if w_gate.dim() != 2:
         raise ValueError("w_gate must be [f, d]")
     f, d = w_gate.shape
+    _fits(max(d, f), "d and f")
     _exact(w_up, (f, d), "w_up")
     _exact(w_down, (d, f), "w_down")
     for name, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
@@ -367,7 +378,7 @@ def _ffn_weights(w_gate, w_up, w_down):
 def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, preact: bool = False) -> int:
     """Bytes of workspace that gated_ffn (gated_ffn_bwd; with kept pre-activations) takes for up to N tokens."""
     flags = (FFN_BACKWARD if backward else 0) | (FFN_PREACT if preact else 0)
-    return int(load().pspo_gated_ffn_workspace_bytes(N, d, f, flags))
+    return int(load().pspo_gated_ffn_workspace_bytes(_fits(N, "N"), _fits(d, "d"), _fits(f, "f"), flags))
 
 
 def _ffn_workspace(workspace, N, d, f, flags, like, device):
