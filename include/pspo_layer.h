@@ -14,7 +14,8 @@
  *
  * "First N rows": every call reads and writes rows 0 .. N-1 of its per-token
  * tensors and leaves the rows behind them as they were.  N = 0 is valid; the
- * gradients of weights are then zero.  Outputs must not alias inputs.
+ * gradients of weights are then zero.  Outputs and workspaces must not alias
+ * inputs or each other.
  */
 #ifndef PSPO_LAYER_H_
 #define PSPO_LAYER_H_

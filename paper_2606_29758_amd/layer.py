@@ -106,17 +106,24 @@ def _exact(t: torch.Tensor, shape, name: str) -> None:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
-def _apart(out: torch.Tensor, name: str, *ins) -> None:
-    """Outputs must not alias inputs."""
-    if out.numel() == 0:
+def _apart(out: torch.Tensor, name: str, *others, used: Optional[int] = None) -> None:
+    """`out` (its first `used` bytes, if given) must not share memory with the call's other tensors."""
+    size = out.numel() * out.element_size()
+    if used is not None and used < size:
+        size = used
+    if size == 0:
         return
-    lo, hi = out.data_ptr(), out.data_ptr() + out.numel() * out.element_size()
-    for t in ins:
+    lo = out.data_ptr()
+    hi = lo + size
+    for t in others:
         if t is None or t.numel() == 0:
             continue
-        last = sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
-        if t.data_ptr() < hi and t.data_ptr() + (last + 1) * t.element_size() > lo:
-            raise ValueError(f"{name} overlaps an input")
+        at = t.data_ptr()
+        if at >= hi:
+            continue
+        last = t.numel() - 1 if t.is_contiguous() else sum((s - 1) * st for s, st in zip(t.shape, t.stride()))
+        if at + (last + 1) * t.element_size() > lo:
+            raise ValueError(f"{name} overlaps an input or another output")
 
 
 def _ints(t: Optional[torch.Tensor], n: int, name: str, device: int) -> None:
@@ -210,7 +217,8 @@ def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seql
     heads = (N, R, q.shape[1], 0 if k is None else k.shape[1], D, rot)
     ins = (q.data_ptr(), _ptr(k), _row_stride(q), _row_stride(k), _ptr(q_weight), _ptr(k_weight), _ptr(inv_freq),
            _ptr(positions), _ptr(seq_id), _ptr(cu_seqlens), _ptr(first_pos))
-    return device, ty, D, flags, ins, heads
+    read = (q, k, q_weight, k_weight, inv_freq, positions, seq_id, cu_seqlens, first_pos, err_flag)
+    return device, ty, D, flags, ins, heads, read
 
 
 def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq_id=None, cu_seqlens=None,
@@ -226,8 +234,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq
     Returns q and k ([N, H, D] contiguous; k None if there is none).
     """
     N = _count(N)
-    device, ty, D, flags, ins, heads = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens,
-                                                  first_pos, interleaved, norm, err_flag)
+    device, ty, D, flags, ins, heads, read = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id,
+                                                        cu_seqlens, first_pos, interleaved, norm, err_flag)
     outs = []
     for name, x, o in (("q_out", q, q_out), ("k_out", k, k_out)):
         if x is None:
@@ -238,7 +246,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq
         else:
             _rows(o, N, (x.shape[1], D), name)
             _here(o, x.dtype, name, device)
-            _apart(o, name, q, k, q_weight, k_weight, *outs)
+            _apart(o, name, *read, *outs)
         outs.append(o)
     qo, ko = outs
     _check((_lib or load()).pspo_qk_norm_rope_fwd(*ins, *heads, eps, ty, flags, qo.data_ptr(), _ptr(ko),
@@ -260,8 +268,8 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int,
     (unless want_weights is False), dq_weight and dk_weight (float32 [D]).
     """
     N = _count(N)
-    device, ty, D, flags, ins, heads = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seqlens,
-                                                  first_pos, interleaved, norm, err_flag)
+    device, ty, D, flags, ins, heads, read = _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id,
+                                                        cu_seqlens, first_pos, interleaved, norm, err_flag)
     if (k is None) != (dk_out is None):
         raise ValueError("k and dk_out must be both given or both None")
     dx = []
@@ -275,12 +283,14 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, inv_freq, N: int,
     dw = [torch.empty(D, dtype=torch.float32, device=q.device) if w is not None and want_weights else None
           for w in (q_weight, k_weight)]
     lib = _lib or load()
-    if workspace is None:
-        if dw[0] is not None or dw[1] is not None:
-            need = lib.pspo_qk_norm_rope_workspace_bytes(N, D)
-            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    else:
+    if workspace is not None:
         _here(workspace, torch.uint8, "workspace", device)
+    if dw[0] is not None or dw[1] is not None:
+        need = lib.pspo_qk_norm_rope_workspace_bytes(N, D)
+        if workspace is None:
+            workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        else:
+            _apart(workspace, "workspace", *read, dq_out, dk_out, used=need)
     _check(lib.pspo_qk_norm_rope_bwd(
         dq_out.data_ptr(), _ptr(dk_out), *ins, *heads, eps, ty, flags, dx[0].data_ptr(), _ptr(dx[1]), _ptr(dw[0]),
         _ptr(dw[1]), _ptr(err_flag), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(device)))
@@ -319,7 +329,7 @@ def dropout_add(x, N: int, p: float, seed: int, offset: int = 0, residual: Optio
     else:
         _rows(out, N, (d,), "out")
         _here(out, x.dtype, "out", device)
-        _apart(out, "out", x, residual)
+        _apart(out, "out", x, residual, row_ids)
     _check((_lib or load()).pspo_dropout_add_fwd(x.data_ptr(), _ptr(residual), _ptr(row_ids), N, d, p, seed & _U64_MASK,
                                                  offset & _U64_MASK, ty, out.data_ptr(), _stream(device)))
     return out if out.shape[0] == N else out[:N]
@@ -345,7 +355,7 @@ def dropout_bwd(dy, N: int, p: float, seed: int, offset: int = 0, row_ids: Optio
     else:
         _rows(out, N, (d,), "out")
         _here(out, out_dtype or out.dtype, "out", device)
-        _apart(out, "out", dy)
+        _apart(out, "out", dy, row_ids)
     _check((_lib or load()).pspo_dropout_bwd(dy.data_ptr(), _ptr(row_ids), N, d, p, seed & _U64_MASK,
                                              offset & _U64_MASK, ty, _type(out, "out"), out.data_ptr(),
                                              _stream(device)))
@@ -381,11 +391,12 @@ def gated_ffn_workspace_bytes(N: int, d: int, f: int, backward: bool = False, pr
     return int(load().pspo_gated_ffn_workspace_bytes(_fits(N, "N"), _fits(d, "d"), _fits(f, "f"), flags))
 
 
-def _ffn_workspace(workspace, N, d, f, flags, like, device):
+def _ffn_workspace(workspace, N, d, f, flags, like, device, *others):
+    need = (_lib or load()).pspo_gated_ffn_workspace_bytes(N, d, f, flags)
     if workspace is None:
-        need = (_lib or load()).pspo_gated_ffn_workspace_bytes(N, d, f, flags)
         return torch.empty(max(need, 256), dtype=torch.uint8, device=like.device)
     _here(workspace, torch.uint8, "workspace", device)
+    _apart(workspace, "workspace", *others, used=need)
     return workspace
 
 
@@ -408,7 +419,7 @@ def gated_ffn(x, w_gate, w_up, w_down, N: int, act: str = "silu", keep: bool = F
         _here(out, torch.bfloat16, "out", device)
         _apart(out, "out", x, w_gate, w_up, w_down)
     pre = torch.empty((N, 2 * f), dtype=torch.float32, device=x.device) if keep else None
-    workspace = _ffn_workspace(workspace, N, d, f, 0, x, device)
+    workspace = _ffn_workspace(workspace, N, d, f, 0, x, device, x, w_gate, w_up, w_down, out)
     _check((_lib or load()).pspo_gated_ffn_fwd(
         x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), N, d, f, kind, out.data_ptr(), _ptr(pre),
         workspace.data_ptr(), workspace.numel(), _stream(device)))
@@ -450,7 +461,7 @@ def gated_ffn_bwd(dy, x, w_gate, w_up, w_down, N: int, act: str = "silu", preact
     flags = (FFN_DW_F32 if dw[0].dtype == torch.float32 else 0) | (pspo.PSPO_ACCUMULATE_DW if accumulate else 0)
     dx = torch.empty((N, d), dtype=torch.bfloat16, device=x.device)
     need = FFN_BACKWARD | (FFN_PREACT if preact is not None else 0)
-    workspace = _ffn_workspace(workspace, N, d, f, need, x, device)
+    workspace = _ffn_workspace(workspace, N, d, f, need, x, device, dy, x, w_gate, w_up, w_down, preact, *dw)
     _check((_lib or load()).pspo_gated_ffn_bwd(
         dy.data_ptr(), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), _ptr(preact), N, d, f,
         kind, flags, dx.data_ptr(), dw[0].data_ptr(), dw[1].data_ptr(), dw[2].data_ptr(), workspace.data_ptr(),
