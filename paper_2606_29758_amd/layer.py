@@ -102,6 +102,8 @@ def _rows(t: torch.Tensor, N: int, shape, name: str) -> None:
 
 
 def _exact(t: torch.Tensor, shape, name: str) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
@@ -374,6 +376,8 @@ def _act(act: str) -> int:
 
 def _ffn_weights(w_gate, w_up, w_down):
     device = torch.cuda.current_device()
+    if not isinstance(w_gate, torch.Tensor):
+        raise TypeError("w_gate must be a torch.Tensor")
     if w_gate.dim() != 2:
         raise ValueError("w_gate must be [f, d]")
     f, d = w_gate.shape

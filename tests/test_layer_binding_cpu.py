@@ -159,3 +159,15 @@ def test_gated_ffn_workspace_stands_apart(name, device):
         with pytest.raises(ValueError, match="overlaps"):
             layer.gated_ffn_bwd(at("dy", BF, N, d), x, *ws, N, preact=at("preact", F4, N, 2 * f), dw=dw,
                                 workspace=m.as_subclass(Here))
+
+
+def test_arguments_that_are_no_tensors_are_named(device):
+    x, w, wd = _new(BF, 4, 8), _new(BF, 16, 8), _new(BF, 8, 16)
+    for args, name in (((x, None, w, wd), "w_gate"), ((x, w, None, wd), "w_up"), ((x, w, w, [1.0]), "w_down"),
+                       ((None, w, w, wd), "x")):
+        with pytest.raises(TypeError, match=f"{name} must be a torch.Tensor"):
+            layer.gated_ffn(*args, 4)
+        with pytest.raises(TypeError, match=f"{name} must be a torch.Tensor"):
+            layer.gated_ffn_bwd(x, *args, 4)
+    with pytest.raises(TypeError, match="out must be a torch.Tensor"):
+        layer.dropout_add(x, 4, 0.1, 1, out=[0.0])
