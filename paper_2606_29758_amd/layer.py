@@ -241,6 +241,8 @@ def qk_norm_rope(q, k, q_weight, k_weight, inv_freq, N: int, positions=None, seq
     outs = []
     for name, x, o in (("q_out", q, q_out), ("k_out", k, k_out)):
         if x is None:
+            if o is not None:
+                raise ValueError(f"{name} is given without its input")
             outs.append(None)
             continue
         if o is None:

@@ -171,3 +171,9 @@ def test_arguments_that_are_no_tensors_are_named(device):
             layer.gated_ffn_bwd(x, *args, 4)
     with pytest.raises(TypeError, match="out must be a torch.Tensor"):
         layer.dropout_add(x, 4, 0.1, 1, out=[0.0])
+
+
+def test_a_key_output_without_keys_is_refused(device):
+    q = _new(BF, 4, 2, 16)
+    with pytest.raises(ValueError, match="k_out"):
+        layer.qk_norm_rope(q, None, None, None, None, 4, k_out=_new(BF, 4, 1, 16))
