@@ -173,12 +173,13 @@ struct RowSide {
   // asm, which has no output register: beside the builtin the compiler waits for every
   // load in flight before each transpose read.  It knows nothing of these loads:
   // row_barrier waits for them, and settle() keeps the wait states that a vector write
-  // of a scalar register needs before a load reads it.
+  // of a scalar register needs before a load reads it.  The LDS place goes in as an operand
+  // in m0, so that the compiler knows that it is written.
   template <int Q>
   __device__ __forceinline__ void load(const Stage& st, uint32_t lds, int wave) const {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                  :
-                 : "s"(lds + (Q * 4 + wave) * 1024), "v"(voff[Q] + st.add), "s"(st.rsrc), "s"(st.soff)
+                 : "{m0}"(lds + (Q * 4 + wave) * 1024), "v"(voff[Q] + st.add), "s"(st.rsrc), "s"(st.soff)
                  : "memory");
   }
   // Read R of half stage `Half` into f (K-outer: two reads make one block).
