@@ -148,7 +148,8 @@ def _fits(n: int, name: str) -> int:
 def _count(N: int) -> int:
     if N < 0:
         raise ValueError("N must be >= 0")
-    return _fits(int(N), "N")
+    N = int(N)
+    return N if N <= _MOST else _fits(N, "N")
 
 
 # ---------------------------------------------------------------------------
@@ -168,7 +169,8 @@ def _heads(t: torch.Tensor, N: int, name: str, device: int, like: Optional[torch
     if like is not None and t.dtype != like.dtype:
         raise TypeError(f"{name} must have dtype {like.dtype}, got {t.dtype}")
     _, H, D = t.shape
-    _fits(max(H, D), f"heads and head_dim of {name}")
+    if H > _MOST or D > _MOST:
+        _fits(max(H, D), f"heads and head_dim of {name}")
     if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
         raise ValueError(f"the heads of {name} must be contiguous within a row")
     return t
@@ -200,7 +202,9 @@ def _qk_common(q, k, q_weight, k_weight, inv_freq, N, positions, seq_id, cu_seql
         _here(inv_freq, torch.float32, "inv_freq", device)
         if inv_freq.dim() != 1:
             raise ValueError("inv_freq must be [rot_dim / 2]")
-        rot = _fits(2 * inv_freq.shape[0], "rot_dim")
+        rot = 2 * inv_freq.shape[0]
+        if rot > _MOST:
+            _fits(rot, "rot_dim")
         if positions is not None:
             _ints(positions, N, "positions", device)
             seq_id = cu_seqlens = first_pos = None
@@ -383,7 +387,8 @@ def _ffn_weights(w_gate, w_up, w_down):
     if w_gate.dim() != 2:
         raise ValueError("w_gate must be [f, d]")
     f, d = w_gate.shape
-    _fits(max(d, f), "d and f")
+    if d > _MOST or f > _MOST:
+        _fits(max(d, f), "d and f")
     _exact(w_up, (f, d), "w_up")
     _exact(w_down, (d, f), "w_down")
     for name, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
