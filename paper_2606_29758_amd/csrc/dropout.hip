@@ -8,6 +8,7 @@
 #include <cmath>
 
 #include "pspo_layer.h"
+#include "token_plan.h"
 #include "vec8.h"
 
 namespace pspo {
@@ -85,30 +86,19 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs a) {
 
 template <class Tin, class Tout, bool kResidual>
 int launch(DropArgs a, hipStream_t stream) {
-  // rows shorter than a wave share one; long rows of few tokens are split over the grid's y
-  int lanes = 64;
-  while (lanes > 1 && lanes / 2 >= a.vecs) lanes /= 2;
-  const int rows_per = 256 / lanes;
-  const int64_t gx = ((int64_t)a.N + rows_per - 1) / rows_per;
+  const DropPlan p = drop_plan(a.N, a.vecs, Tin::kBytes * (kResidual ? 2 : 1) + Tout::kBytes);
   // a launch holds less than 2^32 threads along x
-  PSPO_REQUIRE(gx < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "dropout supports at most 2^26 long rows per call");
-  // one step of one row's lanes at least per part, parts until some 2,048 work-groups are there
-  const int64_t steps = ((int64_t)a.vecs + lanes - 1) / lanes;
-  int64_t parts = gx >= 2048 ? 1 : (2048 + gx - 1) / gx;
-  if (parts > steps) parts = steps;
-  a.per_part = (int32_t)((steps + parts - 1) / parts * lanes);
-  parts = ((int64_t)a.vecs + a.per_part - 1) / a.per_part;
-  const dim3 grid((uint32_t)gx, (uint32_t)parts);
-  // past the caches: 113,926 x 3584 with the residual (2.45 GB) 451 -> 418 us
-  const int64_t bytes = (int64_t)a.N * a.vecs * 8 * (Tin::kBytes * (kResidual ? 2 : 1) + Tout::kBytes);
-  if (bytes >= kPastBytes && lanes == 64) {
+  PSPO_REQUIRE(p.gx < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "dropout supports at most 2^26 long rows per call");
+  a.per_part = p.per_part;
+  const dim3 grid((uint32_t)p.gx, (uint32_t)p.parts);
+  if (p.past) {
     hipLaunchKernelGGL((dropout_kernel<Tin, Tout, kResidual, 64, true>), grid, dim3(256), 0, stream, a);
     PSPO_LAUNCHED("dropout_kernel", stream);
     return PSPO_OK;
   }
 #define PSPO_DROP(L) \
   hipLaunchKernelGGL((dropout_kernel<Tin, Tout, kResidual, L, false>), grid, dim3(256), 0, stream, a)
-  switch (lanes) {
+  switch (p.lanes) {
     case 64: PSPO_DROP(64); break;
     case 32: PSPO_DROP(32); break;
     case 16: PSPO_DROP(16); break;

@@ -11,13 +11,14 @@
 // a float32 product pos * inv_freq is off by 0.004 rad at position 65,536) and
 // serve all of its heads, 64 / L heads at once.
 #include "pspo_layer.h"
+#include "token_plan.h"
 #include "vec8.h"
 
 namespace pspo {
 namespace {
 
 constexpr int kMaxDim = 512;
-constexpr int kWaves = 4;
+constexpr int kWaves = kQkWaves;
 
 struct QkArgs {
   const unsigned char *q, *k;        // inputs
@@ -306,27 +307,6 @@ __global__ __launch_bounds__(1024) void qk_dweight_kernel(const float* partials,
   }
 }
 
-// Work-groups of the backward and side: four to a CU keep some 16 waves with their
-// loads in flight.
-constexpr int kBwdGroups = 1024;
-
-int bwd_groups(int32_t N) {
-  const int64_t g = ((int64_t)N + kWaves - 1) / kWaves;
-  return (int)(g < kBwdGroups ? g : kBwdGroups);
-}
-
-int lanes_of(int D) {
-  int L = 1;
-  while (L * 8 < D) L <<= 1;
-  return L;
-}
-
-// The forward stores past the caches, the backward loads and stores (28,481 tokens of 32 heads of
-// 128: 89 -> 73 us, 171 -> 162 us, before the later steps; the forward's loads too 84).
-bool past(const QkArgs& a, int bytes, int times) {
-  return (int64_t)a.N * (a.Hq + a.Hk) * a.D * bytes * times >= kPastBytes;
-}
-
 template <class T, bool kPast>
 void launch_fwd(const QkArgs& a, int L, dim3 grid, hipStream_t stream) {
 #define PSPO_QK(W) \
@@ -343,14 +323,14 @@ void launch_bwd(const QkArgs& a, int L, dim3 grid, hipStream_t stream) {
 }
 template <class T>
 void launch(const QkArgs& a, int L, dim3 grid, bool backward, hipStream_t stream) {
-  const bool p = past(a, T::kBytes, backward ? 3 : 2);
+  const bool p = qk_past(a.N, a.Hq + a.Hk, a.D, T::kBytes, backward);
   if (backward) p ? launch_bwd<T, true>(a, L, grid, stream) : launch_bwd<T, false>(a, L, grid, stream);
   else p ? launch_fwd<T, true>(a, L, grid, stream) : launch_fwd<T, false>(a, L, grid, stream);
 }
 
 bool head_dim_fits(int32_t D) { return D >= 8 && D % 8 == 0 && D <= kMaxDim; }
 // A launch holds less than 2^32 threads along x.
-bool tokens_fit(int32_t N) { return ((int64_t)N + kWaves - 1) / kWaves < (int64_t(1) << 24); }
+bool tokens_fit(int32_t N) { return token_groups(N) < (int64_t(1) << 24); }
 
 // Checks shared by both directions; fills the common arguments.
 int check(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const void* qw, const void* kw,
@@ -437,16 +417,10 @@ int pspo_qk_norm_rope_fwd(const void* q, const void* k, int64_t q_stride, int64_
   if (int rc = require_gfx950()) return rc;
   a.q_out = static_cast<unsigned char*>(q_out);
   a.k_out = static_cast<unsigned char*>(k_out);
-  const int L = lanes_of(head_dim), heads = 64 / L;
-  const int passes = (heads_q + heads - 1) / heads + (heads_k + heads - 1) / heads;
-  const int64_t gx = ((int64_t)N + kWaves - 1) / kWaves;
-  // few tokens: a token's heads over several waves, each with its own angles, until
-  // some 2,048 work-groups are there
-  int parts = (int)(gx >= 2048 ? 1 : (2048 + gx - 1) / gx);
-  if (parts > passes) parts = passes;
-  a.per_part = (passes + parts - 1) / parts;
-  parts = (passes + a.per_part - 1) / a.per_part;
-  const dim3 grid((uint32_t)gx, (uint32_t)parts);
+  const int L = lanes_of(head_dim);
+  const QkForward p = qk_forward(N, heads_q, heads_k, head_dim);
+  a.per_part = p.per_part;
+  const dim3 grid((uint32_t)p.gx, (uint32_t)p.parts);
   if (type == PSPO_TYPE_F32) launch<F32>(a, L, grid, false, stream);
   else launch<Bf16>(a, L, grid, false, stream);
   PSPO_LAUNCHED("qk_fwd_kernel", stream);

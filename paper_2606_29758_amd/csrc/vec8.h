@@ -96,8 +96,4 @@ __device__ __forceinline__ void store8(unsigned char* p, int64_t i, const Vec8& 
   }
 }
 
-// Calls that move this much go past the caches, which would not hold their outputs until the
-// next call reads them; smaller ones leave them there.
-constexpr int64_t kPastBytes = int64_t(160) << 20;
-
 }  // namespace pspo
