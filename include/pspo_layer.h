@@ -16,6 +16,10 @@
  * tensors and leaves the rows behind them as they were.  N = 0 is valid; the
  * gradients of weights are then zero.  Outputs and workspaces must not alias
  * inputs or each other.
+ *
+ * Every result is deterministic: the same arguments give the same bits.  A
+ * token's head norms and dropout do not depend on the other tokens of the call;
+ * its feed-forward block does in rounding (see pspo_gated_ffn_fwd).
  */
 #ifndef PSPO_LAYER_H_
 #define PSPO_LAYER_H_
@@ -139,6 +143,9 @@ size_t pspo_gated_ffn_workspace_bytes(int32_t N, int32_t d, int32_t f, uint32_t 
  * The gated feed-forward block: for every token x (a row of d entries)
  *   g = Wg x,  u = Wu x,  h = act(g) * u,  y = Wd h.
  * Sums in float32; h is rounded to bf16 (the operand of the last product), y once.
+ * The order of a token's sums follows from N and from its place among the rows (tiles, K
+ * parts), so y of the same token may differ in rounding between calls of different N: passes
+ * whose ratio is taken should run on the same rows.
  *
  *  x             device, bf16 bits [N, d] row-major, 16-byte aligned.
  *  w_gate, w_up  device, bf16 bits [f, d] row-major.

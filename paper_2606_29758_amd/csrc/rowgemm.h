@@ -10,8 +10,8 @@
 //
 // Tile: a 256-thread work-group (2 x 2 wave64s) owns (32 BM) x (32 BN) entries of
 // C, each wave BM x BN blocks of v_mfma_f32_16x16x32_bf16 in the accumulator
-// registers.  K advances in stages of 64 through two LDS buffers filled by
-// buffer loads that write LDS directly; the buffer descriptor's range check
+// registers.  K advances in stages of 64 through a ring of two or four LDS buffers
+// filled by buffer loads that write LDS directly; the buffer descriptor's range check
 // turns rows and K past the operand's end into zeros, so no size need be a
 // multiple of the tile.
 //  * K-inner stages hold rows of 64 K entries (128 bytes): row r keeps its
@@ -25,7 +25,7 @@
 // Schedule: while the MFMAs of one half stage (32 K) run on one set of operand
 // registers the other set is read, at most one LDS read or load after each MFMA;
 // one barrier per stage, in its middle, behind which the stage's buffer is free
-// for the loads of the stage after next.
+// for the loads of the stage that takes its place in the ring (two or four on).
 #pragma once
 
 #include "gemm.h"
@@ -202,9 +202,6 @@ struct RowSide {
   }
 };
 
-// Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, slab); a wave
-// has its own part of the LDS; slab = part * (tiles of the launch) + tile.  Lane l's accumulator [i][j][r] is
-// C(tm 32 BM + (wm BM + i) 16 + (l / 16) 4 + r, tn 32 BN + (wn BN + j) 16 + l % 16).
 // Five wait states between whatever wrote the descriptors and the loads that read them.
 template <class SA, class SB>
 __device__ __forceinline__ void settle(SA& a, SB& b) {
@@ -222,6 +219,9 @@ template <int BM, int BN, int kRing>
 constexpr int kRowLds = kRing * (32 * BM + 32 * BN) * kRowK * 2;
 
 // One tile of a product: work-group `bid` of the launch's tiles, K part `part`.
+// Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, slab); a wave has its own part
+// of the LDS; slab = part * (tiles of the launch) + tile.  Lane l's accumulator [i][j][r] is
+// C(tm 32 BM + (wm BM + i) 16 + (l / 16) 4 + r, tn 32 BN + (wn BN + j) 16 + l % 16).
 template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
 __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi, int bid, int part,
                                               unsigned char* lds) {

@@ -416,7 +416,8 @@ def gated_ffn(x, w_gate, w_up, w_down, N: int, act: str = "silu", keep: bool = F
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T of the first N rows of x [>=N, d], all bf16.
 
     w_gate, w_up: [f, d]; w_down: [d, f]; act: "silu" or "gelu_tanh".  Returns y ([N, d]) and, with
-    keep, the float32 pre-activations [N, 2 f] that gated_ffn_bwd takes (else preact is None).
+    keep, the float32 pre-activations [N, 2 f] that gated_ffn_bwd takes (else preact is None).  The
+    same call gives the same bits; a token's y may differ in rounding between calls of different N.
     """
     N = _count(N)
     kind = _act(act)
