@@ -46,13 +46,14 @@ extern "C" {
  *         pos_n * inv_freq[i], i < rot_dim / 2:
  *         (a, b) -> (a cos - b sin, a sin + b cos).
  * The angle is formed in float64 (positions of any size), everything else in
- * float32, with one rounding to the output's type.
+ * float32, with one rounding to the output's type.  (A head whose sum of
+ * squares passes float32, entries of 1e18 and more, is normed to zeros.)
  *
  *  q, k          device [N rows]: token n's heads at q + n * q_stride, heads
  *                contiguous ([heads, D]); strides in elements, >= heads * D, so q
  *                and k may be parts of a fused projection's rows.  16-byte
  *                aligned rows.  heads_k = 0 (k NULL) is valid, heads_q >= 1.
- *  q_weight,     device [D] of the same type, or NULL (all ones).
+ *  q_weight,     device [D] of the same type, 16-byte aligned, or NULL (all ones).
  *  k_weight
  *  inv_freq      device, float32 [rot_dim / 2] (NULL iff rot_dim = 0).
  *  positions     device, int32 [N], or NULL: then

@@ -48,3 +48,25 @@ def test_an_empty_backward_without_a_workspace():
                                     *(t.data_ptr() for t in dw), None, 0, torch.cuda.current_stream().cuda_stream)
         assert rc == 0, lib.pspo_last_error()
         assert all((t == want).all() for t in dw)
+
+
+@pytest.mark.parametrize("dtype", [BF, F4])
+def test_head_norms_at_the_ends_of_float32(dtype):
+    """The largest entries whose squares still add up, the first that do not (zeros, as documented), and tiny ones
+    (the epsilon alone); the other heads of the token are what they were."""
+    N, H, D = 3, 4, 64
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(N, H, D, device="cuda", generator=g).to(dtype)
+    x[0, 1], x[1, 2], x[2, 3] = 2.0 ** 60, 2.0 ** 70, 2.0 ** -100
+    pos, inv = torch.arange(N, dtype=torch.int32, device="cuda"), torch.ones(16, device="cuda")
+    d = torch.ones_like(x)
+    y = layer.qk_norm_rope(x, None, None, None, inv, N, positions=pos)["q"]
+    b = layer.qk_norm_rope_bwd(d, None, x, None, None, None, inv, N, positions=pos)["dq"]
+    z = torch.ones_like(x)
+    ref = layer.qk_norm_rope(z, None, None, None, inv, N, positions=pos)["q"]
+    # 2^60 and 1 differ by the epsilon in 1 + eps: 5e-7; then one rounding each
+    step = (2.0 ** -8 if dtype == BF else 2.0 ** -24) * 2 + 1e-6
+    assert ((y[0, 1] - ref[0, 1]).abs() <= step * 1.5).all()
+    assert (y[1, 2] == 0).all() and (b[1, 2] == 0).all()
+    assert (y[2, 3].abs() <= 2.0 ** -89).all() and torch.isfinite(b[2, 3]).all()   # 2^-100 sqrt(2) / sqrt(eps) < 2^-89
+    assert torch.isfinite(y).all() and torch.isfinite(b).all()
