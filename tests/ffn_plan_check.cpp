@@ -71,7 +71,7 @@ int main(int argc, char** argv) {
     for (const auto& w : widths) {
       for (int64_t N = 0; N < 1500; ++N)
         if (check(N, w[0], w[1])) return 1;
-      for (int64_t N = 1500; N < 20000; N += 3)
+      for (int64_t N = 1501; N < 20000; N += 3)
         if (check(N, w[0], w[1])) return 1;
       for (int64_t N = 20000; N < 400000; N += 117)
         if (check(N, w[0], w[1])) return 1;

@@ -24,9 +24,9 @@ QK_PATHS = [
     (9001, 280, 70, 16, 16, True, _B), (9001, 200, 100, 16, 16, False, _F),
     (9001, 140, 30, 32, 32, False, _B), (9001, 140, 50, 24, 16, False, _F),
     (9001, 70, 20, 56, 48, False, _B), (9001, 35, 9, 64, 64, False, _F),
-    (28481, 28, 4, 128, 128, False, _B), (9001, 20, 4, 128, 128, False, _F),
+    (28481, 28, 4, 128, 128, False, _B), (9001, 21, 4, 128, 128, False, _F),
     (9001, 20, 6, 200, 64, True, _B), (9001, 9, 2, 256, 256, False, _F),
-    (9001, 9, 2, 512, 128, False, _B), (9001, 4, 2, 512, 512, True, _F),
+    (9001, 9, 2, 512, 128, False, _B), (9001, 5, 2, 512, 512, True, _F),
 ]
 
 # (N, d, type in, type out, residual) of dropout calls past the caches.

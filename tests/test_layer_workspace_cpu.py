@@ -14,7 +14,7 @@ WIDTHS = [(3584, 14336), (1536, 6144), (1000, 4104), (64, 72), (8, 8), (8, 4096)
 
 def _counts():
     """Every count up to 300 tokens, then steps that meet every remainder of a tile, then around powers of two."""
-    return sorted({*range(300), *range(300, 9000, 7), *range(9000, 70000, 131),
+    return sorted({*range(301), *range(301, 9000, 7), *range(9000, 70000, 131),
                    *(2 ** b + e for b in range(10, 20) for e in (-1, 1, 129))})
 
 
