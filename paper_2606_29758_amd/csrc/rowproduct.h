@@ -1,0 +1,237 @@
+// Launches of the row-major products (rowgemm.h, skinny.h): the epilogue that stores, K parts and
+// their joins, one product as its plan (row_plan.h) covers it.  The names are internal to each source
+// file that includes this.
+#pragma once
+
+#include "row_plan.h"
+#include "skinny.h"
+#include "vec8.h"
+
+namespace pspo {
+namespace {
+
+// ---- epilogues -----------------------------------------------------------------
+// What becomes of eight entries (m .. m + 7, n) of a product; the same for a tile's accumulators
+// (Epi::apply) and for the joined sums of its K parts (row_join_kernel).
+struct Nothing {};
+
+__device__ __forceinline__ void put_f32(float* to, const f32x4* v) {
+  reinterpret_cast<f32x4*>(to)[0] = v[0];
+  reinterpret_cast<f32x4*>(to)[1] = v[1];
+}
+__device__ __forceinline__ void put_bf16(uint16_t* to, const float* v) {
+  u32x4 p;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+  *reinterpret_cast<u32x4*>(to) = p;
+}
+
+// C(m, n) -> out[n * ld + m], bf16 or float32 (or added to it); rows n >= split belong to a
+// second matrix.
+struct EpiStore {
+  static constexpr bool kPair = false;
+  void *out, *out2;
+  int64_t ld;
+  int M, N, split, f32, add;
+  using Fetched = Nothing;
+  __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return {}; }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, Nothing) const {
+    if (n >= N || m >= M) return;   // M % 8 == 0
+    void* base = n < split ? out : out2;
+    const int64_t at = (n < split ? n : n - split) * ld + m;
+    if (f32) {
+      float* to = static_cast<float*>(base) + at;
+      f32x4 s[2] = {v[0], v[1]};
+      if (add) {
+        s[0] += reinterpret_cast<const f32x4*>(to)[0];
+        s[1] += reinterpret_cast<const f32x4*>(to)[1];
+      }
+      put_f32(to, s);
+    } else {
+      put_bf16(static_cast<uint16_t*>(base) + at, reinterpret_cast<const float*>(v));
+    }
+  }
+};
+
+// A K part's whole tile in float32 to slab number `slab`: the 16 x 16 blocks one after
+// another (those of a column of blocks together), each as its lanes hold it, so that a store
+// writes 1 KB in one piece.  slab_piece says where four entries lie.
+struct Slab {
+  float* base;
+  int N;
+};
+template <int BM, int BN>
+__device__ __forceinline__ void put_slab(const f32x4 (&acc)[BM][BN], int tn, int wm, int wn, int lane, int slab,
+                                         const Slab& s) {
+  float* to = s.base + (int64_t)slab * (1024 * BM * BN) + (wn * BN * 2 * BM + wm * BM) * 256 + lane * 4;
+  repeat<BN>([&](auto jc) {
+    constexpr int j = decltype(jc)::value;
+    if (((tn * 2 + wn) * BN + j) * 16 >= s.N) return;   // nobody joins columns that do not exist
+#pragma unroll
+    for (int i = 0; i < BM; ++i) {
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
+      *reinterpret_cast<f32x4*>(to + (j * 2 * BM + i) * 256) = v;
+    }
+  });
+}
+// Offset of entries (m .. m + 3, n) of a tile of `tile` rows, m % 4 == 0.
+__device__ __forceinline__ int slab_piece(int tile, int m, int n) {
+  return ((n >> 4) * (tile >> 4) + (m >> 4)) * 256 + (((m >> 2) & 3) * 16 + (n & 15)) * 4;
+}
+
+// The epilogue of a launch: slabs where the tiles are parts, else `op`.
+template <class Op>
+struct Epi {
+  Op op;
+  Slab slab;
+  template <int BM, int BN>
+  __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
+                                        unsigned char* lds, int index) const {
+    if (slab.base != nullptr) put_slab(acc, tn, wm, wn, lane, index, slab);
+    else row_pieces<BM, BN, Op::kPair>(acc, tm, tn, wm, wn, lane, lds, op);
+  }
+};
+
+// ---- parts of K joined ------------------------------------------------------------
+// The slabs of a tile's parts added in order and given to the product's epilogue.
+struct JoinShape {
+  const float* slab;
+  RowShape g;
+  int tile, tile_n;
+};
+template <class Op>
+__device__ __forceinline__ void join_tile(const JoinShape& a, const Op& op, int index, int block) {
+  int tm, tn;
+  row_tile_at(a.g, a.g.tile0 + index, tm, tn);
+  // a wave takes 8 columns x 64 entries: whole lines of the output, 128-byte pieces of the slabs
+  const int width = Op::kPair ? a.tile / 2 : a.tile;
+  const int w = block * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int col = w / (width / 64) * 8 + lane / 8, m0 = w % (width / 64) * 64 + lane % 8 * 8;
+  if (col >= a.tile_n) return;
+  const int64_t n = (int64_t)tn * a.tile_n + col, m = (int64_t)tm * width + m0;
+  if (n >= op.N) return;   // its slab columns are not written
+  // gate and up in turn, 16 rows each; the next four entries of a piece lie 64 floats on
+  const int row = Op::kPair ? m0 / 16 * 32 + m0 % 16 : m0;
+  const int64_t size = (int64_t)a.tile * a.tile_n;
+  const float* from = a.slab + index * size;
+  const int p0 = slab_piece(a.tile, row, col), p1 = Op::kPair ? slab_piece(a.tile, row + 16, col) : 0;
+  const typename Op::Fetched x = op.fetch(n, m);
+  f32x4 v[Op::kPair ? 4 : 2] = {};
+  // four parts' loads out before the first is added; the sums in the parts' order
+  const int64_t next = a.g.count * size;
+  constexpr int kV = Op::kPair ? 4 : 2;
+  for (int p = 0; p < a.g.parts; p += 4) {
+    f32x4 t[4][kV];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (p + q < a.g.parts) {
+        const float* at = from + (p + q) * next;
+        t[q][0] = *reinterpret_cast<const f32x4*>(at + p0);
+        t[q][1] = *reinterpret_cast<const f32x4*>(at + p0 + 64);
+        if constexpr (Op::kPair) {
+          t[q][2] = *reinterpret_cast<const f32x4*>(at + p1);
+          t[q][3] = *reinterpret_cast<const f32x4*>(at + p1 + 64);
+        }
+      }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (p + q < a.g.parts)
+#pragma unroll
+        for (int k = 0; k < kV; ++k) v[k] += t[q][k];
+  }
+  op.piece(n, m, v, x);
+}
+// Work-groups for a tile's join: a wave for 8 columns x 64 entries.
+inline int join_blocks(int width, int tile_n) { return (width / 64 * (tile_n / 8) + 3) / 4; }
+
+template <class Op>
+__global__ __launch_bounds__(256) void row_join_kernel(JoinShape a, Op op) {
+  join_tile(a, op, blockIdx.x, blockIdx.y);
+}
+template <class Op>
+int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
+  hipLaunchKernelGGL((row_join_kernel<Op>),
+                     dim3((uint32_t)g.count, (uint32_t)join_blocks(Op::kPair ? tile / 2 : tile, tile_n)), dim3(256), 0,
+                     stream, JoinShape{slab, g, tile, tile_n}, op);
+  PSPO_LAUNCHED("row_join_kernel", stream);
+  return PSPO_OK;
+}
+
+template <bool kOuterA, bool kOuterB, class Op>
+int launch(const RowShape& g, const Plan& p, const Epi<Op>& epi, const char* name, hipStream_t stream) {
+  const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
+  const bool deep = deep_ring((int64_t)g.count * g.parts);
+#define PSPO_ROW(BM, BN, RING)                                                                                    \
+  hipLaunchKernelGGL((row_gemm_kernel<BM, BN, RING, kOuterA, kOuterB, Op::kPair, Epi<Op>>), grid, dim3(256), 0, \
+                     stream, g, epi)
+  if (p.tile == 256) {
+    PSPO_ROW(8, 8, 2);
+  } else if (p.tile_n == 128) {
+    if (deep) PSPO_ROW(4, 4, kDeep);
+    else PSPO_ROW(4, 4, 2);
+  } else if constexpr (!kOuterA) {
+    if (deep) PSPO_ROW(4, 2, kDeep);
+    else PSPO_ROW(4, 2, 2);
+  }
+#undef PSPO_ROW
+  PSPO_LAUNCHED(name, stream);
+  return PSPO_OK;
+}
+
+// One product with its epilogue, covered as `p` says: the whole tiles, then the rest in parts and their join.
+template <bool kOuterA, bool kOuterB, class Op>
+int product(RowShape g, const Plan& p, int64_t N, const Op& op, float* slab, const char* name, hipStream_t stream) {
+  const int64_t total = (int64_t)p.tiles_m * p.tiles_n;
+  PSPO_REQUIRE(total < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
+  g.tiles_m = p.tiles_m;
+  g.tiles_n = p.tiles_n;
+  g.tile0 = 0;
+  g.count = p.whole;
+  g.parts = 1;
+  if (g.count > 0)
+    if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {nullptr, 0}}, name, stream)) return rc;
+  g.tile0 = p.whole;
+  g.count = (int)(total - p.whole);
+  if (g.count == 0) return PSPO_OK;
+  g.parts = p.parts;
+  if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {slab, (int)N}}, name, stream)) return rc;
+  return join_parts(op, g, p.tile, p.tile_n, slab, stream);
+}
+
+RowShape shape(const uint16_t* a, const uint16_t* a2, int64_t lda, int rows_a, const uint16_t* b, int64_t ldb, int rows_b,
+               int K, int segs = 1, int64_t seg_b = 0) {
+  RowShape g{};
+  g.a = RowOperand{{a, a2}, lda, rows_a, 0};
+  g.b = RowOperand{{b, b}, ldb, rows_b, seg_b};
+  g.K = K;
+  g.segs = segs;
+  return g;
+}
+
+// ---- few tokens -----------------------------------------------------------------------
+// Waves of a work-group: enough that the chip holds some 4,096, at most one for each
+// step of K and 64 KB of sums.
+template <int kMats, class Epi>
+int skinny(const SkinnyArgs& a, const Epi& epi, const char* name, hipStream_t stream) {
+  const int groups = (a.M + 15) / 16, blocks = (a.N + 15) / 16, steps = (a.K + kSkinnyK - 1) / kSkinnyK;
+  int waves = 1;
+  while (waves < (blocks > 1 ? 8 : 16) && waves * 2 <= steps && (int64_t)groups * waves < 4096 &&
+         waves * 2 * kMats * blocks * 1024 <= 65536)
+    waves *= 2;
+  const size_t lds = (size_t)waves * kMats * blocks * 1024;
+#define PSPO_SKINNY(NB, AHEAD)   hipLaunchKernelGGL((skinny_kernel<kMats, NB, AHEAD, Epi>), dim3(groups), dim3(64 * waves), lds, stream, a, epi)
+  switch (blocks) {
+    case 1: PSPO_SKINNY(1, 4); break;
+    case 2: PSPO_SKINNY(2, 2); break;
+    case 3: PSPO_SKINNY(3, 2); break;
+    default: PSPO_SKINNY(4, 1); break;
+  }
+#undef PSPO_SKINNY
+  PSPO_LAUNCHED(name, stream);
+  return PSPO_OK;
+}
+
+}  // namespace
+}  // namespace pspo
