@@ -1,0 +1,916 @@
+// Training objectives through the LM head: the policy loss with a reference penalty, the
+// preference loss on pairs, distillation from top logits; forward and gradient in one call.
+//
+// All three have the same shape.  With z_i = W h_i, s = 1 / temperature and p_i = softmax(s z_i),
+// the loss depends on row i through log p_i at a few ids (one, or a teacher's list), so its logit
+// gradient is G_i = a_i p_i with those entries replaced:
+//   log-prob l_i of one id o, delta_i = d loss / d l_i:  a_i = -s delta_i,
+//       G_io = s delta_i (1 - p_io) = -s delta_i expm1(l_i)  (no cancellation as p -> 1);
+//   divergence from q_i with weight c_i:  a_i = s c_i,  G_ij = s c_i (p_ij - q_ij).
+//
+// Schedule:
+//   1. gather: the rows that take part, copied (zeros for the others: a NaN there must not reach a
+//      sum over rows), and the logits at the ids as float32 dot products;
+//   2. product Z^T = W H^T; its epilogue writes exp(s (z - m_g)) in bf16, m_g the maximum over the
+//      group of 64 vocabulary entries, and (m_g, sum of the unrounded exponentials) of the group;
+//   3. finalize: a row's groups merged into log sum exp, then the objective's terms (the preference
+//      loss takes three small steps more: sequences, pairs, rows);
+//   4. convert, in place: G = a exp(s m_g - lse) * entry, and the entries at the ids;
+//   5. products dH = G W and dW = G^T H.
+// The matrix-core work is that of the formulas, 6 N d V, with no logit computed twice: the entries
+// cost 6 bytes each on their way (written, read and written again) against 2 d flops, 1.4 against 5
+// ns per 1000 entries at d = 3584.
+#include <cmath>
+
+#include "pspo_objective.h"
+#include "rowproduct.h"
+
+namespace pspo {
+namespace {
+
+constexpr int kGroup = 64;         // vocabulary entries of one (maximum, sum)
+constexpr int kFewGroup = 2048;    // ... where the logits are kept in float32
+constexpr int kMostIds = 64;
+
+// ---- lane exchanges within 8 lanes ------------------------------------------------
+__device__ __forceinline__ float lane_move(float x, int which) {
+  const int v = __float_as_int(x);
+  const int r = which == 0   ? __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true)     // lane ^ 1
+                : which == 1 ? __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true)     // lane ^ 2
+                             : __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);   // 7 - lane, of 8
+  return __int_as_float(r);
+}
+__device__ __forceinline__ float max_of_8_lanes(float x) {
+  x = fmaxf(x, lane_move(x, 0));
+  x = fmaxf(x, lane_move(x, 1));
+  return fmaxf(x, lane_move(x, 2));
+}
+__device__ __forceinline__ float sum_of_8_lanes(float x) {
+  x += lane_move(x, 0);
+  x += lane_move(x, 1);
+  return x + lane_move(x, 2);
+}
+
+// ---- forward product ---------------------------------------------------------------
+// Eight logits (vocabulary entries m .. m + 7 of row n); the 8 lanes of a group of 64 entries
+// hold it together, in a tile's epilogue and in a join alike.  The exponential's argument is formed
+// as (z - m) * t: as z t - m t in one fma it would carry the rounding of m t, 1e-6 of the sum.
+struct EpiSoftmax {
+  static constexpr bool kPair = false;
+  uint16_t* e;      // [N][ld]
+  f32x2* part;      // [N][ld / 64]: maximum, sum
+  int64_t ld;
+  int V, N;
+  float t;          // log2(e) / temperature
+  using Fetched = Nothing;
+  __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return {}; }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, Nothing) const {
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = m + k < V ? v[k / 4][k % 4] : -INFINITY;
+    float top = x[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
+    top = max_of_8_lanes(top);
+    const float from = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = __builtin_amdgcn_exp2f((x[k] - from) * t);
+      sum += x[k];
+    }
+    sum = sum_of_8_lanes(sum);
+    if (n >= N || m >= ld) return;
+    put_bf16(e + n * ld + m, x);
+    if (m % kGroup == 0) part[n * (ld / kGroup) + m / kGroup] = f32x2{top, sum};
+  }
+};
+
+// Few rows: the logits as they are.
+struct SkinnyLogits {
+  float* z;   // [N][ld]
+  int64_t ld;
+  __device__ __forceinline__ void operator()(int m, int n, const float (&s)[1]) const { z[n * ld + m] = s[0]; }
+};
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
+  return x;
+}
+template <class T>
+__device__ __forceinline__ T wave_sum(T x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+// Over the 256 threads of a work-group, in a fixed order; every thread gets the result.
+__device__ __forceinline__ float block_max(float x, float* sh) {
+  x = wave_max(x);
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = x;
+  __syncthreads();
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+template <class T>
+__device__ __forceinline__ T block_total(T x, T* sh) {
+  x = wave_sum(x);
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = x;
+  __syncthreads();
+  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+}
+
+// (Maximum, sum) of the groups of 2,048 logits of a row.  Grid (N, groups).
+__global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict__ z, int64_t ld, int V, float t,
+                                                         f32x2* __restrict__ part) {
+  __shared__ float sh[4];
+  const int v0 = blockIdx.y * kFewGroup + threadIdx.x * 8;
+  const float* row = z + (int64_t)blockIdx.x * ld;
+  float x[8], top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    x[k] = v0 + k < V ? row[v0 + k] : -INFINITY;
+    top = fmaxf(top, x[k]);
+  }
+  top = block_max(top, sh);
+  const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f((x[k] - from) * t);
+  sum = block_total(sum, sh);
+  if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{top, sum};
+}
+
+// ---- what a call's kernels share ------------------------------------------------------
+struct Rows {
+  int N, d, V, k;          // k ids a row
+  int64_t ld, groups;      // entries between softmax rows; groups of a row
+  double inv_t;
+  int32_t* use;            // 1: takes part, 0: left out, -1: left out for an invalid id
+  float* zs;               // [N][k] logits at the ids
+  f32x2* part;
+  double* lse;
+  float* a;                // factor of p_i
+  int32_t* ids;            // [N][k] places of the entries set apart (-1: none) and their values
+  float* g;
+  double* terms;           // [4][N] of the loss
+  int32_t* err;
+};
+
+__device__ __forceinline__ void raise(int32_t* err, int bit) {
+  if (err != nullptr) atomicOr(err, bit);
+}
+
+// ---- 1. gather -------------------------------------------------------------------------
+// A wave per row.  Op::use(i, lane, err): as Rows::use, the same in all lanes; Op::id(i, j): the
+// row's j-th id or -1.  Four ids' rows of W at a time beside the hidden row.
+template <class Op>
+__global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16_t* __restrict__ hidden,
+                                                     const uint16_t* __restrict__ w, uint16_t* __restrict__ copy) {
+  const int i = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+  if (i >= r.N) return;
+  const int use = op.use(i, lane, r);
+  if (lane == 0) r.use[i] = use;
+  const u32x4* from = reinterpret_cast<const u32x4*>(hidden + (int64_t)i * r.d);
+  u32x4* to = reinterpret_cast<u32x4*>(copy + (int64_t)i * r.d);
+  const int pieces = r.d / 8;
+  for (int c = lane; c < pieces; c += 64) {
+    u32x4 x = {0, 0, 0, 0};
+    if (use == 1) x = from[c];
+    to[c] = x;
+  }
+  if (use != 1) return;
+  constexpr int kAt = 4;
+  for (int j0 = 0; j0 < r.k; j0 += kAt) {
+    const u32x4* row[kAt];
+    bool on[kAt];
+    float sum[kAt] = {};
+#pragma unroll
+    for (int j = 0; j < kAt; ++j) {
+      const int id = j0 + j < r.k ? op.id(i, j0 + j, r) : -1;
+      on[j] = id >= 0;
+      row[j] = reinterpret_cast<const u32x4*>(w + (int64_t)(on[j] ? id : 0) * r.d);
+    }
+    for (int c = lane; c < pieces; c += 64) {
+      const u32x4 hv = from[c];
+#pragma unroll
+      for (int j = 0; j < kAt; ++j) {
+        if (!on[j]) continue;   // the same in all lanes
+        const u32x4 wv = row[j][c];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          sum[j] = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), sum[j]);
+          sum[j] = fmaf(__uint_as_float(hv[q] & 0xFFFF0000u), __uint_as_float(wv[q] & 0xFFFF0000u), sum[j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAt; ++j) {
+      sum[j] = wave_sum(sum[j]);
+      if (lane == 0 && j0 + j < r.k) r.zs[(int64_t)i * r.k + j0 + j] = sum[j];
+    }
+  }
+}
+
+// ---- 3. finalize -----------------------------------------------------------------------
+// A work-group per row: log sum exp of its groups, merged in a fixed order, then op.row, called
+// by the first wave.
+template <class Op>
+__global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
+  __shared__ float shf[4];
+  __shared__ double shd[4];
+  const int i = blockIdx.x;
+  const int use = r.use[i];
+  double lse = 0.0;
+  if (use == 1) {
+    const f32x2* part = r.part + (int64_t)i * r.groups;
+    const float t = (float)(r.inv_t * 1.4426950408889634);
+    float top = -INFINITY, sum = 0.f;
+    for (int g = threadIdx.x; g < r.groups; g += 256) {
+      const f32x2 p = part[g];
+      if (p.x > top) {
+        sum = sum * __builtin_amdgcn_exp2f((top - p.x) * t) + p.y;
+        top = p.x;
+      } else if (p.x != -INFINITY || p.y != 0.f) {   // (a group of no entries adds nothing; a NaN stays)
+        sum += p.y * __builtin_amdgcn_exp2f((p.x - top) * t);
+      }
+    }
+    const float all = block_max(top, shf);
+    const double total = block_total(top == -INFINITY && sum == 0.f
+                                         ? 0.0 : (double)sum * (double)__builtin_amdgcn_exp2f((top - all) * t), shd);
+    lse = (double)all * r.inv_t + log(total);
+  }
+  if (threadIdx.x >= 64) return;
+  if (threadIdx.x == 0) r.lse[i] = lse;
+  op.row(i, threadIdx.x, use, lse, r);
+}
+
+// Sums over the rows of up to four terms each ([4][n]), in a fixed order; one work-group.
+struct Sums {
+  double out[4];
+};
+__device__ __forceinline__ Sums sum_terms(const double* terms, int64_t n, int count, double* sh) {
+  Sums s{};
+  for (int q = 0; q < count; ++q) {
+    double x = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) x += terms[q * n + i];
+    s.out[q] = block_total(x, sh);
+  }
+  return s;
+}
+
+// ---- policy loss ---------------------------------------------------------------------------
+// One id a row, its use checked by the objectives of a target.
+__device__ __forceinline__ int target_use(int i, const int32_t* target, const float* weight, const Rows& r, int lane) {
+  if (weight != nullptr && weight[i] == 0.f) return 0;
+  const int o = target[i];
+  if (o >= 0 && o < r.V) return 1;
+  if (lane == 0) raise(r.err, PSPO_DEVERR_TARGET);
+  return -1;
+}
+
+struct Policy {
+  const int32_t* target;
+  const float *logp_old, *logp_ref, *weight;
+  const int32_t* seq_id;
+  const float* advantage;
+  int R;
+  float eps_low, eps_high, kl_coef, scale;
+  int kl;
+  float* logp_new;
+
+  __device__ __forceinline__ int use(int i, int lane, const Rows& r) const {
+    const int u = target_use(i, target, weight, r, lane);
+    if (u != 1) return u;
+    const int s = seq_id[i];
+    if (s >= 0 && s < R) return 1;
+    if (lane == 0) raise(r.err, PSPO_DEVERR_SEQ_ID);
+    return -1;
+  }
+  __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
+  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
+    if (lane != 0) return;
+    double gain = 0.0, div = 0.0, clipped = 0.0, delta = 0.0, l = 0.0;
+    if (use == 1) {
+      l = (double)r.zs[i] * r.inv_t - lse;
+      const double c = (double)weight[i] * (double)scale, A = advantage[seq_id[i]];
+      const double rho = exp(l - (double)logp_old[i]);
+      const double lo = 1.0 - (double)eps_low, hi = 1.0 + (double)eps_high;
+      const double in = rho < lo ? lo : (rho > hi ? hi : rho);   // (a NaN stays)
+      gain = c * (rho * A < in * A ? rho * A : in * A);
+      const bool pass = (A > 0.0 && rho <= hi) || (A < 0.0 && rho >= lo);
+      clipped = A != 0.0 && !pass ? 1.0 : 0.0;
+      delta = pass ? -c * rho * A : 0.0;
+      if (logp_ref != nullptr) {
+        const double u = l - (double)logp_ref[i];
+        div = c * (kl == PSPO_KL_K1 ? u : kl == PSPO_KL_K2 ? 0.5 * u * u : expm1(-u) + u);
+        if (kl_coef != 0.f) delta += (double)kl_coef * c * (kl == PSPO_KL_K1 ? 1.0 : kl == PSPO_KL_K2 ? u : -expm1(-u));
+      }
+      const double loss = kl_coef != 0.f ? (double)kl_coef * div - gain : -gain;
+      if (!(std::isfinite(lse) && std::isfinite((float)rho) && std::isfinite(loss) && std::isfinite((float)delta)))
+        raise(r.err, PSPO_DEVERR_NONFINITE);
+    }
+    const int64_t n = r.N;
+    r.terms[i] = gain;
+    r.terms[n + i] = div;
+    r.terms[2 * n + i] = clipped;
+    r.terms[3 * n + i] = use == 1 ? 1.0 : 0.0;
+    r.a[i] = (float)(-delta * r.inv_t);
+    r.ids[i] = use == 1 ? target[i] : -1;
+    r.g[i] = use == 1 ? (float)(-delta * r.inv_t * expm1(l)) : 0.f;
+    if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
+  }
+};
+
+__global__ __launch_bounds__(256) void policy_loss_kernel(const double* __restrict__ terms, int64_t n, float kl_coef,
+                                                          double* __restrict__ loss, double* __restrict__ stats) {
+  __shared__ double sh[4];
+  const Sums s = sum_terms(terms, n, 4, sh);
+  if (threadIdx.x != 0) return;
+  *loss = kl_coef != 0.f ? (double)kl_coef * s.out[1] - s.out[0] : -s.out[0];
+  if (stats != nullptr)
+    for (int q = 0; q < 4; ++q) stats[q] = s.out[q];
+}
+
+// ---- preference loss ------------------------------------------------------------------------
+struct Preference {
+  const int32_t* target;
+  const float *logp_ref, *weight;
+  float* logp_new;
+
+  __device__ __forceinline__ int use(int i, int lane, const Rows& r) const {
+    return target_use(i, target, weight, r, lane);
+  }
+  __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
+  // terms: the log-prob, the row's part of its sequence's log ratio, its weight
+  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
+    if (lane != 0) return;
+    double l = 0.0, part = 0.0, c = 0.0;
+    if (use == 1) {
+      l = (double)r.zs[i] * r.inv_t - lse;
+      c = weight != nullptr ? (double)weight[i] : 1.0;
+      part = c * (logp_ref != nullptr ? l - (double)logp_ref[i] : l);
+      if (!(std::isfinite(lse) && std::isfinite(part))) raise(r.err, PSPO_DEVERR_NONFINITE);
+    }
+    const int64_t n = r.N;
+    r.terms[i] = l;
+    r.terms[n + i] = part;
+    r.terms[2 * n + i] = c;
+    if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
+  }
+};
+
+struct Pairs {
+  const int32_t *cu, *chosen, *rejected;
+  int R, P, kind, average;
+  float beta, smoothing, scale;
+  double *ratio, *norm, *coef;   // [R]
+  double *pair, *pair_loss;      // [P]
+  float *seq_ratio, *margin;
+  int32_t* err;
+};
+
+// Sequence r's rows, clamped to [0, N].
+__device__ __forceinline__ bool sequence_rows(const Pairs& q, int r, int N, int& lo, int& hi) {
+  const int a = q.cu[r], b = q.cu[r + 1];
+  lo = min(max(a, 0), N);
+  hi = min(max(b, lo), N);
+  return a >= 0 && b >= a && b <= N;
+}
+
+// A work-group per sequence: its log ratio and the factor that its rows' terms enter it with.
+__global__ __launch_bounds__(256) void pref_sequences_kernel(Pairs q, int N, const double* __restrict__ terms) {
+  __shared__ double sh[4];
+  const int r = blockIdx.x;
+  int lo, hi;
+  const bool fine = sequence_rows(q, r, N, lo, hi);
+  if (!fine && threadIdx.x == 0) raise(q.err, PSPO_DEVERR_SEQ_ID);
+  double part = 0.0, c = 0.0;
+  for (int i = lo + threadIdx.x; i < hi; i += 256) {
+    part += terms[(int64_t)N + i];
+    c += terms[2 * (int64_t)N + i];
+  }
+  part = block_total(part, sh);
+  c = block_total(c, sh);
+  if (threadIdx.x != 0) return;
+  const double norm = q.average ? (c != 0.0 ? 1.0 / c : 0.0) : 1.0;
+  const double ratio = norm != 0.0 ? part * norm : 0.0;
+  q.norm[r] = norm;
+  q.ratio[r] = ratio;
+  if (q.seq_ratio != nullptr) q.seq_ratio[r] = (float)ratio;
+}
+
+// d loss / d u of each pair, and its part of the loss.
+__global__ __launch_bounds__(256) void pref_pairs_kernel(Pairs q) {
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= q.P) return;
+  const int a = q.chosen[p], b = q.rejected[p];
+  double loss = 0.0, du = 0.0, m = NAN;
+  if (a >= 0 && a < q.R && b >= 0 && b < q.R) {
+    const double u = q.ratio[a] - q.ratio[b], beta = q.beta, eps = q.smoothing;
+    m = beta * u;
+    if (q.kind == PSPO_PREF_SIGMOID) {
+      // -log s(x) = max(-x, 0) + log1p(exp(-|x|)), s(-x) = exp(-x) s(x)
+      const double e = exp(-fabs(m)), tail = log1p(e);
+      const double up = m > 0.0 ? tail : tail - m, down = m > 0.0 ? tail + m : tail;   // -log s(m), -log s(-m)
+      const double s = m > 0.0 ? 1.0 / (1.0 + e) : e / (1.0 + e), s_neg = m > 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e);
+      loss = eps != 0.0 ? (1.0 - eps) * up + eps * down : up;
+      du = beta * (eps * s - (1.0 - eps) * s_neg);
+    } else {
+      const double x = u - 0.5 / beta;
+      loss = x * x;
+      du = 2.0 * x;
+    }
+    if (!std::isfinite(loss)) raise(q.err, PSPO_DEVERR_NONFINITE);
+  } else {
+    raise(q.err, PSPO_DEVERR_SEQ_ID);
+  }
+  q.pair[p] = du * (double)q.scale;
+  q.pair_loss[p] = loss * (double)q.scale;
+  if (q.margin != nullptr) q.margin[p] = (float)m;
+}
+
+// A work-group per sequence: what its pairs give it, in the pairs' order within each thread's share.
+// The last one sums the loss.
+__global__ __launch_bounds__(256) void pref_coef_kernel(Pairs q, double* __restrict__ loss) {
+  __shared__ double sh[4];
+  const int r = blockIdx.x;
+  if (r == q.R) {
+    const Sums s = sum_terms(q.pair_loss, q.P, 1, sh);
+    if (threadIdx.x == 0) *loss = s.out[0];
+    return;
+  }
+  double c = 0.0;
+  for (int p = threadIdx.x; p < q.P; p += 256) {
+    const int a = q.chosen[p], b = q.rejected[p];
+    if ((a != r && b != r) || a < 0 || a >= q.R || b < 0 || b >= q.R) continue;
+    c += a == r ? (b == r ? 0.0 : q.pair[p]) : -q.pair[p];
+  }
+  c = block_total(c, sh);
+  if (threadIdx.x == 0) q.coef[r] = q.norm[r] != 0.0 ? c * q.norm[r] : 0.0;
+}
+
+// The row's factors, from its sequence's.
+__global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q, const int32_t* __restrict__ target) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= r.N) return;
+  int s = 0, e = q.R;   // the last sequence that starts at or before row i
+  while (s < e) {
+    const int mid = s + (e - s) / 2;
+    if (q.cu[mid + 1] > i) e = mid;
+    else s = mid + 1;
+  }
+  const bool in = s < q.R && q.cu[s] <= i;
+  const int64_t n = r.N;
+  const bool on = in && r.use[i] == 1;
+  const double l = r.terms[i], delta = on ? q.coef[s] * r.terms[2 * n + i] : 0.0;
+  if (on && !std::isfinite((float)delta)) raise(r.err, PSPO_DEVERR_NONFINITE);
+  r.a[i] = (float)(-delta * r.inv_t);
+  r.ids[i] = on ? target[i] : -1;
+  r.g[i] = on ? (float)(-delta * r.inv_t * expm1(l)) : 0.f;
+}
+
+// ---- distillation -----------------------------------------------------------------------------
+struct Distill {
+  const int32_t* topk_ids;
+  const float* topk;
+  const float* weight;
+  float scale;
+  float* kl;
+
+  // An entry: an id that is not negative with a teacher value above -inf (or NaN, which shows).
+  __device__ __forceinline__ bool entry(int64_t at) const {
+    return topk_ids[at] >= 0 && !(topk[at] == -INFINITY);
+  }
+  __device__ __forceinline__ int use(int i, int lane, const Rows& r) const {
+    if (weight != nullptr && weight[i] == 0.f) return 0;
+    const int64_t at = (int64_t)i * r.k + lane;
+    const bool on = lane < r.k && entry(at);
+    if (__any(on && topk_ids[at] >= r.V)) {
+      if (lane == 0) raise(r.err, PSPO_DEVERR_TARGET);
+      return -1;
+    }
+    return __any(on) ? 1 : 0;
+  }
+  __device__ __forceinline__ int id(int i, int j, const Rows& r) const {
+    const int64_t at = (int64_t)i * r.k + j;
+    return entry(at) ? topk_ids[at] : -1;
+  }
+  // Lane j has the list's entry j.
+  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
+    const int64_t at = (int64_t)i * r.k + lane;
+    const bool on = use == 1 && lane < r.k && entry(at);
+    const int my = on ? topk_ids[at] : -1;
+    double div = 0.0, c = 0.0, g = 0.0;
+    bool first = on;
+    if (use == 1) {
+      const double x = on ? (double)topk[at] * r.inv_t : -INFINITY;
+      double top = x;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {   // (a NaN stays)
+        const double y = __shfl_xor(top, o);
+        top = y > top || y != y ? y : top;
+      }
+      const double e = on ? exp(x - top) : 0.0;
+      const double q = e / wave_sum(e);
+      double same = 0.0;   // the probability of this lane's id
+      for (int j = 0; j < r.k; ++j) {
+        const int other = __shfl(my, j);
+        const double qj = __shfl(q, j);
+        if (on && other == my) {
+          same += qj;
+          first = first && j >= lane;
+        }
+      }
+      c = (weight != nullptr ? (double)weight[i] : 1.0) * (double)scale;
+      const double lp = on ? (double)r.zs[at] * r.inv_t - lse : 0.0;
+      const double each = first && !(same == 0.0) ? same * (log(same) - lp) : 0.0;
+      div = wave_sum(each);
+      g = c * r.inv_t * (exp(lp) - same);
+      if (lane == 0 && !(std::isfinite(lse) && std::isfinite(c * div) && std::isfinite((float)(c * r.inv_t))))
+        raise(r.err, PSPO_DEVERR_NONFINITE);
+    }
+    if (lane < r.k) {
+      r.ids[at] = first ? my : -1;
+      r.g[at] = first ? (float)g : 0.f;
+    }
+    if (lane != 0) return;
+    r.terms[i] = use == 1 ? c * div : 0.0;
+    r.a[i] = (float)(c * r.inv_t);
+    if (kl != nullptr) kl[i] = use < 0 ? NAN : (float)div;
+  }
+};
+
+__global__ __launch_bounds__(256) void distill_loss_kernel(const double* __restrict__ terms, int64_t n,
+                                                           double* __restrict__ loss) {
+  __shared__ double sh[4];
+  const Sums s = sum_terms(terms, n, 1, sh);
+  if (threadIdx.x == 0) *loss = s.out[0];
+}
+
+// ---- 4. convert ---------------------------------------------------------------------------------
+// G of a row from its softmax entries (in place) or, kLogits, from its float32 logits: eight
+// entries a thread.  A row of factor 0 (left out, or clipped) is zeros whatever its entries are.
+// Grid (N, ceil(ld / 2048)).
+template <bool kLogits>
+__global__ __launch_bounds__(256) void convert_kernel(Rows r, const float* __restrict__ z, uint16_t* __restrict__ e) {
+  const int i = blockIdx.x, v0 = (blockIdx.y * 256 + threadIdx.x) * 8;
+  if (v0 >= r.ld) return;
+  const float a = r.a[i];
+  uint16_t* row = e + (int64_t)i * r.ld;
+  float x[8] = {};
+  if (a != 0.f) {
+    const float t = (float)(r.inv_t * 1.4426950408889634);
+    const double l2 = r.lse[i] * 1.4426950408889634;
+    if constexpr (kLogits) {
+      const f32x4* from = reinterpret_cast<const f32x4*>(z + (int64_t)i * r.ld + v0);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (v0 + k < r.V) x[k] = a * __builtin_amdgcn_exp2f(fmaf(from[k / 4][k % 4], t, -(float)l2));
+    } else {
+      const float f = a * __builtin_amdgcn_exp2f((float)((double)r.part[(int64_t)i * r.groups + v0 / kGroup].x * t - l2));
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(row + v0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[2 * k] = f * __uint_as_float(raw[k] << 16);
+        x[2 * k + 1] = f * __uint_as_float(raw[k] & 0xFFFF0000u);
+      }
+    }
+  }
+  put_bf16(row + v0, x);
+  const int32_t* ids = r.ids + (int64_t)i * r.k;
+  for (int j = 0; j < r.k; ++j) {
+    const int id = ids[j];
+    if ((uint32_t)(id - v0) < 8u) row[id] = (uint16_t)pack_bf16(r.g[(int64_t)i * r.k + j], 0.f);
+  }
+}
+
+__global__ __launch_bounds__(256) void fill_zero_kernel(u32x4* __restrict__ p, int64_t n) {
+  for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = u32x4{0, 0, 0, 0};
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+constexpr int kMostVocab = 1 << 21, kMostWidth = 1 << 20;   // a tile's rows stay below 2^31 bytes
+
+inline bool few_rows(int64_t N) { return N <= kSkinnyTokens; }
+
+struct Layout {
+  int64_t ld, groups;
+  int64_t use, zs, part, lse, a, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
+};
+// R, P: sequences and pairs of the preference loss.
+Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
+  Layout s{};
+  s.ld = round_up(V, kGroup);
+  const bool few = few_rows(N);
+  s.groups = few ? (V + kFewGroup - 1) / kFewGroup : s.ld / kGroup;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t x = at;
+    at = round_up(at + bytes, 256);
+    return x;
+  };
+  s.use = take(N * 4);
+  s.zs = take(N * k * 4);
+  s.part = take(N * s.groups * 8);
+  s.lse = take(N * 8);
+  s.a = take(N * 4);
+  s.ids = take(N * k * 4);
+  s.g = take(N * k * 4);
+  s.terms = take(N * 4 * 8);
+  s.copy = take(N * d * 2);
+  s.z = take(few ? N * s.ld * 4 : 0);
+  s.e = take(few && !grads ? 0 : N * s.ld * 2);
+  int64_t slab = slab_reserve(V, N, (int)d);
+  if (grads) slab = std::max({slab, slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
+  s.slab = take(slab);
+  s.seqs = take(R * 3 * 8);
+  s.pairs = take(P * 2 * 8);
+  s.total = at;
+  return s;
+}
+bool sizes_fit(int64_t N, int64_t d, int64_t V) {
+  return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab;
+}
+// Enough for any call of up to N rows: the float32 logits of few rows may take more than a few rows more do.
+size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
+  if (!sizes_fit(N, d, V)) return 0;
+  return (size_t)std::max(layout_of(N, d, V, k, R, P, grads).total,
+                          layout_of(std::min<int64_t>(N, kSkinnyTokens), d, V, k, R, P, grads).total);
+}
+
+// Tiles of both operands K-outer, or of A: 256 or 128 square.
+Plan plan_square(int64_t M, int64_t N, int K) {
+  const int nk = (K + kRowK - 1) / kRowK;
+  const Plan small = plan_tile(M, N, nk, 128, 128, false), big = plan_tile(M, N, nk, 256, 256, false);
+  return big.us <= small.us ? big : small;
+}
+
+struct Call {
+  const uint16_t *hidden, *w;
+  int32_t N, d, V, k;
+  float temperature, scale;
+  uint32_t flags, allowed;
+  void *dh, *dw;
+  double* loss;
+  int32_t* err;
+  void* workspace;
+  size_t workspace_bytes;
+  hipStream_t stream;
+  bool grads() const { return dh != nullptr || dw != nullptr; }
+};
+
+// The checks that the three calls share.
+int check(const Call& c) {
+  PSPO_REQUIRE(c.N >= 0, PSPO_ERR_INVALID_ARG, "N must be >= 0");
+  PSPO_REQUIRE(c.d > 0 && c.V > 0, PSPO_ERR_INVALID_ARG, "d and V must be > 0");
+  PSPO_REQUIRE(c.d % 8 == 0, PSPO_ERR_UNSUPPORTED, "d must be a multiple of 8");
+  PSPO_REQUIRE(c.d <= kMostWidth && c.V <= kMostVocab, PSPO_ERR_UNSUPPORTED, "d is at most 2^20 and V at most 2^21");
+  PSPO_REQUIRE((c.flags & ~c.allowed) == 0, PSPO_ERR_INVALID_ARG, "unknown flag bits");
+  PSPO_REQUIRE((c.flags & PSPO_ACCUMULATE_DW) == 0 || (c.flags & PSPO_OBJ_DW_F32) != 0, PSPO_ERR_INVALID_ARG,
+               "accumulating needs a float32 d_w_head");
+  PSPO_REQUIRE(std::isfinite(c.temperature) && c.temperature > 0.f && std::isfinite(1.f / c.temperature),
+               PSPO_ERR_INVALID_ARG, "temperature must be positive and finite");
+  PSPO_REQUIRE(std::isfinite(c.scale), PSPO_ERR_INVALID_ARG, "loss_scale must be finite");
+  PSPO_REQUIRE(c.loss != nullptr && aligned(c.loss, 8), PSPO_ERR_INVALID_ARG, "loss must be given, 8-byte aligned");
+  PSPO_REQUIRE(aligned(c.dh, 16) && aligned(c.dw, 16), PSPO_ERR_INVALID_ARG,
+               "d_hidden and d_w_head must be 16-byte aligned");
+  PSPO_REQUIRE(aligned(c.err, 4), PSPO_ERR_INVALID_ARG, "misaligned err_flag");
+  PSPO_REQUIRE(aligned(c.workspace, 256), PSPO_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (c.N > 0) {
+    PSPO_REQUIRE(c.hidden && c.w, PSPO_ERR_INVALID_ARG, "null input pointer");
+    PSPO_REQUIRE(aligned(c.hidden, 16) && aligned(c.w, 16), PSPO_ERR_INVALID_ARG,
+                 "hidden and w_head must be 16-byte aligned");
+  }
+  return PSPO_OK;
+}
+int check_workspace(const Call& c, int64_t need) {
+  PSPO_REQUIRE(need == 0 || c.workspace != nullptr, PSPO_ERR_INVALID_ARG, "workspace must be given");
+  PSPO_REQUIRE((int64_t)c.workspace_bytes >= need, PSPO_ERR_WORKSPACE,
+               "workspace too small: need " + std::to_string(need) + " bytes");
+  return require_gfx950();
+}
+
+Rows rows_of(const Call& c, const Layout& s) {
+  unsigned char* ws = static_cast<unsigned char*>(c.workspace);
+  Rows r{};
+  r.N = c.N;
+  r.d = c.d;
+  r.V = c.V;
+  r.k = c.k;
+  r.ld = s.ld;
+  r.groups = s.groups;
+  r.inv_t = 1.0 / (double)c.temperature;
+  r.use = reinterpret_cast<int32_t*>(ws + s.use);
+  r.zs = reinterpret_cast<float*>(ws + s.zs);
+  r.part = reinterpret_cast<f32x2*>(ws + s.part);
+  r.lse = reinterpret_cast<double*>(ws + s.lse);
+  r.a = reinterpret_cast<float*>(ws + s.a);
+  r.ids = reinterpret_cast<int32_t*>(ws + s.ids);
+  r.g = reinterpret_cast<float*>(ws + s.g);
+  r.terms = reinterpret_cast<double*>(ws + s.terms);
+  r.err = c.err;
+  return r;
+}
+
+// Steps 1 to 3 (N > 0).
+template <class Op>
+int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
+  unsigned char* ws = static_cast<unsigned char*>(c.workspace);
+  uint16_t *copy = reinterpret_cast<uint16_t*>(ws + s.copy), *e = reinterpret_cast<uint16_t*>(ws + s.e);
+  float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
+  const float t = (float)(r.inv_t * 1.4426950408889634);
+  hipLaunchKernelGGL(gather_kernel<Op>, dim3((unsigned)((c.N + 3) / 4)), dim3(256), 0, c.stream, r, op, c.hidden, c.w,
+                     copy);
+  PSPO_LAUNCHED("gather_kernel", c.stream);
+  if (few_rows(c.N)) {
+    if (int rc = skinny<1>(SkinnyArgs{{c.w, c.w}, copy, c.V, c.N, c.d}, SkinnyLogits{z, s.ld}, "objective_logits",
+                           c.stream))
+      return rc;
+    hipLaunchKernelGGL(few_groups_kernel, dim3((unsigned)c.N, (unsigned)s.groups), dim3(256), 0, c.stream, z, s.ld,
+                       c.V, t, r.part);
+    PSPO_LAUNCHED("few_groups_kernel", c.stream);
+  } else {
+    const Plan p = plan_of(c.V, c.N, (c.d + kRowK - 1) / kRowK, false);
+    if (int rc = product<false, false>(shape(c.w, c.w, c.d, c.V, copy, c.d, c.N, c.d), p, c.N,
+                                       EpiSoftmax{e, r.part, s.ld, c.V, c.N, t}, slab, "objective_logits", c.stream))
+      return rc;
+  }
+  hipLaunchKernelGGL(finalize_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op);
+  PSPO_LAUNCHED("finalize_kernel", c.stream);
+  return PSPO_OK;
+}
+
+// Steps 4 and 5.
+int backward(const Call& c, const Layout& s, const Rows& r) {
+  if (!c.grads()) return PSPO_OK;
+  unsigned char* ws = static_cast<unsigned char*>(c.workspace);
+  uint16_t *copy = reinterpret_cast<uint16_t*>(ws + s.copy), *e = reinterpret_cast<uint16_t*>(ws + s.e);
+  float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
+  const bool f32 = (c.flags & PSPO_OBJ_DW_F32) != 0, add = (c.flags & PSPO_ACCUMULATE_DW) != 0;
+  if (c.N == 0) {
+    if (c.dw == nullptr || add) return PSPO_OK;
+    hipLaunchKernelGGL(fill_zero_kernel, dim3(1024), dim3(256), 0, c.stream, static_cast<u32x4*>(c.dw),
+                       (int64_t)c.V * c.d / (f32 ? 4 : 8));
+    PSPO_LAUNCHED("fill_zero_kernel", c.stream);
+    return PSPO_OK;
+  }
+  const dim3 grid((unsigned)c.N, (unsigned)((s.ld + 2047) / 2048));
+  if (few_rows(c.N))
+    hipLaunchKernelGGL(convert_kernel<true>, grid, dim3(256), 0, c.stream, r, (const float*)z, e);
+  else
+    hipLaunchKernelGGL(convert_kernel<false>, grid, dim3(256), 0, c.stream, r, (const float*)nullptr, e);
+  PSPO_LAUNCHED("convert_kernel", c.stream);
+  if (c.dh != nullptr) {
+    const EpiStore o{c.dh, c.dh, c.d, c.d, c.N, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0, 0};
+    if (int rc = product<true, false>(shape(c.w, c.w, c.d, c.d, e, s.ld, c.N, c.V), plan_square(c.d, c.N, c.V), c.N, o,
+                                      slab, "objective_dh", c.stream))
+      return rc;
+  }
+  if (c.dw != nullptr) {
+    const EpiStore o{c.dw, c.dw, c.d, c.d, c.V, c.V, f32, add};
+    return product<true, true>(shape(copy, copy, c.d, c.d, e, s.ld, c.V, c.N), plan_square(c.d, c.V, c.N), c.V, o, slab,
+                               "objective_dw", c.stream);
+  }
+  return PSPO_OK;
+}
+
+}  // namespace
+}  // namespace pspo
+
+extern "C" {
+
+size_t pspo_policy_loss_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t grads) {
+  return pspo::workspace_size(N, d, V, 1, 0, 0, grads != 0);
+}
+size_t pspo_preference_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t R, int32_t P, int32_t grads) {
+  if (R < 0 || P < 0) return 0;
+  return pspo::workspace_size(N, d, V, 1, R, P, grads != 0);
+}
+size_t pspo_distill_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t k, int32_t grads) {
+  if (k < 1 || k > pspo::kMostIds) return 0;
+  return pspo::workspace_size(N, d, V, k, 0, 0, grads != 0);
+}
+
+int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
+                             const float* logp_old, const float* logp_ref, const float* weight, const int32_t* seq_id,
+                             const float* advantage, int32_t N, int32_t d, int32_t V, int32_t R, float eps_low,
+                             float eps_high, float kl_coef, int32_t kl_kind, float temperature, float loss_scale,
+                             uint32_t flags, double* loss, void* d_hidden, void* d_w_head, float* logp_new,
+                             double* stats, int32_t* err_flag, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream) {
+  using namespace pspo;
+  clear_last_error();
+  TraceRange trace_range("pspo_policy_loss_fwd_bwd");
+  const Call c{hidden, w_head, N, d, V, 1, temperature, loss_scale, flags,
+               PSPO_OBJ_DH_F32 | PSPO_OBJ_DW_F32 | PSPO_ACCUMULATE_DW, d_hidden, d_w_head, loss, err_flag, workspace,
+               workspace_bytes, stream};
+  if (int rc = check(c)) return rc;
+  PSPO_REQUIRE(R >= 0 && (N == 0 || R > 0), PSPO_ERR_INVALID_ARG, "R must be > 0 when N > 0");
+  PSPO_REQUIRE(std::isfinite(eps_low) && eps_low >= 0.f && eps_low < 1.f && std::isfinite(eps_high) &&
+                   eps_high >= 0.f && eps_high < 1.f,
+               PSPO_ERR_INVALID_ARG, "eps_low and eps_high must lie in [0, 1)");
+  PSPO_REQUIRE(std::isfinite(kl_coef), PSPO_ERR_INVALID_ARG, "kl_coef must be finite");
+  PSPO_REQUIRE(kl_kind >= PSPO_KL_K1 && kl_kind <= PSPO_KL_K3, PSPO_ERR_INVALID_ARG, "unknown kl_kind");
+  PSPO_REQUIRE(kl_coef == 0.f || N == 0 || logp_ref != nullptr, PSPO_ERR_INVALID_ARG, "kl_coef needs logp_ref");
+  PSPO_REQUIRE(aligned(logp_new, 4) && aligned(stats, 8), PSPO_ERR_INVALID_ARG, "misaligned output pointer");
+  if (N > 0) {
+    PSPO_REQUIRE(target && logp_old && weight && seq_id && advantage, PSPO_ERR_INVALID_ARG, "null input pointer");
+    PSPO_REQUIRE(aligned(target, 4) && aligned(logp_old, 4) && aligned(logp_ref, 4) && aligned(weight, 4) &&
+                     aligned(seq_id, 4) && aligned(advantage, 4),
+                 PSPO_ERR_INVALID_ARG, "misaligned per-token pointer");
+  }
+  const Layout s = layout_of(N, d, V, 1, 0, 0, c.grads());
+  if (int rc = check_workspace(c, N > 0 ? s.total : 0)) return rc;
+  const Rows r = rows_of(c, s);
+  if (N > 0)
+    if (int rc = forward(c, s, r,
+                         Policy{target, logp_old, logp_ref, weight, seq_id, advantage, R, eps_low, eps_high, kl_coef,
+                                loss_scale, kl_kind, logp_new}))
+      return rc;
+  hipLaunchKernelGGL(policy_loss_kernel, dim3(1), dim3(256), 0, stream, r.terms, (int64_t)N, kl_coef, loss, stats);
+  PSPO_LAUNCHED("policy_loss_kernel", stream);
+  return backward(c, s, r);
+}
+
+int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
+                            const float* logp_ref, const float* weight, const int32_t* cu_seqlens,
+                            const int32_t* chosen, const int32_t* rejected, int32_t N, int32_t d, int32_t V, int32_t R,
+                            int32_t P, int32_t kind, float beta, float smoothing, float temperature, float loss_scale,
+                            uint32_t flags, double* loss, void* d_hidden, void* d_w_head, float* logp_new,
+                            float* seq_ratio, float* margin, int32_t* err_flag, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream) {
+  using namespace pspo;
+  clear_last_error();
+  TraceRange trace_range("pspo_preference_fwd_bwd");
+  const Call c{hidden, w_head, N, d, V, 1, temperature, loss_scale, flags,
+               PSPO_OBJ_DH_F32 | PSPO_OBJ_DW_F32 | PSPO_ACCUMULATE_DW | PSPO_PREF_AVERAGE, d_hidden, d_w_head, loss,
+               err_flag, workspace, workspace_bytes, stream};
+  if (int rc = check(c)) return rc;
+  PSPO_REQUIRE(R >= 0 && P >= 0, PSPO_ERR_INVALID_ARG, "R and P must be >= 0");
+  PSPO_REQUIRE(kind == PSPO_PREF_SIGMOID || kind == PSPO_PREF_SQUARED, PSPO_ERR_INVALID_ARG, "unknown kind");
+  PSPO_REQUIRE(std::isfinite(beta) && beta > 0.f && std::isfinite(1.f / beta), PSPO_ERR_INVALID_ARG,
+               "beta must be positive and finite");
+  PSPO_REQUIRE(std::isfinite(smoothing) && smoothing >= 0.f && smoothing <= 1.f, PSPO_ERR_INVALID_ARG,
+               "smoothing must lie in [0, 1]");
+  PSPO_REQUIRE(kind == PSPO_PREF_SIGMOID || smoothing == 0.f, PSPO_ERR_INVALID_ARG,
+               "smoothing belongs to PSPO_PREF_SIGMOID");
+  PSPO_REQUIRE(cu_seqlens != nullptr && (P == 0 || (chosen && rejected)), PSPO_ERR_INVALID_ARG, "null input pointer");
+  PSPO_REQUIRE(N == 0 || target, PSPO_ERR_INVALID_ARG, "null input pointer");
+  PSPO_REQUIRE(aligned(target, 4) && aligned(logp_ref, 4) && aligned(weight, 4) && aligned(cu_seqlens, 4) &&
+                   aligned(chosen, 4) && aligned(rejected, 4) && aligned(logp_new, 4) && aligned(seq_ratio, 4) &&
+                   aligned(margin, 4),
+               PSPO_ERR_INVALID_ARG, "misaligned pointer");
+  const Layout s = layout_of(N, d, V, 1, R, P, c.grads());
+  if (int rc = check_workspace(c, s.total)) return rc;
+  const Rows r = rows_of(c, s);
+  double* seqs = reinterpret_cast<double*>(static_cast<unsigned char*>(workspace) + s.seqs);
+  double* pairs = reinterpret_cast<double*>(static_cast<unsigned char*>(workspace) + s.pairs);
+  const Pairs q{cu_seqlens, chosen, rejected, R, P, kind, (flags & PSPO_PREF_AVERAGE) != 0, beta, smoothing, loss_scale,
+                seqs, seqs + R, seqs + 2 * (int64_t)R, pairs, pairs + P, seq_ratio, margin, err_flag};
+  if (N > 0)
+    if (int rc = forward(c, s, r, Preference{target, logp_ref, weight, logp_new})) return rc;
+  if (R > 0) {
+    hipLaunchKernelGGL(pref_sequences_kernel, dim3((unsigned)R), dim3(256), 0, stream, q, N, (const double*)r.terms);
+    PSPO_LAUNCHED("pref_sequences_kernel", stream);
+  }
+  if (P > 0) {
+    hipLaunchKernelGGL(pref_pairs_kernel, dim3((unsigned)(((int64_t)P + 255) / 256)), dim3(256), 0, stream, q);
+    PSPO_LAUNCHED("pref_pairs_kernel", stream);
+  }
+  hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)R + 1), dim3(256), 0, stream, q, loss);
+  PSPO_LAUNCHED("pref_coef_kernel", stream);
+  if (N > 0 && c.grads()) {
+    hipLaunchKernelGGL(pref_rows_kernel, dim3((unsigned)(((int64_t)N + 255) / 256)), dim3(256), 0, stream, r, q, target);
+    PSPO_LAUNCHED("pref_rows_kernel", stream);
+  }
+  return backward(c, s, r);
+}
+
+int pspo_distill_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* topk_ids,
+                         const float* topk_logit, const float* weight, int32_t N, int32_t d, int32_t V, int32_t k,
+                         float temperature, float loss_scale, uint32_t flags, double* loss, void* d_hidden,
+                         void* d_w_head, float* kl, int32_t* err_flag, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream) {
+  using namespace pspo;
+  clear_last_error();
+  TraceRange trace_range("pspo_distill_fwd_bwd");
+  const Call c{hidden, w_head, N, d, V, k, temperature, loss_scale, flags,
+               PSPO_OBJ_DH_F32 | PSPO_OBJ_DW_F32 | PSPO_ACCUMULATE_DW, d_hidden, d_w_head, loss, err_flag, workspace,
+               workspace_bytes, stream};
+  if (int rc = check(c)) return rc;
+  PSPO_REQUIRE(k >= 1 && k <= kMostIds, PSPO_ERR_UNSUPPORTED, "k must lie in 1 .. 64");
+  PSPO_REQUIRE(N == 0 || (topk_ids && topk_logit), PSPO_ERR_INVALID_ARG, "null input pointer");
+  PSPO_REQUIRE(aligned(topk_ids, 4) && aligned(topk_logit, 4) && aligned(weight, 4) && aligned(kl, 4),
+               PSPO_ERR_INVALID_ARG, "misaligned pointer");
+  const Layout s = layout_of(N, d, V, k, 0, 0, c.grads());
+  if (int rc = check_workspace(c, N > 0 ? s.total : 0)) return rc;
+  const Rows r = rows_of(c, s);
+  if (N > 0)
+    if (int rc = forward(c, s, r, Distill{topk_ids, topk_logit, weight, loss_scale, kl})) return rc;
+  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(256), 0, stream, (const double*)r.terms, (int64_t)N, loss);
+  PSPO_LAUNCHED("distill_loss_kernel", stream);
+  return backward(c, s, r);
+}
+
+}  // extern "C"
