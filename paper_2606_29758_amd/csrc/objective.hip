@@ -10,16 +10,20 @@
 //
 // Schedule:
 //   1. gather: the rows that take part, copied (zeros for the others: a NaN there must not reach a
-//      sum over rows), and the logits at the ids as float32 dot products;
-//   2. product Z^T = W H^T; its epilogue writes exp(s (z - m_g)) in bf16, m_g the maximum over the
-//      group of 64 vocabulary entries, and (m_g, sum of the unrounded exponentials) of the group;
-//   3. finalize: a row's groups merged into log sum exp, then the objective's terms (the preference
-//      loss takes three small steps more: sequences, pairs, rows);
-//   4. convert, in place: G = a exp(s m_g - lse) * entry, and the entries at the ids;
-//   5. products dH = G W and dW = G^T H.
-// The matrix-core work is that of the formulas, 6 N d V, with no logit computed twice: the entries
-// cost 6 bytes each on their way (written, read and written again) against 2 d flops, 1.4 against 5
-// ns per 1000 entries at d = 3584.
+//      sum over rows), the logits at the ids as float32 dot products, and from them the row's
+//      reference c, the nearest integer to the largest of them times s log2(e);
+//   2. product Z^T = W H^T; its epilogue writes E = 2^(s log2(e) z - c) in bf16 and, for each group
+//      of 64 vocabulary entries, the sum of the unrounded values;
+//   3. finalize: the sums merged into log sum exp, the objective's terms, the entries at the ids
+//      put into E (the preference loss takes three small steps more: sequences, pairs, rows);
+//   4. products dH = f E W and dW = E^T (f H): a row's factor f = a 2^(c - lse log2(e)) goes into the
+//      epilogue of the first and into the copied hidden rows of the second.
+// The matrix-core work is that of the formulas, 6 N d V: no logit is computed twice, and between the
+// forward and the gradient products nothing passes over the N V entries (a conversion of them to G,
+// with a maximum of each group as reference, took 634 of 13,320 us at 4,999 rows, d = 3584,
+// V = 152064, and 142 of 585 at 2,501, 520, 32003).  c is a logit of the row, so its largest E is
+// 2^-1/2 at least; a group that would pass 2^32 takes its own reference, and its row is brought to
+// one reference in finalize (a power of two: exact).
 #include <cmath>
 
 #include "pspo_objective.h"
@@ -52,37 +56,55 @@ __device__ __forceinline__ float sum_of_8_lanes(float x) {
 }
 
 // ---- forward product ---------------------------------------------------------------
+// 2^(z t - c) with t = log2(e) / temperature in two parts: rounded to float32 alone, t would move
+// every exponent of a row by up to 2^-24 of it the same way, 1e-6 of the sum.
+struct Exponent {
+  float t, t_low;
+  __device__ __forceinline__ float operator()(float z, float c) const {
+    return __builtin_amdgcn_exp2f(fmaf(z, t_low, fmaf(z, t, -c)));
+  }
+};
+constexpr float kFar = 4294967296.f;   // largest sum of a group in its row's reference
+
 // Eight logits (vocabulary entries m .. m + 7 of row n); the 8 lanes of a group of 64 entries
-// hold it together, in a tile's epilogue and in a join alike.  The exponential's argument is formed
-// as (z - m) * t: as z t - m t in one fma it would carry the rounding of m t, 1e-6 of the sum.
+// hold it together, in a tile's epilogue and in a join alike.
 struct EpiSoftmax {
   static constexpr bool kPair = false;
-  uint16_t* e;      // [N][ld]
-  f32x2* part;      // [N][ld / 64]: maximum, sum
+  uint16_t* e;       // [N][ld]
+  f32x2* part;       // [N][ld / 64]: reference, sum
+  const float* c;    // [N]
   int64_t ld;
   int V, N;
-  float t;          // log2(e) / temperature
-  using Fetched = Nothing;
-  __device__ __forceinline__ Nothing fetch(int64_t, int64_t) const { return {}; }
-  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, Nothing) const {
-    float x[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = m + k < V ? v[k / 4][k % 4] : -INFINITY;
-    float top = x[0];
-#pragma unroll
-    for (int k = 1; k < 8; ++k) top = fmaxf(top, x[k]);
-    top = max_of_8_lanes(top);
-    const float from = top == -INFINITY ? 0.f : top;
+  Exponent exponent;
+  struct Fetched {
+    float c;
+  };
+  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t) const { return {n < N ? c[n] : 0.f}; }
+  __device__ __forceinline__ float values(float (&x)[8], const f32x4* v, int64_t m, float ref) const {
     float sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      x[k] = __builtin_amdgcn_exp2f((x[k] - from) * t);
-      sum += x[k];
+    for (int k = 0; k < 8; ++k) x[k] = exponent(v[k / 4][k % 4], ref);
+    if (m + 8 > V) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = m + k < V ? x[k] : 0.f;
     }
-    sum = sum_of_8_lanes(sum);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += x[k];
+    return sum_of_8_lanes(sum);
+  }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, const Fetched& row) const {
+    float x[8], ref = row.c;
+    float sum = values(x, v, m, ref);
+    if (sum > kFar) {   // the same in the 8 lanes
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, m + k < V ? v[k / 4][k % 4] : -INFINITY);
+      ref = rintf(max_of_8_lanes(top) * exponent.t);
+      sum = values(x, v, m, ref);
+    }
     if (n >= N || m >= ld) return;
     put_bf16(e + n * ld + m, x);
-    if (m % kGroup == 0) part[n * (ld / kGroup) + m / kGroup] = f32x2{top, sum};
+    if (m % kGroup == 0) part[n * (ld / kGroup) + m / kGroup] = f32x2{ref, sum};
   }
 };
 
@@ -121,9 +143,9 @@ __device__ __forceinline__ T block_total(T x, T* sh) {
   return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
-// (Maximum, sum) of the groups of 2,048 logits of a row.  Grid (N, groups).
-__global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict__ z, int64_t ld, int V, float t,
-                                                         f32x2* __restrict__ part) {
+// (Reference, sum) of the groups of 2,048 logits of a row.  Grid (N, groups).
+__global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict__ z, int64_t ld, int V,
+                                                         Exponent exponent, f32x2* __restrict__ part) {
   __shared__ float sh[4];
   const int v0 = blockIdx.y * kFewGroup + threadIdx.x * 8;
   const float* row = z + (int64_t)blockIdx.x * ld;
@@ -133,27 +155,29 @@ __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict
     x[k] = v0 + k < V ? row[v0 + k] : -INFINITY;
     top = fmaxf(top, x[k]);
   }
-  top = block_max(top, sh);
-  const float from = top == -INFINITY ? 0.f : top;
+  const float ref = rintf(block_max(top, sh) * exponent.t);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f((x[k] - from) * t);
+  for (int k = 0; k < 8; ++k) sum += v0 + k < V ? exponent(x[k], ref) : 0.f;
   sum = block_total(sum, sh);
-  if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{top, sum};
+  if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{ref, sum};
 }
 
 // ---- what a call's kernels share ------------------------------------------------------
 struct Rows {
   int N, d, V, k;          // k ids a row
+  int few, grads;          // logits kept in float32; gradients wanted
   int64_t ld, groups;      // entries between softmax rows; groups of a row
   double inv_t;
   int32_t* use;            // 1: takes part, 0: left out, -1: left out for an invalid id
   float* zs;               // [N][k] logits at the ids
+  float* c;                // reference of the row
   f32x2* part;
-  double* lse;
-  float* a;                // factor of p_i
+  double* lse2;            // log2 of the sum of 2^(z t)
+  float* f;                // factor of E
   int32_t* ids;            // [N][k] places of the entries set apart (-1: none) and their values
   float* g;
   double* terms;           // [4][N] of the loss
+  uint16_t *copy, *e;      // [N][d], [N][ld]
   int32_t* err;
 };
 
@@ -162,26 +186,31 @@ __device__ __forceinline__ void raise(int32_t* err, int bit) {
 }
 
 // ---- 1. gather -------------------------------------------------------------------------
-// A wave per row.  Op::use(i, lane, err): as Rows::use, the same in all lanes; Op::id(i, j): the
-// row's j-th id or -1.  Four ids' rows of W at a time beside the hidden row.
+// A work-group per row; its waves take four ids each in turn, whose rows of W are read beside the
+// hidden row.  Op::use(i, lane, r): as Rows::use, the same in all lanes; Op::id(i, j, r): the row's
+// j-th id or -1.
 template <class Op>
 __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16_t* __restrict__ hidden,
-                                                     const uint16_t* __restrict__ w, uint16_t* __restrict__ copy) {
-  const int i = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
-  if (i >= r.N) return;
+                                                     const uint16_t* __restrict__ w) {
+  __shared__ float sh[4];
+  const int i = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int use = op.use(i, lane, r);
-  if (lane == 0) r.use[i] = use;
+  if (threadIdx.x == 0) r.use[i] = use;
   const u32x4* from = reinterpret_cast<const u32x4*>(hidden + (int64_t)i * r.d);
-  u32x4* to = reinterpret_cast<u32x4*>(copy + (int64_t)i * r.d);
+  u32x4* to = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
   const int pieces = r.d / 8;
-  for (int c = lane; c < pieces; c += 64) {
+  for (int p = threadIdx.x; p < pieces; p += 256) {
     u32x4 x = {0, 0, 0, 0};
-    if (use == 1) x = from[c];
-    to[c] = x;
+    if (use == 1) x = from[p];
+    to[p] = x;
   }
-  if (use != 1) return;
+  if (use != 1) {
+    if (threadIdx.x == 0) r.c[i] = 0.f;
+    return;
+  }
   constexpr int kAt = 4;
-  for (int j0 = 0; j0 < r.k; j0 += kAt) {
+  float top = -INFINITY;
+  for (int j0 = wave * kAt; j0 < r.k; j0 += 4 * kAt) {
     const u32x4* row[kAt];
     bool on[kAt];
     float sum[kAt] = {};
@@ -191,12 +220,13 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
       on[j] = id >= 0;
       row[j] = reinterpret_cast<const u32x4*>(w + (int64_t)(on[j] ? id : 0) * r.d);
     }
-    for (int c = lane; c < pieces; c += 64) {
-      const u32x4 hv = from[c];
+#pragma unroll 2
+    for (int p = lane; p < pieces; p += 64) {
+      const u32x4 hv = from[p];
 #pragma unroll
       for (int j = 0; j < kAt; ++j) {
         if (!on[j]) continue;   // the same in all lanes
-        const u32x4 wv = row[j][c];
+        const u32x4 wv = row[j][p];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           sum[j] = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), sum[j]);
@@ -208,55 +238,103 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
     for (int j = 0; j < kAt; ++j) {
       sum[j] = wave_sum(sum[j]);
       if (lane == 0 && j0 + j < r.k) r.zs[(int64_t)i * r.k + j0 + j] = sum[j];
+      if (on[j]) top = fmaxf(top, sum[j]);
     }
+  }
+  top = block_max(top, sh);
+  if (threadIdx.x == 0) r.c[i] = rintf(top * (float)(r.inv_t * 1.4426950408889634));
+}
+
+// The row's hidden entries times its factor, the second operand of dW.
+__device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
+  u32x4* row = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
+  for (int p = threadIdx.x; p < r.d / 8; p += 256) {
+    u32x4 x = row[p];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      x[q] = f == 0.f ? 0u : pack_bf16(f * __uint_as_float(x[q] << 16), f * __uint_as_float(x[q] & 0xFFFF0000u));
+    row[p] = x;
   }
 }
 
 // ---- 3. finalize -----------------------------------------------------------------------
-// A work-group per row: log sum exp of its groups, merged in a fixed order, then op.row, called
-// by the first wave.
+// A work-group per row: log2 of the sum over its groups, in a fixed order (a row whose groups have
+// several references brought to the largest one); then op.row, called by the first wave, gives the
+// terms, the row's factor a of p and, in r.ids and r.g, the entries G / a at the ids.  E's own scale
+// is 2^(lse2 - c): the entries go in with it and the factor takes its inverse.
 template <class Op>
 __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   __shared__ float shf[4];
   __shared__ double shd[4];
+  __shared__ float factor;
   const int i = blockIdx.x;
   const int use = r.use[i];
-  double lse = 0.0;
+  uint16_t* row = r.e + (int64_t)i * r.ld;
+  double lse2 = 0.0;
+  float c = 0.f;
   if (use == 1) {
     const f32x2* part = r.part + (int64_t)i * r.groups;
-    const float t = (float)(r.inv_t * 1.4426950408889634);
-    float top = -INFINITY, sum = 0.f;
+    c = r.c[i];
+    float top = -INFINITY;
+    double sum = 0.0;
+    bool far = false;
     for (int g = threadIdx.x; g < r.groups; g += 256) {
       const f32x2 p = part[g];
-      if (p.x > top) {
-        sum = sum * __builtin_amdgcn_exp2f((top - p.x) * t) + p.y;
-        top = p.x;
-      } else if (p.x != -INFINITY || p.y != 0.f) {   // (a group of no entries adds nothing; a NaN stays)
-        sum += p.y * __builtin_amdgcn_exp2f((p.x - top) * t);
-      }
+      sum += p.y;
+      top = fmaxf(top, p.x);
+      far = far || p.x != c;
     }
-    const float all = block_max(top, shf);
-    const double total = block_total(top == -INFINITY && sum == 0.f
-                                         ? 0.0 : (double)sum * (double)__builtin_amdgcn_exp2f((top - all) * t), shd);
-    lse = (double)all * r.inv_t + log(total);
+    if (__syncthreads_or(far)) {
+      top = block_max(top, shf);
+      sum = 0.0;
+      for (int g = threadIdx.x; g < r.groups; g += 256) {
+        const f32x2 p = part[g];
+        if (p.x != -INFINITY || p.y != 0.f) sum += (double)p.y * (double)__builtin_amdgcn_exp2f(p.x - top);
+      }
+      if (!r.few && r.grads)
+        for (int64_t v0 = threadIdx.x * 8; v0 < r.ld; v0 += 2048) {
+          const float down = __builtin_amdgcn_exp2f(part[v0 / kGroup].x - top);
+          u32x4 x = *reinterpret_cast<const u32x4*>(row + v0);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            x[q] = pack_bf16(down * __uint_as_float(x[q] << 16), down * __uint_as_float(x[q] & 0xFFFF0000u));
+          *reinterpret_cast<u32x4*>(row + v0) = x;
+        }
+      c = top;
+    }
+    lse2 = (double)c + log2(block_total(sum, shd));
   }
-  if (threadIdx.x >= 64) return;
-  if (threadIdx.x == 0) r.lse[i] = lse;
-  op.row(i, threadIdx.x, use, lse, r);
+  if (r.few) c = (float)lse2;   // E is written from the logits, relative to the sum
+  if (threadIdx.x < 64) {
+    const float a = op.row(i, threadIdx.x, use, lse2 * 0.6931471805599453, r);
+    if (threadIdx.x == 0) {
+      r.lse2[i] = lse2;
+      r.c[i] = c;
+      factor = use == 1 && a != 0.f ? a * (float)exp2((double)c - lse2) : 0.f;
+      r.f[i] = factor;
+    }
+  }
+  if (!r.grads) return;
+  __syncthreads();   // also: the rescaled row, r.ids and r.g are written
+  if (!r.few && use == 1 && threadIdx.x < r.k) {
+    const int64_t at = (int64_t)i * r.k + threadIdx.x;
+    const int id = r.ids[at];
+    if (id >= 0) row[id] = (uint16_t)pack_bf16((float)((double)r.g[at] * exp2(lse2 - (double)c)), 0.f);
+  }
+  if (Op::kFactor) scale_copy(r, i, factor);
 }
 
-// Sums over the rows of up to four terms each ([4][n]), in a fixed order; one work-group.
-struct Sums {
-  double out[4];
-};
-__device__ __forceinline__ Sums sum_terms(const double* terms, int64_t n, int count, double* sh) {
-  Sums s{};
-  for (int q = 0; q < count; ++q) {
-    double x = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) x += terms[q * n + i];
-    s.out[q] = block_total(x, sh);
-  }
-  return s;
+// Sums over n terms each of up to four kinds ([kinds][n]), in a fixed order; one work-group of 256.
+template <int kKinds>
+__device__ __forceinline__ void sum_terms(const double* terms, int64_t n, double (&out)[kKinds], double* sh) {
+#pragma unroll
+  for (int q = 0; q < kKinds; ++q) out[q] = 0.0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < n; i += 256)
+#pragma unroll
+    for (int q = 0; q < kKinds; ++q) out[q] += terms[q * n + i];
+#pragma unroll
+  for (int q = 0; q < kKinds; ++q) out[q] = block_total(out[q], sh);
 }
 
 // ---- policy loss ---------------------------------------------------------------------------
@@ -270,6 +348,7 @@ __device__ __forceinline__ int target_use(int i, const int32_t* target, const fl
 }
 
 struct Policy {
+  static constexpr bool kFactor = true;   // row() knows the row's factor
   const int32_t* target;
   const float *logp_old, *logp_ref, *weight;
   const int32_t* seq_id;
@@ -288,8 +367,8 @@ struct Policy {
     return -1;
   }
   __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
-  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
-    if (lane != 0) return;
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
+    if (lane != 0) return 0.f;
     double gain = 0.0, div = 0.0, clipped = 0.0, delta = 0.0, l = 0.0;
     if (use == 1) {
       l = (double)r.zs[i] * r.inv_t - lse;
@@ -315,25 +394,27 @@ struct Policy {
     r.terms[n + i] = div;
     r.terms[2 * n + i] = clipped;
     r.terms[3 * n + i] = use == 1 ? 1.0 : 0.0;
-    r.a[i] = (float)(-delta * r.inv_t);
     r.ids[i] = use == 1 ? target[i] : -1;
-    r.g[i] = use == 1 ? (float)(-delta * r.inv_t * expm1(l)) : 0.f;
+    r.g[i] = use == 1 ? (float)expm1(l) : 0.f;
     if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
+    return (float)(-delta * r.inv_t);
   }
 };
 
 __global__ __launch_bounds__(256) void policy_loss_kernel(const double* __restrict__ terms, int64_t n, float kl_coef,
                                                           double* __restrict__ loss, double* __restrict__ stats) {
   __shared__ double sh[4];
-  const Sums s = sum_terms(terms, n, 4, sh);
+  double s[4];
+  sum_terms<4>(terms, n, s, sh);
   if (threadIdx.x != 0) return;
-  *loss = kl_coef != 0.f ? (double)kl_coef * s.out[1] - s.out[0] : -s.out[0];
+  *loss = kl_coef != 0.f ? (double)kl_coef * s[1] - s[0] : -s[0];
   if (stats != nullptr)
-    for (int q = 0; q < 4; ++q) stats[q] = s.out[q];
+    for (int q = 0; q < 4; ++q) stats[q] = s[q];
 }
 
 // ---- preference loss ------------------------------------------------------------------------
 struct Preference {
+  static constexpr bool kFactor = false;   // pref_rows_kernel does
   const int32_t* target;
   const float *logp_ref, *weight;
   float* logp_new;
@@ -343,8 +424,8 @@ struct Preference {
   }
   __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
   // terms: the log-prob, the row's part of its sequence's log ratio, its weight
-  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
-    if (lane != 0) return;
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
+    if (lane != 0) return 0.f;
     double l = 0.0, part = 0.0, c = 0.0;
     if (use == 1) {
       l = (double)r.zs[i] * r.inv_t - lse;
@@ -356,7 +437,10 @@ struct Preference {
     r.terms[i] = l;
     r.terms[n + i] = part;
     r.terms[2 * n + i] = c;
+    r.ids[i] = use == 1 ? target[i] : -1;
+    r.g[i] = use == 1 ? (float)expm1(l) : 0.f;
     if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
+    return 0.f;
   }
 };
 
@@ -436,8 +520,9 @@ __global__ __launch_bounds__(256) void pref_coef_kernel(Pairs q, double* __restr
   __shared__ double sh[4];
   const int r = blockIdx.x;
   if (r == q.R) {
-    const Sums s = sum_terms(q.pair_loss, q.P, 1, sh);
-    if (threadIdx.x == 0) *loss = s.out[0];
+    double s[1];
+    sum_terms<1>(q.pair_loss, q.P, s, sh);
+    if (threadIdx.x == 0) *loss = s[0];
     return;
   }
   double c = 0.0;
@@ -450,28 +535,29 @@ __global__ __launch_bounds__(256) void pref_coef_kernel(Pairs q, double* __restr
   if (threadIdx.x == 0) q.coef[r] = q.norm[r] != 0.0 ? c * q.norm[r] : 0.0;
 }
 
-// The row's factors, from its sequence's.
-__global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q, const int32_t* __restrict__ target) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= r.N) return;
+// The row's factor, from its sequence's; a work-group per row.
+__global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
+  const int i = blockIdx.x;
   int s = 0, e = q.R;   // the last sequence that starts at or before row i
   while (s < e) {
     const int mid = s + (e - s) / 2;
     if (q.cu[mid + 1] > i) e = mid;
     else s = mid + 1;
   }
-  const bool in = s < q.R && q.cu[s] <= i;
-  const int64_t n = r.N;
-  const bool on = in && r.use[i] == 1;
-  const double l = r.terms[i], delta = on ? q.coef[s] * r.terms[2 * n + i] : 0.0;
-  if (on && !std::isfinite((float)delta)) raise(r.err, PSPO_DEVERR_NONFINITE);
-  r.a[i] = (float)(-delta * r.inv_t);
-  r.ids[i] = on ? target[i] : -1;
-  r.g[i] = on ? (float)(-delta * r.inv_t * expm1(l)) : 0.f;
+  const bool on = s < q.R && q.cu[s] <= i && r.use[i] == 1;
+  const double delta = on ? q.coef[s] * r.terms[2 * (int64_t)r.N + i] : 0.0;
+  const float a = (float)(-delta * r.inv_t);
+  const float f = on && a != 0.f ? a * (float)exp2((double)r.c[i] - r.lse2[i]) : 0.f;
+  if (threadIdx.x == 0) {
+    if (on && !std::isfinite(a)) raise(r.err, PSPO_DEVERR_NONFINITE);
+    r.f[i] = f;
+  }
+  scale_copy(r, i, f);
 }
 
 // ---- distillation -----------------------------------------------------------------------------
 struct Distill {
+  static constexpr bool kFactor = true;
   const int32_t* topk_ids;
   const float* topk;
   const float* weight;
@@ -497,7 +583,7 @@ struct Distill {
     return entry(at) ? topk_ids[at] : -1;
   }
   // Lane j has the list's entry j.
-  __device__ __forceinline__ void row(int i, int lane, int use, double lse, const Rows& r) const {
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
     const int64_t at = (int64_t)i * r.k + lane;
     const bool on = use == 1 && lane < r.k && entry(at);
     const int my = on ? topk_ids[at] : -1;
@@ -526,7 +612,7 @@ struct Distill {
       const double lp = on ? (double)r.zs[at] * r.inv_t - lse : 0.0;
       const double each = first && !(same == 0.0) ? same * (log(same) - lp) : 0.0;
       div = wave_sum(each);
-      g = c * r.inv_t * (exp(lp) - same);
+      g = exp(lp) - same;
       if (lane == 0 && !(std::isfinite(lse) && std::isfinite(c * div) && std::isfinite((float)(c * r.inv_t))))
         raise(r.err, PSPO_DEVERR_NONFINITE);
     }
@@ -534,56 +620,67 @@ struct Distill {
       r.ids[at] = first ? my : -1;
       r.g[at] = first ? (float)g : 0.f;
     }
-    if (lane != 0) return;
+    if (lane != 0) return 0.f;
     r.terms[i] = use == 1 ? c * div : 0.0;
-    r.a[i] = (float)(c * r.inv_t);
     if (kl != nullptr) kl[i] = use < 0 ? NAN : (float)div;
+    return (float)(c * r.inv_t);
   }
 };
 
 __global__ __launch_bounds__(256) void distill_loss_kernel(const double* __restrict__ terms, int64_t n,
                                                            double* __restrict__ loss) {
   __shared__ double sh[4];
-  const Sums s = sum_terms(terms, n, 1, sh);
-  if (threadIdx.x == 0) *loss = s.out[0];
+  double s[1];
+  sum_terms<1>(terms, n, s, sh);
+  if (threadIdx.x == 0) *loss = s[0];
 }
 
-// ---- 4. convert ---------------------------------------------------------------------------------
-// G of a row from its softmax entries (in place) or, kLogits, from its float32 logits: eight
-// entries a thread.  A row of factor 0 (left out, or clipped) is zeros whatever its entries are.
-// Grid (N, ceil(ld / 2048)).
-template <bool kLogits>
-__global__ __launch_bounds__(256) void convert_kernel(Rows r, const float* __restrict__ z, uint16_t* __restrict__ e) {
+// ---- E of few rows ---------------------------------------------------------------------------
+// From the float32 logits, relative to the row's sum, eight entries a thread; zeros where the factor
+// is 0.  Grid (N, ceil(ld / 2048)).
+__global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* __restrict__ z, Exponent exponent) {
   const int i = blockIdx.x, v0 = (blockIdx.y * 256 + threadIdx.x) * 8;
   if (v0 >= r.ld) return;
-  const float a = r.a[i];
-  uint16_t* row = e + (int64_t)i * r.ld;
+  uint16_t* row = r.e + (int64_t)i * r.ld;
   float x[8] = {};
-  if (a != 0.f) {
-    const float t = (float)(r.inv_t * 1.4426950408889634);
-    const double l2 = r.lse[i] * 1.4426950408889634;
-    if constexpr (kLogits) {
-      const f32x4* from = reinterpret_cast<const f32x4*>(z + (int64_t)i * r.ld + v0);
+  const bool on = r.f[i] != 0.f;
+  if (on) {
+    const float c = r.c[i];
+    const f32x4* from = reinterpret_cast<const f32x4*>(z + (int64_t)i * r.ld + v0);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (v0 + k < r.V) x[k] = a * __builtin_amdgcn_exp2f(fmaf(from[k / 4][k % 4], t, -(float)l2));
-    } else {
-      const float f = a * __builtin_amdgcn_exp2f((float)((double)r.part[(int64_t)i * r.groups + v0 / kGroup].x * t - l2));
-      const u32x4 raw = *reinterpret_cast<const u32x4*>(row + v0);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[2 * k] = f * __uint_as_float(raw[k] << 16);
-        x[2 * k + 1] = f * __uint_as_float(raw[k] & 0xFFFF0000u);
-      }
-    }
+    for (int k = 0; k < 8; ++k)
+      if (v0 + k < r.V) x[k] = exponent(from[k / 4][k % 4], c);
   }
   put_bf16(row + v0, x);
+  if (!on) return;
   const int32_t* ids = r.ids + (int64_t)i * r.k;
+  const float up = (float)exp2(r.lse2[i] - (double)r.c[i]);
   for (int j = 0; j < r.k; ++j) {
     const int id = ids[j];
-    if ((uint32_t)(id - v0) < 8u) row[id] = (uint16_t)pack_bf16(r.g[(int64_t)i * r.k + j], 0.f);
+    if ((uint32_t)(id - v0) < 8u) row[id] = (uint16_t)pack_bf16(r.g[(int64_t)i * r.k + j] * up, 0.f);
   }
 }
+
+// C(m, n) = sum over the vocabulary of W(v, m) E(n, v): d_hidden[n][m] = f[n] C.
+struct EpiHidden {
+  static constexpr bool kPair = false;
+  void* out;
+  const float* f;
+  int64_t ld;
+  int M, N, f32;
+  struct Fetched {
+    float f;
+  };
+  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t) const { return {n < N ? f[n] : 0.f}; }
+  __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, const Fetched& x) const {
+    if (n >= N || m >= M) return;   // M % 8 == 0
+    f32x4 s[2];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k / 4][k % 4] = x.f == 0.f ? 0.f : x.f * v[k / 4][k % 4];   // a row left out is zeros
+    if (f32) put_f32(static_cast<float*>(out) + n * ld + m, s);
+    else put_bf16(static_cast<uint16_t*>(out) + n * ld + m, reinterpret_cast<const float*>(s));
+  }
+};
 
 __global__ __launch_bounds__(256) void fill_zero_kernel(u32x4* __restrict__ p, int64_t n) {
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = u32x4{0, 0, 0, 0};
@@ -596,7 +693,7 @@ inline bool few_rows(int64_t N) { return N <= kSkinnyTokens; }
 
 struct Layout {
   int64_t ld, groups;
-  int64_t use, zs, part, lse, a, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
+  int64_t use, zs, c, part, lse2, f, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
 };
 // R, P: sequences and pairs of the preference loss.
 Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
@@ -612,9 +709,10 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   };
   s.use = take(N * 4);
   s.zs = take(N * k * 4);
+  s.c = take(N * 4);
   s.part = take(N * s.groups * 8);
-  s.lse = take(N * 8);
-  s.a = take(N * 4);
+  s.lse2 = take(N * 8);
+  s.f = take(N * 4);
   s.ids = take(N * k * 4);
   s.g = take(N * k * 4);
   s.terms = take(N * 4 * 8);
@@ -700,40 +798,48 @@ Rows rows_of(const Call& c, const Layout& s) {
   r.k = c.k;
   r.ld = s.ld;
   r.groups = s.groups;
+  r.few = few_rows(c.N);
+  r.grads = c.grads();
   r.inv_t = 1.0 / (double)c.temperature;
   r.use = reinterpret_cast<int32_t*>(ws + s.use);
   r.zs = reinterpret_cast<float*>(ws + s.zs);
+  r.c = reinterpret_cast<float*>(ws + s.c);
   r.part = reinterpret_cast<f32x2*>(ws + s.part);
-  r.lse = reinterpret_cast<double*>(ws + s.lse);
-  r.a = reinterpret_cast<float*>(ws + s.a);
+  r.lse2 = reinterpret_cast<double*>(ws + s.lse2);
+  r.f = reinterpret_cast<float*>(ws + s.f);
   r.ids = reinterpret_cast<int32_t*>(ws + s.ids);
   r.g = reinterpret_cast<float*>(ws + s.g);
   r.terms = reinterpret_cast<double*>(ws + s.terms);
+  r.copy = reinterpret_cast<uint16_t*>(ws + s.copy);
+  r.e = reinterpret_cast<uint16_t*>(ws + s.e);
   r.err = c.err;
   return r;
+}
+
+Exponent exponent_of(const Rows& r) {
+  const double t = r.inv_t * 1.4426950408889634;
+  return Exponent{(float)t, (float)(t - (double)(float)t)};
 }
 
 // Steps 1 to 3 (N > 0).
 template <class Op>
 int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
-  uint16_t *copy = reinterpret_cast<uint16_t*>(ws + s.copy), *e = reinterpret_cast<uint16_t*>(ws + s.e);
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
-  const float t = (float)(r.inv_t * 1.4426950408889634);
-  hipLaunchKernelGGL(gather_kernel<Op>, dim3((unsigned)((c.N + 3) / 4)), dim3(256), 0, c.stream, r, op, c.hidden, c.w,
-                     copy);
+  hipLaunchKernelGGL(gather_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
   PSPO_LAUNCHED("gather_kernel", c.stream);
-  if (few_rows(c.N)) {
-    if (int rc = skinny<1>(SkinnyArgs{{c.w, c.w}, copy, c.V, c.N, c.d}, SkinnyLogits{z, s.ld}, "objective_logits",
+  if (r.few) {
+    if (int rc = skinny<1>(SkinnyArgs{{c.w, c.w}, r.copy, c.V, c.N, c.d}, SkinnyLogits{z, s.ld}, "objective_logits",
                            c.stream))
       return rc;
     hipLaunchKernelGGL(few_groups_kernel, dim3((unsigned)c.N, (unsigned)s.groups), dim3(256), 0, c.stream, z, s.ld,
-                       c.V, t, r.part);
+                       c.V, exponent_of(r), r.part);
     PSPO_LAUNCHED("few_groups_kernel", c.stream);
   } else {
     const Plan p = plan_of(c.V, c.N, (c.d + kRowK - 1) / kRowK, false);
-    if (int rc = product<false, false>(shape(c.w, c.w, c.d, c.V, copy, c.d, c.N, c.d), p, c.N,
-                                       EpiSoftmax{e, r.part, s.ld, c.V, c.N, t}, slab, "objective_logits", c.stream))
+    if (int rc = product<false, false>(shape(c.w, c.w, c.d, c.V, r.copy, c.d, c.N, c.d), p, c.N,
+                                       EpiSoftmax{r.e, r.part, r.c, s.ld, c.V, c.N, exponent_of(r)}, slab,
+                                       "objective_logits", c.stream))
       return rc;
   }
   hipLaunchKernelGGL(finalize_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op);
@@ -741,11 +847,10 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   return PSPO_OK;
 }
 
-// Steps 4 and 5.
+// Step 4.
 int backward(const Call& c, const Layout& s, const Rows& r) {
   if (!c.grads()) return PSPO_OK;
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
-  uint16_t *copy = reinterpret_cast<uint16_t*>(ws + s.copy), *e = reinterpret_cast<uint16_t*>(ws + s.e);
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
   const bool f32 = (c.flags & PSPO_OBJ_DW_F32) != 0, add = (c.flags & PSPO_ACCUMULATE_DW) != 0;
   if (c.N == 0) {
@@ -755,22 +860,21 @@ int backward(const Call& c, const Layout& s, const Rows& r) {
     PSPO_LAUNCHED("fill_zero_kernel", c.stream);
     return PSPO_OK;
   }
-  const dim3 grid((unsigned)c.N, (unsigned)((s.ld + 2047) / 2048));
-  if (few_rows(c.N))
-    hipLaunchKernelGGL(convert_kernel<true>, grid, dim3(256), 0, c.stream, r, (const float*)z, e);
-  else
-    hipLaunchKernelGGL(convert_kernel<false>, grid, dim3(256), 0, c.stream, r, (const float*)nullptr, e);
-  PSPO_LAUNCHED("convert_kernel", c.stream);
+  if (r.few) {
+    hipLaunchKernelGGL(few_entries_kernel, dim3((unsigned)c.N, (unsigned)((s.ld + 2047) / 2048)), dim3(256), 0,
+                       c.stream, r, (const float*)z, exponent_of(r));
+    PSPO_LAUNCHED("few_entries_kernel", c.stream);
+  }
   if (c.dh != nullptr) {
-    const EpiStore o{c.dh, c.dh, c.d, c.d, c.N, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0, 0};
-    if (int rc = product<true, false>(shape(c.w, c.w, c.d, c.d, e, s.ld, c.N, c.V), plan_square(c.d, c.N, c.V), c.N, o,
-                                      slab, "objective_dh", c.stream))
+    const EpiHidden o{c.dh, r.f, c.d, c.d, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0};
+    if (int rc = product<true, false>(shape(c.w, c.w, c.d, c.d, r.e, s.ld, c.N, c.V), plan_square(c.d, c.N, c.V), c.N,
+                                      o, slab, "objective_dh", c.stream))
       return rc;
   }
   if (c.dw != nullptr) {
     const EpiStore o{c.dw, c.dw, c.d, c.d, c.V, c.V, f32, add};
-    return product<true, true>(shape(copy, copy, c.d, c.d, e, s.ld, c.V, c.N), plan_square(c.d, c.V, c.N), c.V, o, slab,
-                               "objective_dw", c.stream);
+    return product<true, true>(shape(r.copy, r.copy, c.d, c.d, r.e, s.ld, c.V, c.N), plan_square(c.d, c.V, c.N), c.V, o,
+                               slab, "objective_dw", c.stream);
   }
   return PSPO_OK;
 }
@@ -881,7 +985,7 @@ int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, cons
   hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)R + 1), dim3(256), 0, stream, q, loss);
   PSPO_LAUNCHED("pref_coef_kernel", stream);
   if (N > 0 && c.grads()) {
-    hipLaunchKernelGGL(pref_rows_kernel, dim3((unsigned)(((int64_t)N + 255) / 256)), dim3(256), 0, stream, r, q, target);
+    hipLaunchKernelGGL(pref_rows_kernel, dim3((unsigned)N), dim3(256), 0, stream, r, q);
     PSPO_LAUNCHED("pref_rows_kernel", stream);
   }
   return backward(c, s, r);

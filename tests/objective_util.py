@@ -3,12 +3,12 @@
 u = 2^-24 is one float32 rounding, B = 2^-8 half a bf16 step.  Carried through the formulas:
   z     a float32 sum of d exact products: (d + 2) u times the sum of their sizes;
   lse   the mean of z's errors under p, and 64 u + 8 u |z| spread for the exponentials (the instruction's argument
-        (z - m) t carries two roundings of up to |z - m| t, its result one) and the sums of up to 64 + 8 terms
+        carries two roundings of up to its size, its result one) and the sums of up to 64 + 8 terms
         of a group (the groups' sums are joined in float64, their scalings take 4 u);
   l     z's and lse's;
-  G     twice B (the softmax entry, then the product with its factor), the exponent's error, and the factor's;
-        an entry set apart its own error and B once;
-  dH, dW  float32 sums of V and N terms, B once more where the output is bf16.
+  G     B for the softmax entry, the exponent's error, and the factor's; an entry set apart its own error and B;
+  dH    float32 sums of V terms, dW float32 sums of N terms whose hidden rows, times their factors, take B as well;
+        B once more where the output is bf16.
 Second-order terms are covered by a factor 1.02 on the whole.
 """
 import numpy as np
@@ -42,7 +42,7 @@ class Bounds:
         s = 1 / temperature
         self.s, self.h, self.w, self.on = s, np.where(on[:, None], h, 0), w, on
         d = h.shape[1]
-        self.p = np.exp(lp)
+        self.p, self.lp = np.exp(lp), lp
         self.ez = s * (d + 2) * U * (np.abs(self.h) @ np.abs(w).T)
         spread = lp.max(1, keepdims=True) - lp
         self.e_lse = ((self.p * (self.ez + 8 * U * spread)).sum(1) + 64 * U) * 1.02
@@ -51,11 +51,11 @@ class Bounds:
     def logp(self, target):
         i = np.arange(len(target))
         t = np.where(self.on, target, 0)
-        return self.ez[i, t] + self.e_lse + U * np.abs(np.log(self.p[i, t]))
+        return self.ez[i, t] + self.e_lse + U * np.abs(self.lp[i, t])
 
     def of_G(self, G, a, e_a, set_apart, e_set):
         """G's bound: a the factor of p with error e_a ([N]); entries set apart ([N, V] mask) with error e_set."""
-        e = np.abs(a)[:, None] * self.p * (2 * B + B * B + self.ep) + e_a[:, None] * self.p
+        e = np.abs(a)[:, None] * self.p * (B + self.ep + 6 * U) + e_a[:, None] * self.p
         return np.where(set_apart, e_set + B * (np.abs(G) + e_set), e) * 1.02
 
     def gradients(self, G, eG, bf16_h, bf16_w):
@@ -63,7 +63,7 @@ class Bounds:
         dh, dw = oo.gradients(G, self.h, self.w, self.on)
         size = np.abs(G) + eG
         e_h = eG @ aw + (V + 66) * U * (size @ aw)
-        e_w = eG.T @ ah + (N + 66) * U * (size.T @ ah)
+        e_w = (eG + B * size).T @ ah + (N + 66) * U * (1 + B) * (size.T @ ah)
         if bf16_h:
             e_h = e_h + B * (np.abs(dh) + e_h)
         if bf16_w:

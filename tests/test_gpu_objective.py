@@ -47,9 +47,10 @@ def _gradients(o, ref, b, eG, d_hidden, d_w):
     close(d_w, dw, e_w, "d_w_head")
 
 
-def run_policy(N, d, V, seed=0, R=3, kl="k3", coef=0.05, T=1.0, masked=0.2, f32=False):
+def run_policy(N, d, V, seed=0, R=3, kl="k3", coef=0.05, T=1.0, masked=0.2, f32=False, wide=1.0):
     r = np.random.default_rng(seed)
     h, w, target = matrices(N, d, V, seed)
+    h = h * wide
     l = _logp(h, w, target, T)
     seq, adv = np.sort(r.integers(0, R, N)), _f32(r.normal(size=R))
     shift = r.normal(size=N) * 0.2
@@ -83,9 +84,10 @@ def run_policy(N, d, V, seed=0, R=3, kl="k3", coef=0.05, T=1.0, masked=0.2, f32=
 
 
 def run_preference(N, d, V, seed=0, R=4, P=5, kind="sigmoid", smoothing=0.0, average=False, beta=0.1, T=1.0, masked=0.2,
-                   f32=False, ref=True, weights=True):
+                   f32=False, ref=True, weights=True, wide=1.0):
     r = np.random.default_rng(seed)
     h, w, target = matrices(N, d, V, seed)
+    h = h * wide
     refp = _f32(_logp(h, w, target, T) - 0.05 - 0.2 * r.normal(size=N)) if ref else None
     weight = _f32(r.uniform(0.5, 2, N)) if weights else None
     off = _mask(r, N, masked) if weights else np.zeros(N, dtype=bool)
@@ -121,9 +123,10 @@ def run_preference(N, d, V, seed=0, R=4, P=5, kind="sigmoid", smoothing=0.0, ave
     return o
 
 
-def run_distill(N, d, V, seed=0, k=5, T=1.0, masked=0.2, f32=False, weights=True, repeats=True):
+def run_distill(N, d, V, seed=0, k=5, T=1.0, masked=0.2, f32=False, weights=True, repeats=True, wide=1.0):
     r = np.random.default_rng(seed)
     h, w, target = matrices(N, d, V, seed)
+    h = h * wide
     ids = r.integers(0, V, (N, k))   # the same id more than once, where V is small
     if not repeats:
         ids = np.stack([r.permutation(V)[:k] for _ in range(N)])
@@ -194,6 +197,15 @@ def test_preference_pairs(kw):
 @pytest.mark.parametrize("kw", [dict(k=64), dict(k=1), dict(weights=False), dict(V=3, k=9), dict(k=40, repeats=False)])
 def test_distill_lists(kw):
     run_distill(**dict(dict(N=150, d=64, V=500, seed=8), **kw))
+
+
+@pytest.mark.parametrize("N,T", [(40, 1.0), (150, 1.0), (150, 0.25), (300, 0.05)])
+def test_targets_far_below_the_largest_logit(N, T):
+    """Logits of some hundred times the temperature: groups of entries that pass their row's reference, down to
+    rows whose target has no weight left."""
+    run_policy(N, 64, 1000, seed=1, wide=30.0, T=T, kl="k1")
+    run_preference(N, 64, 1000, seed=2, wide=30.0, T=T, beta=0.01)
+    run_distill(N, 64, 1000, seed=3, wide=30.0, T=T, k=3)
 
 
 @pytest.mark.parametrize("N", [20, 200])
