@@ -18,11 +18,11 @@
  * term, d_hidden row and per-token outputs are 0.  A row that has an invalid id
  * raises the error bit, takes no part either and has NaN in its per-token outputs.
  *
- * Precision: logits, softmax sums and log-probs are float32 sums of exact bf16
- * products, per-token terms and the loss float64.  The softmax entries between the
- * forward and the gradient products and the entries of G are rounded to bf16 (the
- * matrix cores' operand type; together 2^-8 relative an entry at most), sums of the
- * gradient products are float32.
+ * Precision: logits and softmax sums are float32 sums of exact bf16 products,
+ * per-row terms and the loss float64.  The softmax entries (with the entries of G at
+ * the ids in their places) and, for d_w_head, the hidden rows times their factors are
+ * rounded to bf16, the matrix cores' operand type, once each; sums of the gradient
+ * products are float32.
  *
  * Memory: the softmax entries of all N rows are kept in the workspace, 2 bytes each
  * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time.
@@ -90,7 +90,8 @@ size_t pspo_distill_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t k, 
  *  err_flag   device, int32 [1] or NULL: PSPO_DEVERR_TARGET, PSPO_DEVERR_SEQ_ID,
  *             PSPO_DEVERR_NONFINITE (a value of a row that takes part is not finite).
  *  workspace  device, 256-byte aligned; contents on entry ignored.
- * Sizes: V <= 2^21, d <= 2^20.  Device pointers of matrices 16-byte aligned.
+ * Sizes: N <= 2^26, V <= 2^21, d <= 2^20, and N d, N V, V d <= 2^36 (PSPO_ERR_UNSUPPORTED
+ * beyond).  Device pointers of matrices 16-byte aligned.
  */
 int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
                              const float* logp_old, const float* logp_ref, const float* weight,

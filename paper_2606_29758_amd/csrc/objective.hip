@@ -688,6 +688,8 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(u32x4* __restrict__ p, i
 
 // ---- host ------------------------------------------------------------------------------------------
 constexpr int kMostVocab = 1 << 21, kMostWidth = 1 << 20;   // a tile's rows stay below 2^31 bytes
+constexpr int kMostRows = 1 << 26;
+constexpr int64_t kMostEntries = int64_t(1) << 36;            // of a matrix: fewer tiles than a launch holds
 
 inline bool few_rows(int64_t N) { return N <= kSkinnyTokens; }
 
@@ -728,7 +730,8 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   return s;
 }
 bool sizes_fit(int64_t N, int64_t d, int64_t V) {
-  return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab;
+  return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab && N <= kMostRows &&
+         N * d <= kMostEntries && N * V <= kMostEntries && V * d <= kMostEntries;
 }
 // Enough for any call of up to N rows: the float32 logits of few rows may take more than a few rows more do.
 size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
@@ -763,7 +766,8 @@ int check(const Call& c) {
   PSPO_REQUIRE(c.N >= 0, PSPO_ERR_INVALID_ARG, "N must be >= 0");
   PSPO_REQUIRE(c.d > 0 && c.V > 0, PSPO_ERR_INVALID_ARG, "d and V must be > 0");
   PSPO_REQUIRE(c.d % 8 == 0, PSPO_ERR_UNSUPPORTED, "d must be a multiple of 8");
-  PSPO_REQUIRE(c.d <= kMostWidth && c.V <= kMostVocab, PSPO_ERR_UNSUPPORTED, "d is at most 2^20 and V at most 2^21");
+  PSPO_REQUIRE(sizes_fit(c.N, c.d, c.V), PSPO_ERR_UNSUPPORTED,
+               "N is at most 2^26, d 2^20, V 2^21, and N d, N V and V d 2^36");
   PSPO_REQUIRE((c.flags & ~c.allowed) == 0, PSPO_ERR_INVALID_ARG, "unknown flag bits");
   PSPO_REQUIRE((c.flags & PSPO_ACCUMULATE_DW) == 0 || (c.flags & PSPO_OBJ_DW_F32) != 0, PSPO_ERR_INVALID_ARG,
                "accumulating needs a float32 d_w_head");
