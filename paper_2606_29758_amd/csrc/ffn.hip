@@ -120,65 +120,12 @@ struct EpiDh {
   }
 };
 
-// The joins of several products in one launch (grid x: their tiles one after another).
-struct JoinJobs {
-  JoinShape a[3];
-  EpiStore op[3];
-};
-__global__ __launch_bounds__(256) void ffn_join_jobs_kernel(JoinJobs j) {
-  int index = blockIdx.x, job = 0;
-  while (index >= j.a[job].g.count) index -= j.a[job++].g.count;   // the counts add up to the grid
-  join_tile(j.a[job], j.op[job], index, blockIdx.y);
-}
 // One product with its epilogue.
 template <bool kOuterA, bool kOuterB, class Op>
 int product(const RowShape& g, int64_t M, int64_t N, const Op& op, float* slab, const char* name, hipStream_t stream) {
   if (M == 0 || N == 0) return PSPO_OK;
   return product<kOuterA, kOuterB>(g, plan_of(M, N, (g.K + kRowK - 1) / kRowK, std::is_same_v<Op, EpiDh>), N, op, slab,
                                    name, stream);
-}
-
-int run_jobs(const JobPlan& p, const RowShape (&g)[3], const EpiStore (&o)[3], unsigned char* slabs,
-             hipStream_t stream) {
-  RowJobs<Epi<EpiStore>> jobs{};
-  int64_t blocks = 0;
-  for (int i = 0; i < 3; ++i) {
-    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
-    PSPO_REQUIRE(tiles < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
-    RowShape& r = jobs.g[i];
-    r = g[i];
-    r.tiles_m = p.tiles_m[i];
-    r.tiles_n = p.tiles_n[i];
-    r.tile0 = 0;
-    r.count = (int)tiles;
-    r.parts = p.parts[i];
-    jobs.blocks[i] = (int)(round_up(tiles, kNumXcd) * p.parts[i]);
-    blocks += jobs.blocks[i];
-    jobs.epi[i] = {o[i], {p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
-  }
-  PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
-  if (p.tile == 256)
-    hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
-  else if (deep_ring(blocks))
-    hipLaunchKernelGGL((row_jobs_kernel<4, 4, kDeep, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
-  else
-    hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, Epi<EpiStore>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
-  PSPO_LAUNCHED("ffn_gradients", stream);
-  JoinJobs join{};
-  int split = 0;
-  int64_t tiles = 0;
-  for (int i = 0; i < 3; ++i)
-    if (p.parts[i] > 1 && jobs.g[i].count > 0) {
-      join.a[split] = JoinShape{reinterpret_cast<float*>(slabs + p.slab[i]), jobs.g[i], p.tile, p.tile};
-      join.op[split++] = o[i];
-      tiles += jobs.g[i].count;
-    }
-  if (split > 0) {
-    hipLaunchKernelGGL(ffn_join_jobs_kernel, dim3((uint32_t)tiles, (uint32_t)join_blocks(p.tile, p.tile)), dim3(256), 0,
-                       stream, join);
-    PSPO_LAUNCHED("ffn_join_jobs_kernel", stream);
-  }
-  return PSPO_OK;
 }
 
 struct SkinnyGateUp {
@@ -300,7 +247,7 @@ int pspo_gated_ffn_bwd(const uint16_t* dy, const uint16_t* x, const uint16_t* w_
   const EpiStore o[3] = {{dx, dx, d, d, N, N, 0, 0},
                          {dw_gate, dw_up, d, d, 2 * f, f, f32, add},
                          {dw_down, dw_down, f, f, d, d, f32, add}};
-  return run_jobs(plan_backward(N, d, f), g, o, reinterpret_cast<unsigned char*>(slab), stream);
+  return run_jobs(plan_backward(N, d, f), g, o, reinterpret_cast<unsigned char*>(slab), "ffn_gradients", stream);
 }
 
 }  // extern "C"

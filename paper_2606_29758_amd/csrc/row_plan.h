@@ -70,6 +70,47 @@ inline Plan plan_of(int64_t M, int64_t N, int nk, bool dh) {
 constexpr int kDeep = 4;
 inline bool deep_ring(int64_t groups) { return groups <= 256; }
 
+// Up to three products as one launch.  All tiles of a size; a product whose tiles have more K
+// stages than a work-group's share of the whole is split along K.
+struct JobPlan {
+  int tile;
+  int tiles_m[3], tiles_n[3], parts[3];
+  int64_t slab[3], slab_bytes;   // bytes from the slabs' start; all of them
+  double us;
+};
+inline JobPlan plan_jobs(const int64_t (&M)[3], const int64_t (&N)[3], const int (&nk)[3], int tile) {
+  JobPlan p{};
+  p.tile = tile;
+  const int64_t slots = tile == 256 ? 256 : 512, bytes = (int64_t)tile * tile * 4;
+  int64_t units = 0, groups = 0;
+  for (int i = 0; i < 3; ++i) {
+    p.tiles_m[i] = (int)((M[i] + tile - 1) / tile);
+    p.tiles_n[i] = (int)((N[i] + tile - 1) / tile);
+    units += (int64_t)p.tiles_m[i] * p.tiles_n[i] * nk[i];
+  }
+  const int64_t share = std::max<int64_t>(units / slots, 4);
+  int longest = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
+    int64_t s = std::min<int64_t>((nk[i] + share - 1) / share, 32);
+    s = std::max<int64_t>(std::min<int64_t>(s, tiles ? kSlabBytes / 3 / (tiles * bytes) : 1), 1);
+    p.parts[i] = (int)s;
+    p.slab[i] = p.slab_bytes;
+    if (s > 1) p.slab_bytes += tiles * s * bytes;
+    groups += tiles * s;
+    if (tiles) longest = std::max(longest, (int)((nk[i] + s - 1) / s));
+  }
+  // A round's stages, half of the longest part idle at the end, the slabs out and in.  A stage of
+  // the small tiles takes 0.85 us here (stages of different products meet on a CU; with 1.1 as for
+  // one product, 777 tokens, d = 1000, f = 4104 would take the large tiles: 72 us with its join
+  // against 61; 300 tokens, d = 2048, f = 8192: 116 against 98).
+  const bool alone = tile == 128 && groups <= 256;
+  const double stage = tile == 256 ? 1.45 : alone ? 0.7 : 0.85;
+  const double rounds = (double)groups / (double)slots;
+  p.us = std::max((double)units / (double)slots + longest * 0.5, (double)longest) * stage +
+         std::max(rounds, 1.0) * (tile == 256 ? 10 : 5) + (double)p.slab_bytes * 2 / 4.5e6 + (p.slab_bytes ? 8 : 0);
+  return p;
+}
 // Most that the parts of any N' <= N take: the plans' own need goes up and down with N (a last
 // round of few tiles is cut finer than one of many), and a workspace asked for N has to serve
 // fewer tokens too.  Tiles of 128 x 64 take no more than the 128 x 128 ones stand for here; up to
@@ -84,6 +125,23 @@ inline int64_t slab_reserve(int64_t M, int64_t N, int K) {
     bytes = std::max(bytes, std::min(tiles, slots) * most * tile * tile * 4);
   }
   return std::min(bytes, kSlabBytes);
+}
+
+// The same of the parts of plan_jobs (M: 0 rows where a product is left out).
+inline int64_t jobs_reserve(const int64_t (&M)[3], const int64_t (&N)[3], const int64_t (&nk)[3]) {
+  int64_t bytes = 0;
+  for (const int64_t tile : {128, 256}) {
+    int64_t sum = 0;
+    for (int i = 0; i < 3; ++i) {
+      const int64_t most = std::min<int64_t>((nk[i] + 3) / 4, 32);   // plan_jobs: a share is 4 stages at least
+      // a product of as many tiles as there are slots has more stages in its share than a tile holds
+      const int64_t tiles = std::min<int64_t>(((M[i] + tile - 1) / tile) * ((N[i] + tile - 1) / tile),
+                                              tile == 256 ? 256 : 512);
+      if (most >= 2) sum += std::min(tiles * most * tile * tile * 4, kSlabBytes / 3);
+    }
+    bytes = std::max(bytes, sum);
+  }
+  return bytes;
 }
 
 }  // namespace pspo

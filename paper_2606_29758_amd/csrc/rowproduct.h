@@ -150,6 +150,18 @@ template <class Op>
 __global__ __launch_bounds__(256) void row_join_kernel(JoinShape a, Op op) {
   join_tile(a, op, blockIdx.x, blockIdx.y);
 }
+// The joins of several products in one launch (grid x: their tiles one after another).
+template <class Op>
+struct JoinJobs {
+  JoinShape a[3];
+  Op op[3];
+};
+template <class Op>
+__global__ __launch_bounds__(256) void row_join_jobs_kernel(JoinJobs<Op> j) {
+  int index = blockIdx.x, job = 0;
+  while (index >= j.a[job].g.count) index -= j.a[job++].g.count;   // the counts add up to the grid
+  join_tile(j.a[job], j.op[job], index, blockIdx.y);
+}
 template <class Op>
 int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const float* slab, hipStream_t stream) {
   hipLaunchKernelGGL((row_join_kernel<Op>),
@@ -198,6 +210,51 @@ int product(RowShape g, const Plan& p, int64_t N, const Op& op, float* slab, con
   g.parts = p.parts;
   if (int rc = launch<kOuterA, kOuterB>(g, p, Epi<Op>{op, {slab, (int)N}}, name, stream)) return rc;
   return join_parts(op, g, p.tile, p.tile_n, slab, stream);
+}
+
+// Up to three products in one launch and their joins in another.
+template <class Op>
+int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Op (&o)[3], unsigned char* slabs, const char* name,
+             hipStream_t stream) {
+  RowJobs<Epi<Op>> jobs{};
+  int64_t blocks = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t tiles = (int64_t)p.tiles_m[i] * p.tiles_n[i];
+    PSPO_REQUIRE(tiles < (int64_t(1) << 23), PSPO_ERR_UNSUPPORTED, "the product has more tiles than a launch holds");
+    RowShape& r = jobs.g[i];
+    r = g[i];
+    r.tiles_m = p.tiles_m[i];
+    r.tiles_n = p.tiles_n[i];
+    r.tile0 = 0;
+    r.count = (int)tiles;
+    r.parts = p.parts[i];
+    jobs.blocks[i] = (int)(round_up(tiles, kNumXcd) * p.parts[i]);
+    blocks += jobs.blocks[i];
+    jobs.epi[i] = {o[i], {p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
+  }
+  PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
+  if (p.tile == 256)
+    hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  else if (deep_ring(blocks))
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, kDeep, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  else
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  PSPO_LAUNCHED(name, stream);
+  JoinJobs<Op> join{};
+  int split = 0;
+  int64_t tiles = 0;
+  for (int i = 0; i < 3; ++i)
+    if (p.parts[i] > 1 && jobs.g[i].count > 0) {
+      join.a[split] = JoinShape{reinterpret_cast<float*>(slabs + p.slab[i]), jobs.g[i], p.tile, p.tile};
+      join.op[split++] = o[i];
+      tiles += jobs.g[i].count;
+    }
+  if (split > 0) {
+    hipLaunchKernelGGL(row_join_jobs_kernel<Op>, dim3((uint32_t)tiles, (uint32_t)join_blocks(p.tile, p.tile)), dim3(256), 0,
+                       stream, join);
+    PSPO_LAUNCHED("row_join_jobs_kernel", stream);
+  }
+  return PSPO_OK;
 }
 
 RowShape shape(const uint16_t* a, const uint16_t* a2, int64_t lda, int rows_a, const uint16_t* b, int64_t ldb, int rows_b,
