@@ -55,6 +55,12 @@ __device__ __forceinline__ float sum_of_8_lanes(float x) {
   return x + lane_move(x, 2);
 }
 
+// Sum over the four lanes l % 16, the same in all of them.
+__device__ __forceinline__ float across_rows(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
 // ---- forward product ---------------------------------------------------------------
 // 2^(z t - c) with t = log2(e) / temperature in two parts: rounded to float32 alone, t would move
 // every exponent of a row by up to 2^-24 of it the same way, 1e-6 of the sum.
@@ -69,7 +75,7 @@ constexpr float kFar = 4294967296.f;   // largest sum of a group in its row's re
 // Eight logits (vocabulary entries m .. m + 7 of row n); the 8 lanes of a group of 64 entries
 // hold it together, in a tile's epilogue and in a join alike.
 struct EpiSoftmax {
-  static constexpr bool kPair = false;
+  static constexpr bool kPair = false, kTile = true;
   uint16_t* e;       // [N][ld]
   f32x2* part;       // [N][ld / 64]: reference, sum
   const float* c;    // [N]
@@ -105,6 +111,59 @@ struct EpiSoftmax {
     if (n >= N || m >= ld) return;
     put_bf16(e + n * ld + m, x);
     if (m % kGroup == 0) part[n * (ld / kGroup) + m / kGroup] = f32x2{ref, sum};
+  }
+  // A wave's accumulators, a group of 64 entries of 16 rows at a time (four row blocks of a column
+  // block: a lane holds 16 values of one row), without the LDS.
+  template <int BM, int BN>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane) const {
+    const int64_t n0 = (int64_t)(tn * 2 + wn) * BN * 16 + (lane & 15);
+    const int m0 = (tm * 2 + wm) * BM * 16, g4 = (lane >> 4) * 4;
+    float ref[BN];
+    repeat<BN>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+      ref[j] = n0 + j * 16 < N ? c[n0 + j * 16] : 0.f;
+    });
+    repeat<BN>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+      const int64_t n = n0 + j * 16;
+      repeat<BM / 4>([&](auto gc) {
+        constexpr int i0 = decltype(gc)::value * 4;
+        const int m = m0 + i0 * 16;
+        float x[16];
+        auto values = [&](float from) {   // and the sum over the group
+          float sum[4] = {};
+#pragma unroll
+          for (int q = 0; q < 16; ++q) x[q] = exponent(acc_read(acc[i0 + q / 4][j][q % 4]), from);
+          if (m + kGroup > V) {   // the same in all lanes
+#pragma unroll
+            for (int q = 0; q < 16; ++q) x[q] = m + q / 4 * 16 + g4 + q % 4 < V ? x[q] : 0.f;
+          }
+#pragma unroll
+          for (int q = 0; q < 16; ++q) sum[q % 4] += x[q];
+          return across_rows((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        };
+        float from = ref[j], sum = values(from);
+        if (__any(sum > kFar)) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            top = fmaxf(top, m + q / 4 * 16 + g4 + q % 4 < V ? acc_read(acc[i0 + q / 4][j][q % 4]) : -INFINITY);
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          if (sum > kFar) from = rintf(top * exponent.t);
+          sum = values(from);
+        }
+        const bool on = n < N && m < ld;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float* v = x + h * 8;
+          const u32x4 o = eight_rows(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])},
+                                     u32x2{pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
+          if (on) *reinterpret_cast<u32x4*>(e + n * ld + m + h * 32 + eight_rows_at(lane)) = o;
+        }
+        if (on && lane < 16) part[n * (ld / kGroup) + m / kGroup] = f32x2{from, sum};
+      });
+    });
   }
 };
 
@@ -324,17 +383,48 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   if (Op::kFactor) scale_copy(r, i, factor);
 }
 
-// Sums over n terms each of up to four kinds ([kinds][n]), in a fixed order; one work-group of 256.
-template <int kKinds>
-__device__ __forceinline__ void sum_terms(const double* terms, int64_t n, double (&out)[kKinds], double* sh) {
-#pragma unroll
-  for (int q = 0; q < kKinds; ++q) out[q] = 0.0;
+// The loss from the rows' terms, in a fixed order: terms [kinds][n], loss = times[0] sum 0 + times[1]
+// sum 1, stats the sums.  One work-group, of any size; it goes along with the launch of the gradients.
+struct LossSum {
+  const double* terms;
+  int64_t n;
+  int kinds;             // 1 or 4
+  float times[2];
+  double *loss, *stats;  // loss NULL: nothing to do
+
+  template <int kKinds>
+  __device__ __forceinline__ void sum(double (&out)[4], double* sh) const {
+    double x[kKinds] = {};
 #pragma unroll 4
-  for (int64_t i = threadIdx.x; i < n; i += 256)
+    for (int64_t i = threadIdx.x; i < n; i += blockDim.x)
 #pragma unroll
-    for (int q = 0; q < kKinds; ++q) out[q] += terms[q * n + i];
+      for (int q = 0; q < kKinds; ++q) x[q] += terms[q * n + i];
 #pragma unroll
-  for (int q = 0; q < kKinds; ++q) out[q] = block_total(out[q], sh);
+    for (int q = 0; q < kKinds; ++q) {
+      x[q] = wave_sum(x[q]);
+      if (threadIdx.x % 64 == 0) sh[q * 16 + threadIdx.x / 64] = x[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kKinds; ++q) {
+      out[q] = 0.0;
+      for (unsigned w = 0; w < blockDim.x / 64; ++w) out[q] += sh[q * 16 + w];
+    }
+  }
+  __device__ __forceinline__ void run(double* sh) const {   // 64 doubles of LDS
+    if (loss == nullptr) return;
+    double s[4] = {};
+    if (kinds == 4) sum<4>(s, sh);
+    else sum<1>(s, sh);
+    if (threadIdx.x != 0) return;
+    *loss = times[1] != 0.f ? (double)times[0] * s[0] + (double)times[1] * s[1] : (double)times[0] * s[0];
+    if (stats != nullptr)
+      for (int q = 0; q < 4; ++q) stats[q] = s[q];
+  }
+};
+__global__ __launch_bounds__(1024) void loss_sum_kernel(LossSum s) {
+  __shared__ double sh[64];
+  s.run(sh);
 }
 
 // ---- policy loss ---------------------------------------------------------------------------
@@ -401,17 +491,6 @@ struct Policy {
   }
 };
 
-__global__ __launch_bounds__(256) void policy_loss_kernel(const double* __restrict__ terms, int64_t n, float kl_coef,
-                                                          double* __restrict__ loss, double* __restrict__ stats) {
-  __shared__ double sh[4];
-  double s[4];
-  sum_terms<4>(terms, n, s, sh);
-  if (threadIdx.x != 0) return;
-  *loss = kl_coef != 0.f ? (double)kl_coef * s[1] - s[0] : -s[0];
-  if (stats != nullptr)
-    for (int q = 0; q < 4; ++q) stats[q] = s[q];
-}
-
 // ---- preference loss ------------------------------------------------------------------------
 struct Preference {
   static constexpr bool kFactor = false;   // pref_rows_kernel does
@@ -462,7 +541,17 @@ __device__ __forceinline__ bool sequence_rows(const Pairs& q, int r, int N, int&
   return a >= 0 && b >= a && b <= N;
 }
 
-// A work-group per sequence: its log ratio and the factor that its rows' terms enter it with.
+// Its log ratio and the factor that its rows' terms enter it with, from their sum and their weights'.
+__device__ __forceinline__ void sequence_ratio(const Pairs& q, int r, double part, double c, bool write) {
+  if (!write) return;
+  const double norm = q.average ? (c != 0.0 ? 1.0 / c : 0.0) : 1.0;
+  const double ratio = norm != 0.0 ? part * norm : 0.0;
+  q.norm[r] = norm;
+  q.ratio[r] = ratio;
+  if (q.seq_ratio != nullptr) q.seq_ratio[r] = (float)ratio;
+}
+
+// A work-group per sequence.
 __global__ __launch_bounds__(256) void pref_sequences_kernel(Pairs q, int N, const double* __restrict__ terms) {
   __shared__ double sh[4];
   const int r = blockIdx.x;
@@ -476,18 +565,11 @@ __global__ __launch_bounds__(256) void pref_sequences_kernel(Pairs q, int N, con
   }
   part = block_total(part, sh);
   c = block_total(c, sh);
-  if (threadIdx.x != 0) return;
-  const double norm = q.average ? (c != 0.0 ? 1.0 / c : 0.0) : 1.0;
-  const double ratio = norm != 0.0 ? part * norm : 0.0;
-  q.norm[r] = norm;
-  q.ratio[r] = ratio;
-  if (q.seq_ratio != nullptr) q.seq_ratio[r] = (float)ratio;
+  sequence_ratio(q, r, part, c, threadIdx.x == 0);
 }
 
-// d loss / d u of each pair, and its part of the loss.
-__global__ __launch_bounds__(256) void pref_pairs_kernel(Pairs q) {
-  const int p = blockIdx.x * 256 + threadIdx.x;
-  if (p >= q.P) return;
+// d loss / d u of a pair, and its part of the loss.
+__device__ __forceinline__ void pair_terms(const Pairs& q, int p) {
   const int a = q.chosen[p], b = q.rejected[p];
   double loss = 0.0, du = 0.0, m = NAN;
   if (a >= 0 && a < q.R && b >= 0 && b < q.R) {
@@ -513,26 +595,70 @@ __global__ __launch_bounds__(256) void pref_pairs_kernel(Pairs q) {
   q.pair_loss[p] = loss * (double)q.scale;
   if (q.margin != nullptr) q.margin[p] = (float)m;
 }
+__global__ __launch_bounds__(256) void pref_pairs_kernel(Pairs q) {
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p < q.P) pair_terms(q, p);
+}
+
+// What pair p gives sequence r.
+__device__ __forceinline__ double pair_part(const Pairs& q, int r, int p) {
+  const int a = q.chosen[p], b = q.rejected[p];
+  if (a == b || (a != r && b != r) || a < 0 || a >= q.R || b < 0 || b >= q.R) return 0.0;
+  return a == r ? q.pair[p] : -q.pair[p];
+}
 
 // A work-group per sequence: what its pairs give it, in the pairs' order within each thread's share.
 // The last one sums the loss.
 __global__ __launch_bounds__(256) void pref_coef_kernel(Pairs q, double* __restrict__ loss) {
-  __shared__ double sh[4];
+  __shared__ double sh[4], sum[64];
   const int r = blockIdx.x;
   if (r == q.R) {
-    double s[1];
-    sum_terms<1>(q.pair_loss, q.P, s, sh);
-    if (threadIdx.x == 0) *loss = s[0];
+    LossSum{q.pair_loss, q.P, 1, {1.f, 0.f}, loss, nullptr}.run(sum);
     return;
   }
   double c = 0.0;
-  for (int p = threadIdx.x; p < q.P; p += 256) {
-    const int a = q.chosen[p], b = q.rejected[p];
-    if ((a != r && b != r) || a < 0 || a >= q.R || b < 0 || b >= q.R) continue;
-    c += a == r ? (b == r ? 0.0 : q.pair[p]) : -q.pair[p];
-  }
+  for (int p = threadIdx.x; p < q.P; p += 256) c += pair_part(q, r, p);
   c = block_total(c, sh);
   if (threadIdx.x == 0) q.coef[r] = q.norm[r] != 0.0 ? c * q.norm[r] : 0.0;
+}
+
+// All three of the above for a few thousand rows and few pairs, in one work-group: a wave per
+// sequence in turn (8 completions of 257 rows, 4 pairs: two launches less, 8 us a call).
+constexpr int kPrefWaves = 16;
+constexpr int64_t kPrefRows = 16384, kPrefLooks = 1 << 18;   // rows; sequences times pairs
+__global__ __launch_bounds__(64 * kPrefWaves) void pref_all_kernel(Pairs q, int N, const double* __restrict__ terms,
+                                                                   double* __restrict__ loss) {
+  __shared__ double sh[kPrefWaves];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  for (int r = wave; r < q.R; r += kPrefWaves) {
+    int lo, hi;
+    if (!sequence_rows(q, r, N, lo, hi) && lane == 0) raise(q.err, PSPO_DEVERR_SEQ_ID);
+    double part = 0.0, c = 0.0;
+#pragma unroll 4
+    for (int i = lo + lane; i < hi; i += 64) {
+      part += terms[(int64_t)N + i];
+      c += terms[2 * (int64_t)N + i];
+    }
+    sequence_ratio(q, r, wave_sum(part), wave_sum(c), lane == 0);
+  }
+  __syncthreads();
+  for (int p = threadIdx.x; p < q.P; p += 64 * kPrefWaves) pair_terms(q, p);
+  __syncthreads();
+  for (int r = wave; r < q.R; r += kPrefWaves) {
+    double c = 0.0;
+    for (int p = lane; p < q.P; p += 64) c += pair_part(q, r, p);
+    c = wave_sum(c);
+    if (lane == 0) q.coef[r] = q.norm[r] != 0.0 ? c * q.norm[r] : 0.0;
+  }
+  double x = 0.0;
+  for (int p = threadIdx.x; p < q.P; p += 64 * kPrefWaves) x += q.pair_loss[p];
+  x = wave_sum(x);
+  if (lane == 0) sh[wave] = x;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  x = 0.0;
+  for (int k = 0; k < kPrefWaves; ++k) x += sh[k];
+  *loss = x;
 }
 
 // The row's factor, from its sequence's; a work-group per row.
@@ -627,14 +753,6 @@ struct Distill {
   }
 };
 
-__global__ __launch_bounds__(256) void distill_loss_kernel(const double* __restrict__ terms, int64_t n,
-                                                           double* __restrict__ loss) {
-  __shared__ double sh[4];
-  double s[1];
-  sum_terms<1>(terms, n, s, sh);
-  if (threadIdx.x == 0) *loss = s[0];
-}
-
 // ---- E of few rows ---------------------------------------------------------------------------
 // From the float32 logits, relative to the row's sum, eight entries a thread; zeros where the factor
 // is 0.  Grid (N, ceil(ld / 2048)).
@@ -661,24 +779,79 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
   }
 }
 
-// C(m, n) = sum over the vocabulary of W(v, m) E(n, v): d_hidden[n][m] = f[n] C.
-struct EpiHidden {
-  static constexpr bool kPair = false;
+// Both gradients: out[n][m] = f[n] C(m, n), or C alone (f NULL), bf16 or float32 (or added to it).
+struct EpiGrad {
+  static constexpr bool kPair = false, kTile = true;
+  static constexpr bool kExtra = true;
   void* out;
   const float* f;
   int64_t ld;
-  int M, N, f32;
+  int M, N, f32, add;
+  LossSum loss;
+  __device__ __forceinline__ void extra(unsigned char* lds) const { loss.run(reinterpret_cast<double*>(lds)); }
   struct Fetched {
     float f;
   };
-  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t) const { return {n < N ? f[n] : 0.f}; }
+  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t) const { return {f != nullptr && n < N ? f[n] : 1.f}; }
   __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, const Fetched& x) const {
     if (n >= N || m >= M) return;   // M % 8 == 0
     f32x4 s[2];
 #pragma unroll
     for (int k = 0; k < 8; ++k) s[k / 4][k % 4] = x.f == 0.f ? 0.f : x.f * v[k / 4][k % 4];   // a row left out is zeros
-    if (f32) put_f32(static_cast<float*>(out) + n * ld + m, s);
-    else put_bf16(static_cast<uint16_t*>(out) + n * ld + m, reinterpret_cast<const float*>(s));
+    if (f32) {
+      float* to = static_cast<float*>(out) + n * ld + m;
+      if (add) {
+        s[0] += reinterpret_cast<const f32x4*>(to)[0];
+        s[1] += reinterpret_cast<const f32x4*>(to)[1];
+      }
+      put_f32(to, s);
+    } else {
+      put_bf16(static_cast<uint16_t*>(out) + n * ld + m, reinterpret_cast<const float*>(s));
+    }
+  }
+  // The accumulators as they lie: a lane has four consecutive entries of a row, 16 bytes of float32,
+  // or eight after a swap with the next row block, 16 bytes of bf16.
+  template <int BM, int BN>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane) const {
+    const int64_t n0 = (int64_t)(tn * 2 + wn) * BN * 16 + (lane & 15);
+    const int64_t m0 = (int64_t)(tm * 2 + wm) * BM * 16;
+    repeat<BN>([&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+      const int64_t n = n0 + j * 16;
+      const float x = fetch(n, 0).f;
+      auto value = [&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc_read(acc[i][j][r]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = x == 0.f ? 0.f : x * v[r];
+        return v;
+      };
+      if (f32) {
+        float* to = static_cast<float*>(out) + n * ld + m0 + (lane >> 4) * 4;
+        f32x4 old[BM] = {};
+        if (add) {
+#pragma unroll
+          for (int i = 0; i < BM; ++i)
+            if (n < N && m0 + i * 16 + (lane >> 4) * 4 < M) old[i] = *reinterpret_cast<const f32x4*>(to + i * 16);
+        }
+        repeat<BM>([&](auto ic) {
+          constexpr int i = decltype(ic)::value;
+          const f32x4 v = value(ic);
+          if (n < N && m0 + i * 16 + (lane >> 4) * 4 < M) *reinterpret_cast<f32x4*>(to + i * 16) = old[i] + v;
+        });
+      } else {
+        uint16_t* to = static_cast<uint16_t*>(out) + n * ld + m0 + eight_rows_at(lane);
+        repeat<BM / 2>([&](auto ic) {
+          constexpr int i = decltype(ic)::value * 2;
+          const f32x4 a = value(std::integral_constant<int, i>{}), b = value(std::integral_constant<int, i + 1>{});
+          const u32x4 o = eight_rows(u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])},
+                                     u32x2{pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])});
+          if (n < N && m0 + i * 16 + eight_rows_at(lane) < M) *reinterpret_cast<u32x4*>(to + i * 16) = o;
+        });
+      }
+    });
   }
 };
 
@@ -722,7 +895,10 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   s.z = take(few ? N * s.ld * 4 : 0);
   s.e = take(few && !grads ? 0 : N * s.ld * 2);
   int64_t slab = slab_reserve(V, N, (int)d);
-  if (grads) slab = std::max({slab, slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
+  if (grads) {
+    const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0}, nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
+    slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
+  }
   s.slab = take(slab);
   s.seqs = take(R * 3 * 8);
   s.pairs = take(P * 2 * 8);
@@ -740,10 +916,19 @@ size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int
                           layout_of(std::min<int64_t>(N, kSkinnyTokens), d, V, k, R, P, grads).total);
 }
 
-// Tiles of both operands K-outer, or of A: 256 or 128 square.
+// One gradient product, in 256 or 128 square tiles.
 Plan plan_square(int64_t M, int64_t N, int K) {
   const int nk = (K + kRowK - 1) / kRowK;
   const Plan small = plan_tile(M, N, nk, 128, 128, false), big = plan_tile(M, N, nk, 256, 256, false);
+  return big.us <= small.us ? big : small;
+}
+// Both as one launch (against two, us a call: 1 row, d = 1536, V = 151936 411 / 472; 1,301, 1000, 50257 492 /
+// 528; 4,096, 3584, 152064 10,602 / 10,818; 4,999 of the same 13,024 / 12,871).  One alone goes as a product,
+// whose last round is split along K (8,192 rows, d = 3584: 13,536 against 14,105).
+JobPlan plan_gradients(int64_t N, int64_t d, int64_t V) {
+  const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0};
+  const int nk[3] = {(int)((V + kRowK - 1) / kRowK), (int)((N + kRowK - 1) / kRowK), 0};
+  const JobPlan big = plan_jobs(M, C, nk, 256), small = plan_jobs(M, C, nk, 128);
   return big.us <= small.us ? big : small;
 }
 
@@ -852,7 +1037,12 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
 }
 
 // Step 4.
-int backward(const Call& c, const Layout& s, const Rows& r) {
+int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss) {
+  const bool both = c.dh != nullptr && c.dw != nullptr;
+  if (loss.loss != nullptr && (c.N == 0 || !both)) {   // otherwise it goes along below
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, c.stream, loss);
+    PSPO_LAUNCHED("loss_sum_kernel", c.stream);
+  }
   if (!c.grads()) return PSPO_OK;
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
@@ -869,18 +1059,16 @@ int backward(const Call& c, const Layout& s, const Rows& r) {
                        c.stream, r, (const float*)z, exponent_of(r));
     PSPO_LAUNCHED("few_entries_kernel", c.stream);
   }
-  if (c.dh != nullptr) {
-    const EpiHidden o{c.dh, r.f, c.d, c.d, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0};
-    if (int rc = product<true, false>(shape(c.w, c.w, c.d, c.d, r.e, s.ld, c.N, c.V), plan_square(c.d, c.N, c.V), c.N,
-                                      o, slab, "objective_dh", c.stream))
-      return rc;
-  }
-  if (c.dw != nullptr) {
-    const EpiStore o{c.dw, c.dw, c.d, c.d, c.V, c.V, f32, add};
-    return product<true, true>(shape(r.copy, r.copy, c.d, c.d, r.e, s.ld, c.V, c.N), plan_square(c.d, c.V, c.N), c.V, o,
-                               slab, "objective_dw", c.stream);
-  }
-  return PSPO_OK;
+  const RowShape g[3] = {shape(c.w, c.w, c.d, c.d, r.e, s.ld, c.N, c.V),
+                         shape(r.copy, r.copy, c.d, c.d, r.e, s.ld, c.V, c.N), RowShape{}};
+  const EpiGrad o[3] = {{c.dh, r.f, c.d, c.d, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0, 0, loss},
+                        {c.dw, nullptr, c.d, c.d, c.V, f32, add, LossSum{}}, EpiGrad{}};
+  if (both)
+    return run_jobs(plan_gradients(c.N, c.d, c.V), g, o, reinterpret_cast<unsigned char*>(slab), "objective_gradients",
+                    c.stream);
+  if (c.dh != nullptr)
+    return product<true, false>(g[0], plan_square(c.d, c.N, c.V), c.N, o[0], slab, "objective_dh", c.stream);
+  return product<true, true>(g[1], plan_square(c.d, c.V, c.N), c.V, o[1], slab, "objective_dw", c.stream);
 }
 
 }  // namespace
@@ -936,9 +1124,7 @@ int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, con
                          Policy{target, logp_old, logp_ref, weight, seq_id, advantage, R, eps_low, eps_high, kl_coef,
                                 loss_scale, kl_kind, logp_new}))
       return rc;
-  hipLaunchKernelGGL(policy_loss_kernel, dim3(1), dim3(256), 0, stream, r.terms, (int64_t)N, kl_coef, loss, stats);
-  PSPO_LAUNCHED("policy_loss_kernel", stream);
-  return backward(c, s, r);
+  return backward(c, s, r, LossSum{r.terms, N, 4, {-1.f, kl_coef}, loss, stats});
 }
 
 int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
@@ -978,21 +1164,26 @@ int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, cons
                 seqs, seqs + R, seqs + 2 * (int64_t)R, pairs, pairs + P, seq_ratio, margin, err_flag};
   if (N > 0)
     if (int rc = forward(c, s, r, Preference{target, logp_ref, weight, logp_new})) return rc;
-  if (R > 0) {
-    hipLaunchKernelGGL(pref_sequences_kernel, dim3((unsigned)R), dim3(256), 0, stream, q, N, (const double*)r.terms);
-    PSPO_LAUNCHED("pref_sequences_kernel", stream);
+  if (N <= kPrefRows && (int64_t)R * P <= kPrefLooks) {
+    hipLaunchKernelGGL(pref_all_kernel, dim3(1), dim3(64 * kPrefWaves), 0, stream, q, N, (const double*)r.terms, loss);
+    PSPO_LAUNCHED("pref_all_kernel", stream);
+  } else {
+    if (R > 0) {
+      hipLaunchKernelGGL(pref_sequences_kernel, dim3((unsigned)R), dim3(256), 0, stream, q, N, (const double*)r.terms);
+      PSPO_LAUNCHED("pref_sequences_kernel", stream);
+    }
+    if (P > 0) {
+      hipLaunchKernelGGL(pref_pairs_kernel, dim3((unsigned)(((int64_t)P + 255) / 256)), dim3(256), 0, stream, q);
+      PSPO_LAUNCHED("pref_pairs_kernel", stream);
+    }
+    hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)R + 1), dim3(256), 0, stream, q, loss);
+    PSPO_LAUNCHED("pref_coef_kernel", stream);
   }
-  if (P > 0) {
-    hipLaunchKernelGGL(pref_pairs_kernel, dim3((unsigned)(((int64_t)P + 255) / 256)), dim3(256), 0, stream, q);
-    PSPO_LAUNCHED("pref_pairs_kernel", stream);
-  }
-  hipLaunchKernelGGL(pref_coef_kernel, dim3((unsigned)R + 1), dim3(256), 0, stream, q, loss);
-  PSPO_LAUNCHED("pref_coef_kernel", stream);
   if (N > 0 && c.grads()) {
     hipLaunchKernelGGL(pref_rows_kernel, dim3((unsigned)N), dim3(256), 0, stream, r, q);
     PSPO_LAUNCHED("pref_rows_kernel", stream);
   }
-  return backward(c, s, r);
+  return backward(c, s, r, LossSum{});
 }
 
 int pspo_distill_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* topk_ids,
@@ -1016,9 +1207,7 @@ int pspo_distill_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const i
   const Rows r = rows_of(c, s);
   if (N > 0)
     if (int rc = forward(c, s, r, Distill{topk_ids, topk_logit, weight, loss_scale, kl})) return rc;
-  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(256), 0, stream, (const double*)r.terms, (int64_t)N, loss);
-  PSPO_LAUNCHED("distill_loss_kernel", stream);
-  return backward(c, s, r);
+  return backward(c, s, r, LossSum{r.terms, N, 1, {1.f, 0.f}, loss, nullptr});
 }
 
 }  // extern "C"

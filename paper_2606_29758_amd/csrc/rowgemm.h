@@ -349,7 +349,8 @@ void row_gemm_kernel(RowShape g, Epi epi) {
 // Independent products in one launch, the first with A K-outer and B K-inner, the others with
 // both K-outer: their work-groups fill the chip together, so that only the last tiles of all
 // leave part of it idle.  A job's work-groups: its parts one after another, the tiles of a
-// part rounded up to whole rounds of the XCDs.
+// part rounded up to whole rounds of the XCDs.  With Epi::kExtra one more work-group, the last,
+// calls epi[0].extra(lds): a small step that has to wait for the same launch.
 template <class Epi>
 struct RowJobs {
   static constexpr int kJobs = 3;
@@ -362,6 +363,12 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
 void row_jobs_kernel(RowJobs<Epi> jobs) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
   int bid = blockIdx.x;
+  if constexpr (Epi::kExtra) {
+    if (bid == (int)gridDim.x - 1) {
+      jobs.epi[0].extra(lds);
+      return;
+    }
+  }
   if (bid < jobs.blocks[0]) {
     const int per = (jobs.g[0].count + kNumXcd - 1) / kNumXcd * kNumXcd;
     row_gemm_tile<BM, BN, kRing, true, false, false>(jobs.g[0], jobs.epi[0], bid % per, bid / per, lds);

@@ -3,6 +3,8 @@
 // file that includes this.
 #pragma once
 
+#include <type_traits>
+
 #include "row_plan.h"
 #include "skinny.h"
 #include "vec8.h"
@@ -81,15 +83,40 @@ __device__ __forceinline__ int slab_piece(int tile, int m, int n) {
   return ((n >> 4) * (tile >> 4) + (m >> 4)) * 256 + (((m >> 2) & 3) * 16 + (n & 15)) * 4;
 }
 
-// The epilogue of a launch: slabs where the tiles are parts, else `op`.
+// The epilogue of a launch: slabs where the tiles are parts, else `op`, by its own way from the
+// accumulators (tile, kTile true) or piece by piece.
+template <class Op, class = void>
+struct HasTile : std::false_type {};
+template <class Op>
+struct HasTile<Op, std::enable_if_t<Op::kTile>> : std::true_type {};
+
+template <class Op, class = void>
+struct HasExtra : std::false_type {};
+template <class Op>
+struct HasExtra<Op, std::enable_if_t<Op::kExtra>> : std::true_type {};
+
+// Two row blocks of a column (packed bf16: rows 4 g .. 4 g + 3 of lane group g = lane / 16) to eight
+// consecutive rows a lane, from row 16 (g % 2) + 8 (g / 2) of the pair on.
+__device__ __forceinline__ u32x4 eight_rows(const u32x2& a, const u32x2& b) {
+  const auto x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+  return u32x4{x[0], y[0], x[1], y[1]};
+}
+__device__ __forceinline__ int eight_rows_at(int lane) { return ((lane >> 4) & 1) * 16 + (lane >> 5) * 8; }
+
 template <class Op>
 struct Epi {
+  static constexpr bool kExtra = HasExtra<Op>::value;
   Op op;
   Slab slab;
+  __device__ __forceinline__ void extra(unsigned char* lds) const {
+    if constexpr (kExtra) op.extra(lds);
+  }
   template <int BM, int BN>
   __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
                                         unsigned char* lds, int index) const {
     if (slab.base != nullptr) put_slab(acc, tn, wm, wn, lane, index, slab);
+    else if constexpr (HasTile<Op>::value) op.template tile<BM, BN>(acc, tm, tn, wm, wn, lane);
     else row_pieces<BM, BN, Op::kPair>(acc, tm, tn, wm, wn, lane, lds, op);
   }
 };
@@ -233,6 +260,7 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Op (&o)[3], unsigne
     jobs.epi[i] = {o[i], {p.parts[i] > 1 ? reinterpret_cast<float*>(slabs + p.slab[i]) : nullptr, o[i].N}};
   }
   PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
+  if (Epi<Op>::kExtra) ++blocks;
   if (p.tile == 256)
     hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
   else if (deep_ring(blocks))
