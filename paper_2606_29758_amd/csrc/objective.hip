@@ -32,8 +32,12 @@
 namespace pspo {
 namespace {
 
-constexpr int kGroup = 64;         // vocabulary entries of one (maximum, sum)
+constexpr int kGroup = 64;         // vocabulary entries of one (reference, sum)
 constexpr int kFewGroup = 2048;    // ... where the logits are kept in float32
+constexpr int kOnePassGroup = 16;  // ... in one pass over W
+// Ways of a call, by its size (way_of): tiles; up to 64 rows, the logits in float32 first; up to 16
+// rows, logits and d_hidden in one pass over W.
+enum { kTiles, kFew, kOnePass };
 constexpr int kMostIds = 64;
 
 // ---- lane exchanges within 8 lanes ------------------------------------------------
@@ -221,13 +225,17 @@ __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict
   if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{ref, sum};
 }
 
+constexpr int kRescaled = 2;   // of Rows::use
+
 // ---- what a call's kernels share ------------------------------------------------------
 struct Rows {
   int N, d, V, k;          // k ids a row
-  int few, grads;          // logits kept in float32; gradients wanted
+  int way, grads;          // kTiles, kFew or kOnePass; gradients wanted
   int64_t ld, groups;      // entries between softmax rows; groups of a row
+  int group;               // entries of a group
   double inv_t;
-  int32_t* use;            // 1: takes part, 0: left out, -1: left out for an invalid id
+  int32_t* use;            // 1: takes part (kRescaled: with E brought to another reference than it was
+                           // written in), 0: left out, -1: left out for an invalid id
   float* zs;               // [N][k] logits at the ids
   float* c;                // reference of the row
   f32x2* part;
@@ -255,6 +263,10 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
   const int i = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int use = op.use(i, lane, r);
   if (threadIdx.x == 0) r.use[i] = use;
+  if ((int)threadIdx.x < r.k) {   // (finalize writes what becomes of them)
+    const int64_t at = (int64_t)i * r.k + threadIdx.x;
+    r.ids[at] = use == 1 ? op.id(i, threadIdx.x, r) : -1;
+  }
   const u32x4* from = reinterpret_cast<const u32x4*>(hidden + (int64_t)i * r.d);
   u32x4* to = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
   const int pieces = r.d / 8;
@@ -337,6 +349,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
     float top = -INFINITY;
     double sum = 0.0;
     bool far = false;
+#pragma unroll 8
     for (int g = threadIdx.x; g < r.groups; g += 256) {
       const f32x2 p = part[g];
       sum += p.y;
@@ -350,9 +363,9 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
         const f32x2 p = part[g];
         if (p.x != -INFINITY || p.y != 0.f) sum += (double)p.y * (double)__builtin_amdgcn_exp2f(p.x - top);
       }
-      if (!r.few && r.grads)
-        for (int64_t v0 = threadIdx.x * 8; v0 < r.ld; v0 += 2048) {
-          const float down = __builtin_amdgcn_exp2f(part[v0 / kGroup].x - top);
+      if (r.way != kFew && r.grads)
+        for (int64_t v0 = threadIdx.x * 8; v0 < r.groups * r.group; v0 += 2048) {
+          const float down = __builtin_amdgcn_exp2f(part[v0 / r.group].x - top);
           u32x4 x = *reinterpret_cast<const u32x4*>(row + v0);
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -360,10 +373,11 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
           *reinterpret_cast<u32x4*>(row + v0) = x;
         }
       c = top;
+      if (threadIdx.x == 0) r.use[i] = kRescaled;
     }
     lse2 = (double)c + log2(block_total(sum, shd));
   }
-  if (r.few) c = (float)lse2;   // E is written from the logits, relative to the sum
+  if (r.way == kFew) c = (float)lse2;   // E is written from the logits, relative to the sum
   if (threadIdx.x < 64) {
     const float a = op.row(i, threadIdx.x, use, lse2 * 0.6931471805599453, r);
     if (threadIdx.x == 0) {
@@ -375,7 +389,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   }
   if (!r.grads) return;
   __syncthreads();   // also: the rescaled row, r.ids and r.g are written
-  if (!r.few && use == 1 && threadIdx.x < r.k) {
+  if (r.way != kFew && use == 1 && threadIdx.x < r.k) {
     const int64_t at = (int64_t)i * r.k + threadIdx.x;
     const int id = r.ids[at];
     if (id >= 0) row[id] = (uint16_t)pack_bf16((float)((double)r.g[at] * exp2(lse2 - (double)c)), 0.f);
@@ -670,7 +684,7 @@ __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
     if (q.cu[mid + 1] > i) e = mid;
     else s = mid + 1;
   }
-  const bool on = s < q.R && q.cu[s] <= i && r.use[i] == 1;
+  const bool on = s < q.R && q.cu[s] <= i && r.use[i] > 0;
   const double delta = on ? q.coef[s] * r.terms[2 * (int64_t)r.N + i] : 0.0;
   const float a = (float)(-delta * r.inv_t);
   const float f = on && a != 0.f ? a * (float)exp2((double)r.c[i] - r.lse2[i]) : 0.f;
@@ -779,6 +793,234 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
   }
 }
 
+// ---- up to 16 rows: one pass over W ------------------------------------------------------------
+// A work-group takes blocks of 16 vocabulary entries in turn; its 4 waves, one to a SIMD with all of
+// its registers (8 waves of half of them spilled from d = 2,560 on), split the hidden width, 32 F columns
+// each.  A wave's part of the block comes to registers (the next block's while this one is
+// worked on), goes from there into the matrix instructions of the logits and into its own LDS; the
+// waves' sums are exchanged, every wave forms the block's 16 x 16 softmax entries, and reads its part
+// again, transposed, for their product with it, which stays in its accumulators: W is read once for
+// the logits and d_hidden.  Entries at the rows' ids count in the sums but not in the product (they
+// are added at the end with what becomes of them).  The entries of a block that pass 2^32 take their own
+// reference, as in the tiles; their row's accumulators are then of no use (no other row's are touched),
+// and its d_hidden is formed from E (one_pass_hidden_kernel).
+// Bound by W's bytes: MEASURED_PASS.
+constexpr int kPassWaves = 4, kPassRows = 16, kPassBlocks = 256, kHeadWaves = 8;
+constexpr int kMostPassWidth = 28 * 32 * kPassWaves;   // what the registers of a work-group to a CU hold
+
+// Four rows (4 g .. 4 g + 3) of column 16 b + lane % 16 of a wave's rows of bf16 in LDS, `pitch` bytes
+// apart: the matrix instruction's operand with the rows as K.
+__device__ __forceinline__ s16x4 transposed(const unsigned char* rows, int pitch, int b, int lane) {
+  const int p = lane & 15;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_s16x4*)(rows + ((lane >> 4) * 4 + (p >> 2)) * pitch + b * 32 + (p & 3) * 8));
+}
+
+template <int F>
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * kPassWaves, 64 * kPassWaves), amdgpu_waves_per_eu(1, 1)))
+void one_pass_kernel(Rows r, const uint16_t* __restrict__ w,
+Exponent exponent, float* __restrict__ slab) {
+  constexpr int kPitch = 64 * F + 16;   // odd in 16 bytes: a column's 16 rows lie in different banks
+  __shared__ __attribute__((aligned(16))) unsigned char rows[kPassWaves][kPassRows * kPitch];
+  __shared__ f32x4 sums[2][kPassWaves][64];
+  __shared__ int ids[kPassRows * kMostIds];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int p = lane & 15, g = lane >> 4, col0 = wave * 32 * F + g * 8;
+  const int blocks = (r.V + kPassRows - 1) / kPassRows;
+  for (int t = threadIdx.x; t < r.N * r.k; t += 64 * kPassWaves) ids[t / r.k * kMostIds + t % r.k] = r.ids[t];
+  // 16 rows of a matrix that has `have` left, as buffer loads (one address register for all; what lies
+  // past the rows reads as zeros, and so does what lies past the width, by an offset out of range)
+  const uint32_t at = (uint32_t)(p * r.d + col0) * 2u;
+  auto rows_of = [&](const uint16_t* first, int have) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(first), 0, min(max(have, 0), kPassRows) * r.d * 2,
+                                             0x00020000);
+  };
+  auto piece = [&](auto from, int f, int left) {   // left: columns from col0 to the width
+    return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
+                                          from, f * 32 < left ? at : 0x80000000u, f * 64, 0));
+  };
+  auto block = [&](int b) { return rows_of(w + (int64_t)b * kPassRows * r.d, r.V - b * kPassRows); };
+  bf16x8 h[F], x[F];
+  {
+    const auto from = rows_of(r.copy, r.N), first = block(blockIdx.x);
+#pragma unroll
+    for (int f = 0; f < F; ++f) h[f] = piece(from, f, r.d - col0);
+#pragma unroll
+    for (int f = 0; f < F; ++f) x[f] = piece(first, f, r.d - col0);
+  }
+  const float ref = p < r.N ? r.c[p] : 0.f;
+  f32x4 acc[2 * F];
+#pragma unroll
+  for (int b = 0; b < 2 * F; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int buf = 0;
+  __syncthreads();
+  for (int b = blockIdx.x; b < blocks; b += gridDim.x) {
+    // each piece makes room for the next block's at once, so that a block's worth of loads stays in flight
+    const auto next = block(b + (int)gridDim.x);
+    int left = r.d - col0;
+    asm volatile("" : "+v"(left));   // formed again at every block: kept, the F offsets take F registers
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    wave_lds_fence();
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      *reinterpret_cast<u32x4*>(rows[wave] + p * kPitch + f * 64 + g * 16) = __builtin_bit_cast(u32x4, x[f]);
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[f], h[f], z, 0, 0, 0);
+      x[f] = piece(next, f, left);
+      if (f % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+    sums[buf][wave][lane] = z;
+    stage_barrier<63>();   // (the loads stay in flight)
+    z = sums[buf][0][lane];
+#pragma unroll
+    for (int k = 1; k < kPassWaves; ++k) z += sums[buf][k][lane];
+    buf ^= 1;   // a wave writes it again behind the next barrier, which every reader has then passed
+    // entries v0 .. v0 + 3 of row p
+    const int v0 = b * kPassRows + g * 4;
+    float y[4], from = ref, sum = 0.f;
+    auto values = [&] {
+      sum = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        y[q] = v0 + q < r.V ? exponent(z[q], from) : 0.f;
+        sum += y[q];
+      }
+      sum = across_rows(sum);
+    };
+    values();
+    if (__any(sum > kFar)) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) top = fmaxf(top, v0 + q < r.V ? z[q] : -INFINITY);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (sum > kFar) from = rintf(top * exponent.t);
+      values();
+    }
+    if (p < r.N)
+      for (int j = 0; j < r.k; ++j) {
+        const int at = ids[p * kMostIds + j] - v0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = at == q ? 0.f : y[q];
+      }
+    const u32x2 e = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    if (wave == (b / (int)gridDim.x) % kPassWaves && p < r.N) {
+      *reinterpret_cast<u32x2*>(r.e + (int64_t)p * r.ld + v0) = e;
+      if (g == 0) r.part[(int64_t)p * r.groups + b] = f32x2{from, sum};
+    }
+    const s16x4 ev = __builtin_bit_cast(s16x4, e);
+#pragma unroll
+    for (int k = 0; k < 2 * F; ++k) {
+      acc[k] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(transposed(rows[wave], kPitch, k, lane), ev, acc[k], 0, 0, 0);
+      if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  if (p >= r.N) return;
+  float* out = slab + ((int64_t)blockIdx.x * r.N + p) * r.d;
+#pragma unroll
+  for (int k = 0; k < 2 * F; ++k) {
+    const int col = wave * 32 * F + k * 16 + g * 4;
+    if (col < r.d) *reinterpret_cast<f32x4*>(out + col) = acc[k];
+  }
+}
+
+// d_hidden of a row from the work-groups' sums and the rows of W at its ids, in a fixed order; of a row
+// with entries past its reference from its E.  Grid (ceil(d / 256), N): 4 columns a thread, each wave a
+// quarter of the terms.
+__global__ __launch_bounds__(256) void one_pass_hidden_kernel(Rows r, const uint16_t* __restrict__ w,
+                                                              const float* __restrict__ slab, int groups, void* out,
+                                                              int f32) {
+  __shared__ f32x4 sh[4][64];
+  const int i = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 256 + lane * 4;
+  const float f = r.f[i];
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float e, int64_t v) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(w + v * r.d + col);
+    sum += e * f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
+                     __uint_as_float(x.y & 0xFFFF0000u)};
+  };
+  if (f != 0.f && col < r.d) {
+    if (r.use[i] == kRescaled) {
+#pragma unroll 4
+      for (int v = wave; v < r.V; v += 4) add(__uint_as_float((uint32_t)r.e[(int64_t)i * r.ld + v] << 16), v);
+    } else {
+#pragma unroll 8
+      for (int k = wave; k < groups; k += 4)
+        sum += *reinterpret_cast<const f32x4*>(slab + ((int64_t)k * r.N + i) * r.d + col);
+      const float up = (float)exp2(r.lse2[i] - (double)r.c[i]);
+      for (int j = wave; j < r.k; j += 4) {
+        const int64_t at = (int64_t)i * r.k + j;
+        if (r.ids[at] >= 0) add(r.g[at] * up, r.ids[at]);
+      }
+    }
+  }
+  sh[wave][lane] = sum;
+  __syncthreads();
+  if (wave != 0 || col >= r.d) return;
+  sum = ((sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane])) * f;
+  if (f == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t at = (int64_t)i * r.d + col;
+  if (f32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = sum;
+  else
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+}
+
+// dW = E^T (f H) of up to 16 rows: the scaled rows in LDS, a wave 16 vocabulary entries at a time,
+// whose rows of dW it writes from end to end.  Bound by dW's bytes: MEASURED_DW.  The last work-group
+// sums the loss.
+template <int F>
+__global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
+                                                                        LossSum loss) {
+  constexpr int kPitch = 512 * F + 16;   // F parts of 256 columns
+  __shared__ __attribute__((aligned(16))) unsigned char rows[kPassRows * kPitch];
+  __shared__ double sh[64];
+  if (blockIdx.x == gridDim.x - 1) {
+    loss.run(sh);
+    return;
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, g = lane >> 4;
+  for (int t = threadIdx.x; t < kPassRows * 32 * F; t += 64 * kHeadWaves) {
+    const int i = t / (32 * F), col = t % (32 * F) * 8;
+    u32x4 x = {0, 0, 0, 0};
+    if (i < r.N && col < r.d) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
+    *reinterpret_cast<u32x4*>(rows + i * kPitch + col * 2) = x;
+  }
+  __syncthreads();
+  const int blocks = (r.V + 15) / 16, step = ((int)gridDim.x - 1) * kHeadWaves;
+  auto entries = [&](int b) {   // of vocabulary entry 16 b + p, rows 4 g .. 4 g + 3
+    s16x4 y = {0, 0, 0, 0};
+    const int v = b * 16 + p;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (g * 4 + q < r.N && v < r.V) y[q] = (short)r.e[(int64_t)(g * 4 + q) * r.ld + v];
+    return y;
+  };
+  int b = blockIdx.x * kHeadWaves + wave;
+  s16x4 next = b < blocks ? entries(b) : s16x4{0, 0, 0, 0};
+  for (; b < blocks; b += step) {
+    const s16x4 y = next;
+    if (b + step < blocks) next = entries(b + step);
+    const int v = b * 16 + p;
+    for (int k = 0; k * 32 < r.d; ++k) {
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      const f32x4 c0 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(transposed(rows, kPitch, 2 * k, lane), y, zero, 0, 0, 0);
+      const f32x4 c1 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(transposed(rows, kPitch, 2 * k + 1, lane), y, zero, 0, 0, 0);
+      if (f32) {
+        const int col = k * 32 + g * 4;
+        float* to = static_cast<float*>(out) + (int64_t)v * r.d + col;
+        if (v < r.V && col < r.d) *reinterpret_cast<f32x4*>(to) = add ? *reinterpret_cast<f32x4*>(to) + c0 : c0;
+        if (v < r.V && col + 16 < r.d)
+          *reinterpret_cast<f32x4*>(to + 16) = add ? *reinterpret_cast<f32x4*>(to + 16) + c1 : c1;
+      } else {
+        const u32x4 o = eight_rows(u32x2{pack_bf16(c0[0], c0[1]), pack_bf16(c0[2], c0[3])},
+                                   u32x2{pack_bf16(c1[0], c1[1]), pack_bf16(c1[2], c1[3])});
+        const int col = k * 32 + eight_rows_at(lane);
+        if (v < r.V && col < r.d)
+          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + (int64_t)v * r.d + col) = o;
+      }
+    }
+  }
+}
+
 // Both gradients: out[n][m] = f[n] C(m, n), or C alone (f NULL), bf16 or float32 (or added to it).
 struct EpiGrad {
   static constexpr bool kPair = false, kTile = true;
@@ -864,18 +1106,24 @@ constexpr int kMostVocab = 1 << 21, kMostWidth = 1 << 20;   // a tile's rows sta
 constexpr int kMostRows = 1 << 26;
 constexpr int64_t kMostEntries = int64_t(1) << 36;            // of a matrix: fewer tiles than a launch holds
 
-inline bool few_rows(int64_t N) { return N <= kSkinnyTokens; }
+inline int way_of(int64_t N, int64_t d, bool grads) {
+  if (N <= kPassRows && d <= kMostPassWidth && grads) return kOnePass;
+  return N <= kSkinnyTokens ? kFew : kTiles;
+}
+inline int pass_groups(int64_t V) { return (int)std::min<int64_t>((V + kPassRows - 1) / kPassRows, kPassBlocks); }
 
 struct Layout {
   int64_t ld, groups;
+  int group;
   int64_t use, zs, c, part, lse2, f, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
 };
 // R, P: sequences and pairs of the preference loss.
 Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
   Layout s{};
   s.ld = round_up(V, kGroup);
-  const bool few = few_rows(N);
-  s.groups = few ? (V + kFewGroup - 1) / kFewGroup : s.ld / kGroup;
+  const int way = way_of(N, d, grads);
+  s.group = way == kFew ? kFewGroup : way == kOnePass ? kOnePassGroup : kGroup;
+  s.groups = (V + s.group - 1) / s.group;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t x = at;
@@ -892,10 +1140,10 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   s.g = take(N * k * 4);
   s.terms = take(N * 4 * 8);
   s.copy = take(N * d * 2);
-  s.z = take(few ? N * s.ld * 4 : 0);
-  s.e = take(few && !grads ? 0 : N * s.ld * 2);
-  int64_t slab = slab_reserve(V, N, (int)d);
-  if (grads) {
+  s.z = take(way == kFew ? N * s.ld * 4 : 0);
+  s.e = take(way == kFew && !grads ? 0 : N * s.ld * 2);
+  int64_t slab = way == kOnePass ? pass_groups(V) * N * d * 4 : way == kTiles ? slab_reserve(V, N, (int)d) : 0;
+  if (grads && way != kOnePass) {
     const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0}, nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
     slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
   }
@@ -909,11 +1157,13 @@ bool sizes_fit(int64_t N, int64_t d, int64_t V) {
   return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab && N <= kMostRows &&
          N * d <= kMostEntries && N * V <= kMostEntries && V * d <= kMostEntries;
 }
-// Enough for any call of up to N rows: the float32 logits of few rows may take more than a few rows more do.
+// Enough for any call of up to N rows: the ways of few rows may take more than a few rows more do.
 size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
   if (!sizes_fit(N, d, V)) return 0;
-  return (size_t)std::max(layout_of(N, d, V, k, R, P, grads).total,
-                          layout_of(std::min<int64_t>(N, kSkinnyTokens), d, V, k, R, P, grads).total);
+  int64_t most = layout_of(N, d, V, k, R, P, grads).total;
+  for (const int64_t few : {kPassRows, kSkinnyTokens})
+    if (few < N) most = std::max(most, layout_of(few, d, V, k, R, P, grads).total);
+  return (size_t)most;
 }
 
 // One gradient product, in 256 or 128 square tiles.
@@ -987,8 +1237,9 @@ Rows rows_of(const Call& c, const Layout& s) {
   r.k = c.k;
   r.ld = s.ld;
   r.groups = s.groups;
-  r.few = few_rows(c.N);
+  r.way = way_of(c.N, c.d, c.grads());
   r.grads = c.grads();
+  r.group = s.group;
   r.inv_t = 1.0 / (double)c.temperature;
   r.use = reinterpret_cast<int32_t*>(ws + s.use);
   r.zs = reinterpret_cast<float*>(ws + s.zs);
@@ -1010,6 +1261,38 @@ Exponent exponent_of(const Rows& r) {
   return Exponent{(float)t, (float)(t - (double)(float)t)};
 }
 
+// The kernels of one pass by the width that they are built for.
+template <int F, int... More, class Run>
+int pass_width(int parts, const Run& run) {
+  if (parts <= F) return run(std::integral_constant<int, F>{});
+  if constexpr (sizeof...(More) > 0) return pass_width<More...>(parts, run);
+  return fail(PSPO_ERR_UNSUPPORTED, "d is too wide for one pass");
+}
+int one_pass(const Call& c, const Rows& r, float* slab) {
+  return pass_width<2, 4, 8, 12, 16, 20, 24, 28>((c.d + 32 * kPassWaves - 1) / (32 * kPassWaves), [&](auto f) {
+    hipLaunchKernelGGL(one_pass_kernel<f.value>, dim3((unsigned)pass_groups(c.V)), dim3(64 * kPassWaves), 0, c.stream, r,
+                       c.w, exponent_of(r), slab);
+    PSPO_LAUNCHED("one_pass_kernel", c.stream);
+    return (int)PSPO_OK;
+  });
+}
+int one_pass_gradients(const Call& c, const Rows& r, const float* slab, const LossSum& loss) {
+  if (c.dh != nullptr) {
+    hipLaunchKernelGGL(one_pass_hidden_kernel, dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N), dim3(256), 0, c.stream,
+                       r, c.w, slab, pass_groups(c.V), c.dh, (c.flags & PSPO_OBJ_DH_F32) != 0);
+    PSPO_LAUNCHED("one_pass_hidden_kernel", c.stream);
+  }
+  if (c.dw == nullptr) return PSPO_OK;
+  const int64_t blocks = ((int64_t)c.V + 15) / 16;
+  const int groups = (int)std::min<int64_t>((blocks + kHeadWaves - 1) / kHeadWaves, kPassBlocks);
+  return pass_width<1, 2, 4, 6, 10, 14>((c.d + 255) / 256, [&](auto f) {
+    hipLaunchKernelGGL(one_pass_head_kernel<f.value>, dim3((unsigned)groups + 1), dim3(64 * kHeadWaves), 0, c.stream, r,
+                       c.dw, (c.flags & PSPO_OBJ_DW_F32) != 0, (c.flags & PSPO_ACCUMULATE_DW) != 0, loss);
+    PSPO_LAUNCHED("one_pass_head_kernel", c.stream);
+    return (int)PSPO_OK;
+  });
+}
+
 // Steps 1 to 3 (N > 0).
 template <class Op>
 int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
@@ -1017,7 +1300,9 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
   hipLaunchKernelGGL(gather_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
   PSPO_LAUNCHED("gather_kernel", c.stream);
-  if (r.few) {
+  if (r.way == kOnePass) {
+    if (int rc = one_pass(c, r, slab)) return rc;
+  } else if (r.way == kFew) {
     if (int rc = skinny<1>(SkinnyArgs{{c.w, c.w}, r.copy, c.V, c.N, c.d}, SkinnyLogits{z, s.ld}, "objective_logits",
                            c.stream))
       return rc;
@@ -1039,7 +1324,8 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
 // Step 4.
 int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss) {
   const bool both = c.dh != nullptr && c.dw != nullptr;
-  if (loss.loss != nullptr && (c.N == 0 || !both)) {   // otherwise it goes along below
+  const bool along = c.N > 0 && (r.way == kOnePass ? c.dw != nullptr : both);   // the loss's sum, with a launch below
+  if (loss.loss != nullptr && !along) {
     hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(1024), 0, c.stream, loss);
     PSPO_LAUNCHED("loss_sum_kernel", c.stream);
   }
@@ -1054,7 +1340,9 @@ int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss)
     PSPO_LAUNCHED("fill_zero_kernel", c.stream);
     return PSPO_OK;
   }
-  if (r.few) {
+  if (r.way == kOnePass)
+    return one_pass_gradients(c, r, slab, loss);
+  if (r.way == kFew) {
     hipLaunchKernelGGL(few_entries_kernel, dim3((unsigned)c.N, (unsigned)((s.ld + 2047) / 2048)), dim3(256), 0,
                        c.stream, r, (const float*)z, exponent_of(r));
     PSPO_LAUNCHED("few_entries_kernel", c.stream);
