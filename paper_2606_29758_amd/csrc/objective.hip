@@ -35,8 +35,8 @@ namespace {
 constexpr int kGroup = 64;         // vocabulary entries of one (reference, sum)
 constexpr int kFewGroup = 2048;    // ... where the logits are kept in float32
 constexpr int kOnePassGroup = 16;  // ... in one pass over W
-// Ways of a call, by its size (way_of): tiles; up to 64 rows, the logits in float32 first; up to 16
-// rows, logits and d_hidden in one pass over W.
+// Ways of a call, by its size (way_of): tiles; up to 64 rows, logits and d_hidden in one pass over W, or,
+// where d is too wide for that or no gradient is wanted, the logits in float32 first.
 enum { kTiles, kFew, kOnePass };
 constexpr int kMostIds = 64;
 
@@ -189,16 +189,43 @@ __device__ __forceinline__ T wave_sum(T x) {
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
   return x;
 }
-// Over the 256 threads of a work-group, in a fixed order; every thread gets the result.
-__device__ __forceinline__ float block_max(float x, float* sh) {
-  x = wave_max(x);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = x;
-  __syncthreads();
-  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-}
-template <class T>
-__device__ __forceinline__ T block_total(T x, T* sh) {
+// The threads that take a row: a work-group of 256, or, from kTeamRows rows on, a wave (a work-group of
+// four): 2,438 rows, d = 816, V = 1915 79 -> 72 us a call, 764 rows, 1656, 3661 78 -> 82 by waves.  Results
+// of max and sum are the same in all threads, in a fixed order.
+constexpr int64_t kTeamRows = 2048;
+template <int kThreads>
+struct Team {
+  float maxima[4];
+  double sums[4];
+  static __device__ __forceinline__ int row() { return blockIdx.x * (256 / kThreads) + threadIdx.x / kThreads; }
+  static __device__ __forceinline__ int thread() { return threadIdx.x % kThreads; }
+  __device__ __forceinline__ void sync() const {
+    if constexpr (kThreads == 256) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  __device__ __forceinline__ bool any(bool x) const {
+    if constexpr (kThreads == 256) return __syncthreads_or(x);
+    else return __any(x);
+  }
+  __device__ __forceinline__ float max(float x) {
+    x = wave_max(x);
+    if constexpr (kThreads == 64) return x;
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) maxima[threadIdx.x / 64] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
+  }
+  __device__ __forceinline__ double sum(double x) {
+    x = wave_sum(x);
+    if constexpr (kThreads == 64) return x;
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = x;
+    __syncthreads();
+    return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  }
+};
+// Over the 256 threads of a work-group.
+__device__ __forceinline__ double block_total(double x, double* sh) {
   x = wave_sum(x);
   __syncthreads();
   if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = x;
@@ -209,7 +236,7 @@ __device__ __forceinline__ T block_total(T x, T* sh) {
 // (Reference, sum) of the groups of 2,048 logits of a row.  Grid (N, groups).
 __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict__ z, int64_t ld, int V,
                                                          Exponent exponent, f32x2* __restrict__ part) {
-  __shared__ float sh[4];
+  __shared__ Team<256> team;
   const int v0 = blockIdx.y * kFewGroup + threadIdx.x * 8;
   const float* row = z + (int64_t)blockIdx.x * ld;
   float x[8], top = -INFINITY, sum = 0.f;
@@ -218,10 +245,10 @@ __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict
     x[k] = v0 + k < V ? row[v0 + k] : -INFINITY;
     top = fmaxf(top, x[k]);
   }
-  const float ref = rintf(block_max(top, sh) * exponent.t);
+  const float ref = rintf(team.max(top) * exponent.t);
 #pragma unroll
   for (int k = 0; k < 8; ++k) sum += v0 + k < V ? exponent(x[k], ref) : 0.f;
-  sum = block_total(sum, sh);
+  sum = (float)team.sum(sum);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{ref, sum};
 }
 
@@ -253,35 +280,36 @@ __device__ __forceinline__ void raise(int32_t* err, int bit) {
 }
 
 // ---- 1. gather -------------------------------------------------------------------------
-// A work-group per row; its waves take four ids each in turn, whose rows of W are read beside the
-// hidden row.  Op::use(i, lane, r): as Rows::use, the same in all lanes; Op::id(i, j, r): the row's
+// A team per row; its waves take four ids each in turn, whose rows of W are read beside the hidden
+// row.  Op::use(i, lane, r): as Rows::use, the same in all lanes; Op::id(i, j, r): the row's
 // j-th id or -1.
-template <class Op>
+template <int kThreads, class Op>
 __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16_t* __restrict__ hidden,
                                                      const uint16_t* __restrict__ w) {
-  __shared__ float sh[4];
-  const int i = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  __shared__ Team<kThreads> team;
+  const int i = team.row(), t = team.thread(), lane = t % 64, wave = t / 64;
+  if (i >= r.N) return;
   const int use = op.use(i, lane, r);
-  if (threadIdx.x == 0) r.use[i] = use;
-  if ((int)threadIdx.x < r.k) {   // (finalize writes what becomes of them)
-    const int64_t at = (int64_t)i * r.k + threadIdx.x;
-    r.ids[at] = use == 1 ? op.id(i, threadIdx.x, r) : -1;
+  if (t == 0) r.use[i] = use;
+  if (t < r.k) {   // (finalize writes what becomes of them)
+    const int64_t at = (int64_t)i * r.k + t;
+    r.ids[at] = use == 1 ? op.id(i, t, r) : -1;
   }
   const u32x4* from = reinterpret_cast<const u32x4*>(hidden + (int64_t)i * r.d);
   u32x4* to = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
   const int pieces = r.d / 8;
-  for (int p = threadIdx.x; p < pieces; p += 256) {
+  for (int p = t; p < pieces; p += kThreads) {
     u32x4 x = {0, 0, 0, 0};
     if (use == 1) x = from[p];
     to[p] = x;
   }
   if (use != 1) {
-    if (threadIdx.x == 0) r.c[i] = 0.f;
+    if (t == 0) r.c[i] = 0.f;
     return;
   }
   constexpr int kAt = 4;
   float top = -INFINITY;
-  for (int j0 = wave * kAt; j0 < r.k; j0 += 4 * kAt) {
+  for (int j0 = wave * kAt; j0 < r.k; j0 += kThreads / 64 * kAt) {
     const u32x4* row[kAt];
     bool on[kAt];
     float sum[kAt] = {};
@@ -291,7 +319,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
       on[j] = id >= 0;
       row[j] = reinterpret_cast<const u32x4*>(w + (int64_t)(on[j] ? id : 0) * r.d);
     }
-#pragma unroll 2
+#pragma unroll 4
     for (int p = lane; p < pieces; p += 64) {
       const u32x4 hv = from[p];
 #pragma unroll
@@ -312,14 +340,16 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
       if (on[j]) top = fmaxf(top, sum[j]);
     }
   }
-  top = block_max(top, sh);
-  if (threadIdx.x == 0) r.c[i] = rintf(top * (float)(r.inv_t * 1.4426950408889634));
+  top = team.max(top);
+  if (t == 0) r.c[i] = rintf(top * (float)(r.inv_t * 1.4426950408889634));
 }
 
 // The row's hidden entries times its factor, the second operand of dW.
+template <int kThreads>
 __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
   u32x4* row = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
-  for (int p = threadIdx.x; p < r.d / 8; p += 256) {
+#pragma unroll 4
+  for (int p = Team<kThreads>::thread(); p < r.d / 8; p += kThreads) {
     u32x4 x = row[p];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -329,16 +359,17 @@ __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
 }
 
 // ---- 3. finalize -----------------------------------------------------------------------
-// A work-group per row: log2 of the sum over its groups, in a fixed order (a row whose groups have
+// A team per row: log2 of the sum over its groups, in a fixed order (a row whose groups have
 // several references brought to the largest one); then op.row, called by the first wave, gives the
 // terms, the row's factor a of p and, in r.ids and r.g, the entries G / a at the ids.  E's own scale
 // is 2^(lse2 - c): the entries go in with it and the factor takes its inverse.
-template <class Op>
+template <int kThreads, class Op>
 __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
-  __shared__ float shf[4];
-  __shared__ double shd[4];
-  __shared__ float factor;
-  const int i = blockIdx.x;
+  __shared__ Team<kThreads> team;
+  __shared__ float factors[256 / kThreads];
+  const int i = team.row(), t = team.thread();
+  if (i >= r.N) return;
+  float& factor = factors[threadIdx.x / kThreads];
   const int use = r.use[i];
   uint16_t* row = r.e + (int64_t)i * r.ld;
   double lse2 = 0.0;
@@ -350,21 +381,21 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
     double sum = 0.0;
     bool far = false;
 #pragma unroll 8
-    for (int g = threadIdx.x; g < r.groups; g += 256) {
+    for (int g = t; g < r.groups; g += kThreads) {
       const f32x2 p = part[g];
       sum += p.y;
       top = fmaxf(top, p.x);
       far = far || p.x != c;
     }
-    if (__syncthreads_or(far)) {
-      top = block_max(top, shf);
+    if (team.any(far)) {
+      top = team.max(top);
       sum = 0.0;
-      for (int g = threadIdx.x; g < r.groups; g += 256) {
+      for (int g = t; g < r.groups; g += kThreads) {
         const f32x2 p = part[g];
         if (p.x != -INFINITY || p.y != 0.f) sum += (double)p.y * (double)__builtin_amdgcn_exp2f(p.x - top);
       }
       if (r.way != kFew && r.grads)
-        for (int64_t v0 = threadIdx.x * 8; v0 < r.groups * r.group; v0 += 2048) {
+        for (int64_t v0 = t * 8; v0 < r.groups * r.group; v0 += kThreads * 8) {
           const float down = __builtin_amdgcn_exp2f(part[v0 / r.group].x - top);
           u32x4 x = *reinterpret_cast<const u32x4*>(row + v0);
 #pragma unroll
@@ -373,14 +404,14 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
           *reinterpret_cast<u32x4*>(row + v0) = x;
         }
       c = top;
-      if (threadIdx.x == 0) r.use[i] = kRescaled;
+      if (t == 0) r.use[i] = kRescaled;
     }
-    lse2 = (double)c + log2(block_total(sum, shd));
+    lse2 = (double)c + log2(team.sum(sum));
   }
   if (r.way == kFew) c = (float)lse2;   // E is written from the logits, relative to the sum
-  if (threadIdx.x < 64) {
-    const float a = op.row(i, threadIdx.x, use, lse2 * 0.6931471805599453, r);
-    if (threadIdx.x == 0) {
+  if (t < 64) {
+    const float a = op.row(i, t, use, lse2 * 0.6931471805599453, r);
+    if (t == 0) {
       r.lse2[i] = lse2;
       r.c[i] = c;
       factor = use == 1 && a != 0.f ? a * (float)exp2((double)c - lse2) : 0.f;
@@ -388,13 +419,13 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
     }
   }
   if (!r.grads) return;
-  __syncthreads();   // also: the rescaled row, r.ids and r.g are written
-  if (r.way != kFew && use == 1 && threadIdx.x < r.k) {
-    const int64_t at = (int64_t)i * r.k + threadIdx.x;
+  team.sync();   // also: the rescaled row, r.ids and r.g are written
+  if (r.way != kFew && use == 1 && t < r.k) {
+    const int64_t at = (int64_t)i * r.k + t;
     const int id = r.ids[at];
     if (id >= 0) row[id] = (uint16_t)pack_bf16((float)((double)r.g[at] * exp2(lse2 - (double)c)), 0.f);
   }
-  if (Op::kFactor) scale_copy(r, i, factor);
+  if (Op::kFactor) scale_copy<kThreads>(r, i, factor);
 }
 
 // The loss from the rows' terms, in a fixed order: terms [kinds][n], loss = times[0] sum 0 + times[1]
@@ -675,9 +706,11 @@ __global__ __launch_bounds__(64 * kPrefWaves) void pref_all_kernel(Pairs q, int 
   *loss = x;
 }
 
-// The row's factor, from its sequence's; a work-group per row.
+// The row's factor, from its sequence's; a team per row.
+template <int kThreads>
 __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
-  const int i = blockIdx.x;
+  const int i = Team<kThreads>::row();
+  if (i >= r.N) return;
   int s = 0, e = q.R;   // the last sequence that starts at or before row i
   while (s < e) {
     const int mid = s + (e - s) / 2;
@@ -688,11 +721,11 @@ __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
   const double delta = on ? q.coef[s] * r.terms[2 * (int64_t)r.N + i] : 0.0;
   const float a = (float)(-delta * r.inv_t);
   const float f = on && a != 0.f ? a * (float)exp2((double)r.c[i] - r.lse2[i]) : 0.f;
-  if (threadIdx.x == 0) {
+  if (Team<kThreads>::thread() == 0) {
     if (on && !std::isfinite(a)) raise(r.err, PSPO_DEVERR_NONFINITE);
     r.f[i] = f;
   }
-  scale_copy(r, i, f);
+  scale_copy<kThreads>(r, i, f);
 }
 
 // ---- distillation -----------------------------------------------------------------------------
@@ -793,7 +826,7 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
   }
 }
 
-// ---- up to 16 rows: one pass over W ------------------------------------------------------------
+// ---- up to 64 rows: one pass over W ------------------------------------------------------------
 // A work-group takes blocks of 16 vocabulary entries in turn; its 4 waves, one to a SIMD with all of
 // its registers (8 waves of half of them spilled from d = 2,560 on), split the hidden width, 32 F columns
 // each.  A wave's part of the block comes to registers (the next block's while this one is
@@ -803,9 +836,10 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
 // the logits and d_hidden.  Entries at the rows' ids count in the sums but not in the product (they
 // are added at the end with what becomes of them).  The entries of a block that pass 2^32 take their own
 // reference, as in the tiles; their row's accumulators are then of no use (no other row's are touched),
-// and its d_hidden is formed from E (one_pass_hidden_kernel).
+// and its d_hidden is formed from E (one_pass_hidden_kernel).  16 rows to a work-group, those of the others
+// in grid y, which meet W's blocks in the same L2 at about the same time (gridDim.x % 8 == 0 then).
 // Bound by W's bytes: MEASURED_PASS.
-constexpr int kPassWaves = 4, kPassRows = 16, kPassBlocks = 256, kHeadWaves = 8;
+constexpr int kPassWaves = 4, kPassRows = 16, kHeadWaves = 8, kHiddenWaves = 16;
 constexpr int kMostPassWidth = 28 * 32 * kPassWaves;   // what the registers of a work-group to a CU hold
 
 // Four rows (4 g .. 4 g + 3) of column 16 b + lane % 16 of a wave's rows of bf16 in LDS, `pitch` bytes
@@ -816,18 +850,26 @@ __device__ __forceinline__ s16x4 transposed(const unsigned char* rows, int pitch
       (lds_s16x4*)(rows + ((lane >> 4) * 4 + (p >> 2)) * pitch + b * 32 + (p & 3) * 8));
 }
 
+constexpr int pass_per_cu(int parts) { return parts <= 4 ? 4 : (parts <= 12 ? 2 : 1); }
 template <int F>
-__global__ __attribute__((amdgpu_flat_work_group_size(64 * kPassWaves, 64 * kPassWaves), amdgpu_waves_per_eu(1, 1)))
+__global__ __attribute__((amdgpu_flat_work_group_size(64 * kPassWaves, 64 * kPassWaves),
+                          amdgpu_waves_per_eu(pass_per_cu(F), pass_per_cu(F))))
 void one_pass_kernel(Rows r, const uint16_t* __restrict__ w,
 Exponent exponent, float* __restrict__ slab) {
   constexpr int kPitch = 64 * F + 16;   // odd in 16 bytes: a column's 16 rows lie in different banks
   __shared__ __attribute__((aligned(16))) unsigned char rows[kPassWaves][kPassRows * kPitch];
   __shared__ f32x4 sums[2][kPassWaves][64];
-  __shared__ int ids[kPassRows * kMostIds];
+  __shared__ int ids[kPassRows * kMostIds], count;   // those in this work-group's blocks: id + 2^21 (row of the 16)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int p = lane & 15, g = lane >> 4, col0 = wave * 32 * F + g * 8;
+  const int i0 = blockIdx.y * kPassRows, n = min(r.N - i0, kPassRows), i = i0 + p;   // this work-group's rows, this lane's
   const int blocks = (r.V + kPassRows - 1) / kPassRows;
-  for (int t = threadIdx.x; t < r.N * r.k; t += 64 * kPassWaves) ids[t / r.k * kMostIds + t % r.k] = r.ids[t];
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  for (int t = threadIdx.x; t < n * r.k; t += 64 * kPassWaves) {
+    const int id = r.ids[(int64_t)i0 * r.k + t];
+    if (id >= 0 && id / kPassRows % (int)gridDim.x == (int)blockIdx.x) ids[atomicAdd(&count, 1)] = id | t / r.k << 21;
+  }
   // 16 rows of a matrix that has `have` left, as buffer loads (one address register for all; what lies
   // past the rows reads as zeros, and so does what lies past the width, by an offset out of range)
   const uint32_t at = (uint32_t)(p * r.d + col0) * 2u;
@@ -842,18 +884,19 @@ Exponent exponent, float* __restrict__ slab) {
   auto block = [&](int b) { return rows_of(w + (int64_t)b * kPassRows * r.d, r.V - b * kPassRows); };
   bf16x8 h[F], x[F];
   {
-    const auto from = rows_of(r.copy, r.N), first = block(blockIdx.x);
+    const auto from = rows_of(r.copy + (int64_t)i0 * r.d, n), first = block(blockIdx.x);
 #pragma unroll
     for (int f = 0; f < F; ++f) h[f] = piece(from, f, r.d - col0);
 #pragma unroll
     for (int f = 0; f < F; ++f) x[f] = piece(first, f, r.d - col0);
   }
-  const float ref = p < r.N ? r.c[p] : 0.f;
+  const float ref = p < n ? r.c[i] : 0.f;
   f32x4 acc[2 * F];
 #pragma unroll
   for (int b = 0; b < 2 * F; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   int buf = 0;
   __syncthreads();
+  const int own = count;
   for (int b = blockIdx.x; b < blocks; b += gridDim.x) {
     // each piece makes room for the next block's at once, so that a block's worth of loads stays in flight
     const auto next = block(b + (int)gridDim.x);
@@ -896,16 +939,15 @@ Exponent exponent, float* __restrict__ slab) {
       if (sum > kFar) from = rintf(top * exponent.t);
       values();
     }
-    if (p < r.N)
-      for (int j = 0; j < r.k; ++j) {
-        const int at = ids[p * kMostIds + j] - v0;
+    for (int j = 0; j < own; ++j) {
+      const int at = ids[j] - (v0 | p << 21);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[q] = at == q ? 0.f : y[q];
-      }
+      for (int q = 0; q < 4; ++q) y[q] = at == q ? 0.f : y[q];
+    }
     const u32x2 e = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-    if (wave == (b / (int)gridDim.x) % kPassWaves && p < r.N) {
-      *reinterpret_cast<u32x2*>(r.e + (int64_t)p * r.ld + v0) = e;
-      if (g == 0) r.part[(int64_t)p * r.groups + b] = f32x2{from, sum};
+    if (wave == (b / (int)gridDim.x) % kPassWaves && p < n) {
+      *reinterpret_cast<u32x2*>(r.e + (int64_t)i * r.ld + v0) = e;
+      if (g == 0) r.part[(int64_t)i * r.groups + b] = f32x2{from, sum};
     }
     const s16x4 ev = __builtin_bit_cast(s16x4, e);
 #pragma unroll
@@ -914,8 +956,8 @@ Exponent exponent, float* __restrict__ slab) {
       if (k % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
   }
-  if (p >= r.N) return;
-  float* out = slab + ((int64_t)blockIdx.x * r.N + p) * r.d;
+  if (p >= n) return;
+  float* out = slab + ((int64_t)blockIdx.x * r.N + i) * r.d;
 #pragma unroll
   for (int k = 0; k < 2 * F; ++k) {
     const int col = wave * 32 * F + k * 16 + g * 4;
@@ -925,11 +967,11 @@ Exponent exponent, float* __restrict__ slab) {
 
 // d_hidden of a row from the work-groups' sums and the rows of W at its ids, in a fixed order; of a row
 // with entries past its reference from its E.  Grid (ceil(d / 256), N): 4 columns a thread, each wave a
-// quarter of the terms.
-__global__ __launch_bounds__(256) void one_pass_hidden_kernel(Rows r, const uint16_t* __restrict__ w,
+// sixteenth of the terms.
+__global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows r, const uint16_t* __restrict__ w,
                                                               const float* __restrict__ slab, int groups, void* out,
                                                               int f32) {
-  __shared__ f32x4 sh[4][64];
+  __shared__ f32x4 sh[kHiddenWaves][64];
   const int i = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 256 + lane * 4;
   const float f = r.f[i];
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -941,13 +983,13 @@ __global__ __launch_bounds__(256) void one_pass_hidden_kernel(Rows r, const uint
   if (f != 0.f && col < r.d) {
     if (r.use[i] == kRescaled) {
 #pragma unroll 4
-      for (int v = wave; v < r.V; v += 4) add(__uint_as_float((uint32_t)r.e[(int64_t)i * r.ld + v] << 16), v);
+      for (int v = wave; v < r.V; v += kHiddenWaves) add(__uint_as_float((uint32_t)r.e[(int64_t)i * r.ld + v] << 16), v);
     } else {
 #pragma unroll 8
-      for (int k = wave; k < groups; k += 4)
+      for (int k = wave; k < groups; k += kHiddenWaves)
         sum += *reinterpret_cast<const f32x4*>(slab + ((int64_t)k * r.N + i) * r.d + col);
       const float up = (float)exp2(r.lse2[i] - (double)r.c[i]);
-      for (int j = wave; j < r.k; j += 4) {
+      for (int j = wave; j < r.k; j += kHiddenWaves) {
         const int64_t at = (int64_t)i * r.k + j;
         if (r.ids[at] >= 0) add(r.g[at] * up, r.ids[at]);
       }
@@ -956,7 +998,9 @@ __global__ __launch_bounds__(256) void one_pass_hidden_kernel(Rows r, const uint
   sh[wave][lane] = sum;
   __syncthreads();
   if (wave != 0 || col >= r.d) return;
-  sum = ((sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane])) * f;
+#pragma unroll
+  for (int k = 1; k < kHiddenWaves; ++k) sum += sh[k][lane];
+  sum *= f;
   if (f == 0.f) sum = f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t at = (int64_t)i * r.d + col;
   if (f32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = sum;
@@ -1107,10 +1151,15 @@ constexpr int kMostRows = 1 << 26;
 constexpr int64_t kMostEntries = int64_t(1) << 36;            // of a matrix: fewer tiles than a launch holds
 
 inline int way_of(int64_t N, int64_t d, bool grads) {
-  if (N <= kPassRows && d <= kMostPassWidth && grads) return kOnePass;
-  return N <= kSkinnyTokens ? kFew : kTiles;
+  if (N > kSkinnyTokens) return kTiles;
+  return d <= kMostPassWidth && grads ? kOnePass : kFew;
 }
-inline int pass_groups(int64_t V) { return (int)std::min<int64_t>((V + kPassRows - 1) / kPassRows, kPassBlocks); }
+// Work-groups of one pass for each 16 rows: as many as run at once.
+inline int64_t pass_groups(int64_t N, int64_t d, int64_t V) {
+  const int64_t all = 256 * pass_per_cu((int)((d + 32 * kPassWaves - 1) / (32 * kPassWaves)));
+  const int64_t most = all / ((N + kPassRows - 1) / kPassRows) / kNumXcd * kNumXcd;
+  return std::min<int64_t>((V + kPassRows - 1) / kPassRows, most);
+}
 
 struct Layout {
   int64_t ld, groups;
@@ -1142,10 +1191,12 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   s.copy = take(N * d * 2);
   s.z = take(way == kFew ? N * s.ld * 4 : 0);
   s.e = take(way == kFew && !grads ? 0 : N * s.ld * 2);
-  int64_t slab = way == kOnePass ? pass_groups(V) * N * d * 4 : way == kTiles ? slab_reserve(V, N, (int)d) : 0;
-  if (grads && way != kOnePass) {
-    const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0}, nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
-    slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
+  int64_t slab = way == kOnePass ? pass_groups(N, d, V) * N * d * 4 : way == kTiles ? slab_reserve(V, N, (int)d) : 0;
+  if (grads && (way != kOnePass || N > kPassRows)) {
+    const int64_t M[3] = {way == kOnePass ? 0 : d, d, 0}, C[3] = {N, V, 0};
+    const int64_t nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
+    if (way == kOnePass) slab = std::max(slab, jobs_reserve(M, C, nk));
+    else slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
   }
   s.slab = take(slab);
   s.seqs = take(R * 3 * 8);
@@ -1157,11 +1208,11 @@ bool sizes_fit(int64_t N, int64_t d, int64_t V) {
   return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab && N <= kMostRows &&
          N * d <= kMostEntries && N * V <= kMostEntries && V * d <= kMostEntries;
 }
-// Enough for any call of up to N rows: the ways of few rows may take more than a few rows more do.
+// Enough for any call of up to N rows: 16, 32, 48 and 64 may take more than a few rows more do.
 size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
   if (!sizes_fit(N, d, V)) return 0;
   int64_t most = layout_of(N, d, V, k, R, P, grads).total;
-  for (const int64_t few : {kPassRows, kSkinnyTokens})
+  for (int64_t few = kPassRows; few <= kSkinnyTokens; few += kPassRows)
     if (few < N) most = std::max(most, layout_of(few, d, V, k, R, P, grads).total);
   return (size_t)most;
 }
@@ -1175,8 +1226,8 @@ Plan plan_square(int64_t M, int64_t N, int K) {
 // Both as one launch (against two, us a call: 1 row, d = 1536, V = 151936 411 / 472; 1,301, 1000, 50257 492 /
 // 528; 4,096, 3584, 152064 10,602 / 10,818; 4,999 of the same 13,024 / 12,871).  One alone goes as a product,
 // whose last round is split along K (8,192 rows, d = 3584: 13,536 against 14,105).
-JobPlan plan_gradients(int64_t N, int64_t d, int64_t V) {
-  const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0};
+JobPlan plan_gradients(int64_t N, int64_t d, int64_t V, bool dh) {
+  const int64_t M[3] = {dh ? d : 0, d, 0}, C[3] = {N, V, 0};
   const int nk[3] = {(int)((V + kRowK - 1) / kRowK), (int)((N + kRowK - 1) / kRowK), 0};
   const JobPlan big = plan_jobs(M, C, nk, 256), small = plan_jobs(M, C, nk, 128);
   return big.us <= small.us ? big : small;
@@ -1270,21 +1321,16 @@ int pass_width(int parts, const Run& run) {
 }
 int one_pass(const Call& c, const Rows& r, float* slab) {
   return pass_width<2, 4, 8, 12, 16, 20, 24, 28>((c.d + 32 * kPassWaves - 1) / (32 * kPassWaves), [&](auto f) {
-    hipLaunchKernelGGL(one_pass_kernel<f.value>, dim3((unsigned)pass_groups(c.V)), dim3(64 * kPassWaves), 0, c.stream, r,
+    hipLaunchKernelGGL(one_pass_kernel<f.value>, dim3((unsigned)pass_groups(c.N, c.d, c.V), (unsigned)((c.N + kPassRows - 1) / kPassRows)),
+                       dim3(64 * kPassWaves), 0, c.stream, r,
                        c.w, exponent_of(r), slab);
     PSPO_LAUNCHED("one_pass_kernel", c.stream);
     return (int)PSPO_OK;
   });
 }
-int one_pass_gradients(const Call& c, const Rows& r, const float* slab, const LossSum& loss) {
-  if (c.dh != nullptr) {
-    hipLaunchKernelGGL(one_pass_hidden_kernel, dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N), dim3(256), 0, c.stream,
-                       r, c.w, slab, pass_groups(c.V), c.dh, (c.flags & PSPO_OBJ_DH_F32) != 0);
-    PSPO_LAUNCHED("one_pass_hidden_kernel", c.stream);
-  }
-  if (c.dw == nullptr) return PSPO_OK;
+int one_pass_head(const Call& c, const Rows& r, const LossSum& loss) {
   const int64_t blocks = ((int64_t)c.V + 15) / 16;
-  const int groups = (int)std::min<int64_t>((blocks + kHeadWaves - 1) / kHeadWaves, kPassBlocks);
+  const int groups = (int)std::min<int64_t>((blocks + kHeadWaves - 1) / kHeadWaves, 256);
   return pass_width<1, 2, 4, 6, 10, 14>((c.d + 255) / 256, [&](auto f) {
     hipLaunchKernelGGL(one_pass_head_kernel<f.value>, dim3((unsigned)groups + 1), dim3(64 * kHeadWaves), 0, c.stream, r,
                        c.dw, (c.flags & PSPO_OBJ_DW_F32) != 0, (c.flags & PSPO_ACCUMULATE_DW) != 0, loss);
@@ -1298,7 +1344,10 @@ template <class Op>
 int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
-  hipLaunchKernelGGL(gather_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
+  if (c.N < kTeamRows || c.k > 4)   // (a wave's turn takes four ids: 663 rows of lists 97 -> 121 us by waves)
+    hipLaunchKernelGGL((gather_kernel<256, Op>), dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
+  else
+    hipLaunchKernelGGL((gather_kernel<64, Op>), dim3((unsigned)((c.N + 3) / 4)), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
   PSPO_LAUNCHED("gather_kernel", c.stream);
   if (r.way == kOnePass) {
     if (int rc = one_pass(c, r, slab)) return rc;
@@ -1316,7 +1365,10 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
                                        "objective_logits", c.stream))
       return rc;
   }
-  hipLaunchKernelGGL(finalize_kernel<Op>, dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op);
+  if (c.N < kTeamRows)
+    hipLaunchKernelGGL((finalize_kernel<256, Op>), dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op);
+  else
+    hipLaunchKernelGGL((finalize_kernel<64, Op>), dim3((unsigned)((c.N + 3) / 4)), dim3(256), 0, c.stream, r, op);
   PSPO_LAUNCHED("finalize_kernel", c.stream);
   return PSPO_OK;
 }
@@ -1340,8 +1392,14 @@ int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss)
     PSPO_LAUNCHED("fill_zero_kernel", c.stream);
     return PSPO_OK;
   }
-  if (r.way == kOnePass)
-    return one_pass_gradients(c, r, slab, loss);
+  if (r.way == kOnePass && c.dh != nullptr) {
+    hipLaunchKernelGGL(one_pass_hidden_kernel, dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N),
+                       dim3(64 * kHiddenWaves), 0, c.stream, r, c.w, (const float*)slab, (int)pass_groups(c.N, c.d, c.V), c.dh,
+                       (c.flags & PSPO_OBJ_DH_F32) != 0);
+    PSPO_LAUNCHED("one_pass_hidden_kernel", c.stream);
+  }
+  if (r.way == kOnePass && c.dw == nullptr) return PSPO_OK;
+  if (r.way == kOnePass && c.N <= kPassRows) return one_pass_head(c, r, loss);
   if (r.way == kFew) {
     hipLaunchKernelGGL(few_entries_kernel, dim3((unsigned)c.N, (unsigned)((s.ld + 2047) / 2048)), dim3(256), 0,
                        c.stream, r, (const float*)z, exponent_of(r));
@@ -1351,8 +1409,11 @@ int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss)
                          shape(r.copy, r.copy, c.d, c.d, r.e, s.ld, c.V, c.N), RowShape{}};
   const EpiGrad o[3] = {{c.dh, r.f, c.d, c.d, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0, 0, loss},
                         {c.dw, nullptr, c.d, c.d, c.V, f32, add, LossSum{}}, EpiGrad{}};
+  if (r.way == kOnePass)
+    return run_jobs(plan_gradients(c.N, c.d, c.V, false), g, o, reinterpret_cast<unsigned char*>(slab), "objective_dw",
+                    c.stream);
   if (both)
-    return run_jobs(plan_gradients(c.N, c.d, c.V), g, o, reinterpret_cast<unsigned char*>(slab), "objective_gradients",
+    return run_jobs(plan_gradients(c.N, c.d, c.V, true), g, o, reinterpret_cast<unsigned char*>(slab), "objective_gradients",
                     c.stream);
   if (c.dh != nullptr)
     return product<true, false>(g[0], plan_square(c.d, c.N, c.V), c.N, o[0], slab, "objective_dh", c.stream);
@@ -1468,7 +1529,8 @@ int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, cons
     PSPO_LAUNCHED("pref_coef_kernel", stream);
   }
   if (N > 0 && c.grads()) {
-    hipLaunchKernelGGL(pref_rows_kernel, dim3((unsigned)N), dim3(256), 0, stream, r, q);
+    if (N < kTeamRows) hipLaunchKernelGGL(pref_rows_kernel<256>, dim3((unsigned)N), dim3(256), 0, stream, r, q);
+    else hipLaunchKernelGGL(pref_rows_kernel<64>, dim3((unsigned)((N + 3) / 4)), dim3(256), 0, stream, r, q);
     PSPO_LAUNCHED("pref_rows_kernel", stream);
   }
   return backward(c, s, r, LossSum{});
