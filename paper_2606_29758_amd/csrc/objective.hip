@@ -1154,11 +1154,16 @@ inline int way_of(int64_t N, int64_t d, bool grads) {
   if (N > kSkinnyTokens) return kTiles;
   return d <= kMostPassWidth && grads ? kOnePass : kFew;
 }
-// Work-groups of one pass for each 16 rows: as many as run at once.
+// Work-groups of one pass for each 16 rows: as many as run at once, but with four blocks of the
+// vocabulary to each beyond one a CU (their sums are read again: 5 rows, d = 376, V = 22700 47 us with
+// 1,024 of them, 39 with 354).  From d = 520 on one to a CU is better for up to 32 rows (17, d = 1536,
+// V = 151936 357 / 383 us a call), two for more (40: 458 / 416).
 inline int64_t pass_groups(int64_t N, int64_t d, int64_t V) {
-  const int64_t all = 256 * pass_per_cu((int)((d + 32 * kPassWaves - 1) / (32 * kPassWaves)));
-  const int64_t most = all / ((N + kPassRows - 1) / kPassRows) / kNumXcd * kNumXcd;
-  return std::min<int64_t>((V + kPassRows - 1) / kPassRows, most);
+  const int64_t parts = (d + 32 * kPassWaves - 1) / (32 * kPassWaves);
+  const int64_t per_cu = parts > 4 && N <= 32 ? 1 : pass_per_cu((int)parts);
+  const int64_t blocks = (V + kPassRows - 1) / kPassRows, one = 256 / ((N + kPassRows - 1) / kPassRows);
+  const int64_t most = std::min(one * per_cu, std::max(one, blocks / 4)) / kNumXcd * kNumXcd;
+  return std::min(blocks, most);
 }
 
 struct Layout {
