@@ -59,7 +59,8 @@ extern "C" {
 
 /*
  * Bytes of device workspace each call below needs for up to N rows (host-only, pure
- * function; 0 for sizes that the calls refuse).  grads: whether a gradient is wanted.
+ * function; 0 for sizes that the calls refuse).  grads: whether a gradient is wanted (a
+ * size asked for with them serves calls without them too).
  */
 size_t pspo_policy_loss_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t grads);
 size_t pspo_preference_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t R, int32_t P, int32_t grads);

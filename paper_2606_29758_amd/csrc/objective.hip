@@ -1161,7 +1161,7 @@ inline int way_of(int64_t N, int64_t d, bool grads) {
 inline int64_t pass_groups(int64_t N, int64_t d, int64_t V) {
   const int64_t parts = (d + 32 * kPassWaves - 1) / (32 * kPassWaves);
   const int64_t per_cu = parts > 4 && N <= 32 ? 1 : pass_per_cu((int)parts);
-  const int64_t blocks = (V + kPassRows - 1) / kPassRows, one = 256 / ((N + kPassRows - 1) / kPassRows);
+  const int64_t blocks = (V + kPassRows - 1) / kPassRows, one = 256 / ((std::max<int64_t>(N, 1) + kPassRows - 1) / kPassRows);
   const int64_t most = std::min(one * per_cu, std::max(one, blocks / 4)) / kNumXcd * kNumXcd;
   return std::min(blocks, most);
 }
@@ -1213,12 +1213,16 @@ bool sizes_fit(int64_t N, int64_t d, int64_t V) {
   return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab && N <= kMostRows &&
          N * d <= kMostEntries && N * V <= kMostEntries && V * d <= kMostEntries;
 }
-// Enough for any call of up to N rows: 16, 32, 48 and 64 may take more than a few rows more do.
+// Enough for any call of up to N rows (16, 32, 48 and 64 may take more than a few rows more do), with
+// gradients for the calls without them too.
 size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
   if (!sizes_fit(N, d, V)) return 0;
-  int64_t most = layout_of(N, d, V, k, R, P, grads).total;
-  for (int64_t few = kPassRows; few <= kSkinnyTokens; few += kPassRows)
-    if (few < N) most = std::max(most, layout_of(few, d, V, k, R, P, grads).total);
+  int64_t most = 0;
+  for (const bool with : {false, grads}) {
+    most = std::max(most, layout_of(N, d, V, k, R, P, with).total);
+    for (int64_t few = kPassRows; few <= kSkinnyTokens; few += kPassRows)
+      if (few < N) most = std::max(most, layout_of(few, d, V, k, R, P, with).total);
+  }
   return (size_t)most;
 }
 

@@ -161,7 +161,12 @@ def run_distill(N, d, V, seed=0, k=5, T=1.0, masked=0.2, f32=False, weights=True
 
 SIZES = [(1, 8, 1), (1, 64, 2), (1, 200, 4099), (2, 8, 7), (3, 64, 64), (16, 128, 65), (17, 200, 255), (33, 72, 2048),
          (63, 136, 2049), (64, 64, 2050), (65, 8, 9), (65, 64, 1000), (127, 520, 257), (129, 64, 4099), (257, 264, 512),
-         (300, 72, 130), (513, 64, 2113), (1025, 40, 321)]
+         (300, 72, 130), (513, 64, 2113), (1025, 40, 321),
+         # every width that the single pass is built for, its widest and past it, 1 to 4 work-groups of 16 rows
+         (5, 256, 60), (9, 392, 70), (20, 520, 333), (16, 1032, 100), (33, 1544, 45), (50, 2056, 40), (12, 2568, 90),
+         (40, 3080, 33), (64, 3584, 50), (17, 3584, 1000), (3, 3592, 33), (40, 3600, 70),
+         # tiles split along K, 256 x 256 tiles, rows by waves
+         (70, 2048, 300), (300, 1024, 700), (2100, 72, 6000), (2300, 136, 515), (4200, 16, 90)]
 
 
 @pytest.mark.parametrize("N,d,V", SIZES)
@@ -199,13 +204,14 @@ def test_distill_lists(kw):
     run_distill(**dict(dict(N=150, d=64, V=500, seed=8), **kw))
 
 
-@pytest.mark.parametrize("N,T", [(40, 1.0), (150, 1.0), (150, 0.25), (300, 0.05)])
-def test_targets_far_below_the_largest_logit(N, T):
+@pytest.mark.parametrize("N,d,T", [(5, 64, 1.0), (40, 64, 1.0), (20, 3592, 1.0), (150, 64, 1.0), (150, 64, 0.25),
+                                   (300, 64, 0.05), (2050, 64, 0.25)])
+def test_targets_far_below_the_largest_logit(N, d, T):
     """Logits of some hundred times the temperature: groups of entries that pass their row's reference, down to
     rows whose target has no weight left."""
-    run_policy(N, 64, 1000, seed=1, wide=30.0, T=T, kl="k1")
-    run_preference(N, 64, 1000, seed=2, wide=30.0, T=T, beta=0.01)
-    run_distill(N, 64, 1000, seed=3, wide=30.0, T=T, k=3)
+    run_policy(N, d, 1000, seed=1, wide=30.0, T=T, kl="k1")
+    run_preference(N, d, 1000, seed=2, wide=30.0, T=T, beta=0.01)
+    run_distill(N, d, 1000, seed=3, wide=30.0, T=T, k=3)
 
 
 @pytest.mark.parametrize("N", [20, 200])
