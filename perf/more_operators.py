@@ -167,7 +167,10 @@ def _own(s):
                                   1.0 / N, logp_ref=s["ref"], kl_coef=c["coef"], kl=c["kl"], **kw)
         more = [o["logp_new"]]
     elif c["op"] == "pref":
-        o = objective.preference_loss(s["h"], s["w"], s["target"], s["cu"], s["chosen"], s["rejected"], N, c["beta"],
+        cu = s["cu"]
+        if c["R"] > N:   # offsets that may leave the rows out: those of the sequences that they are counted in
+            cu = torch.searchsorted(s["seq"], torch.arange(c["R"] + 1, dtype=torch.int32, device=DEV), out_int32=True)
+        o = objective.preference_loss(s["h"], s["w"], s["target"], cu, s["chosen"], s["rejected"], N, c["beta"],
                                       1.0 / c["P"], logp_ref=s["ref"], weight=s["weight"], kind=c["kind"],
                                       smoothing=c["smooth"], average=c["average"], **kw)
         more = [o["logp_new"], o["seq_ratio"]]
