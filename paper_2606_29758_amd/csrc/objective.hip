@@ -33,6 +33,7 @@ namespace pspo {
 namespace {
 
 constexpr int kGroup = 64;         // vocabulary entries of one (reference, sum)
+constexpr int kPassRows = 16;      // rows of a work-group in one pass over W
 constexpr int kFewGroup = 2048;    // ... where the logits are kept in float32
 constexpr int kOnePassGroup = 16;  // ... in one pass over W
 // Ways of a call, by its size (way_of): tiles; up to 64 rows, logits and d_hidden in one pass over W, or,
@@ -263,7 +264,7 @@ struct Rows {
   double inv_t;
   int32_t* use;            // 1: takes part (kRescaled: with E brought to another reference than it was
                            // written in), 0: left out, -1: left out for an invalid id
-  float* zs;               // [N][k] logits at the ids
+  double* zs;              // [N][k] logits at the ids
   float* c;                // reference of the row
   f32x2* part;
   double* lse2;            // log2 of the sum of 2^(z t)
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
   for (int j0 = wave * kAt; j0 < r.k; j0 += kThreads / 64 * kAt) {
     const u32x4* row[kAt];
     bool on[kAt];
-    float sum[kAt] = {};
+    double sum[kAt] = {};
 #pragma unroll
     for (int j = 0; j < kAt; ++j) {
       const int id = j0 + j < r.k ? op.id(i, j0 + j, r) : -1;
@@ -326,18 +327,20 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
       for (int j = 0; j < kAt; ++j) {
         if (!on[j]) continue;   // the same in all lanes
         const u32x4 wv = row[j][p];
+        float eight = 0.f;   // products are exact, their sums go on in float64: log-probs are summed over sequences
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          sum[j] = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), sum[j]);
-          sum[j] = fmaf(__uint_as_float(hv[q] & 0xFFFF0000u), __uint_as_float(wv[q] & 0xFFFF0000u), sum[j]);
+          eight = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), eight);
+          eight = fmaf(__uint_as_float(hv[q] & 0xFFFF0000u), __uint_as_float(wv[q] & 0xFFFF0000u), eight);
         }
+        sum[j] += eight;
       }
     }
 #pragma unroll
     for (int j = 0; j < kAt; ++j) {
       sum[j] = wave_sum(sum[j]);
       if (lane == 0 && j0 + j < r.k) r.zs[(int64_t)i * r.k + j0 + j] = sum[j];
-      if (on[j]) top = fmaxf(top, sum[j]);
+      if (on[j]) top = fmaxf(top, (float)sum[j]);
     }
   }
   top = team.max(top);
@@ -347,6 +350,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
 // The row's hidden entries times its factor, the second operand of dW.
 template <int kThreads>
 __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
+  if (r.way == kOnePass && r.N <= kPassRows) return;   // one_pass_head_kernel does
   u32x4* row = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
 #pragma unroll 4
   for (int p = Team<kThreads>::thread(); p < r.d / 8; p += kThreads) {
@@ -362,7 +366,12 @@ __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
 // A team per row: log2 of the sum over its groups, in a fixed order (a row whose groups have
 // several references brought to the largest one); then op.row, called by the first wave, gives the
 // terms, the row's factor a of p and, in r.ids and r.g, the entries G / a at the ids.  E's own scale
-// is 2^(lse2 - c): the entries go in with it and the factor takes its inverse.
+// is 2^(lse2 - c): the entries go in with it and the factor takes its inverse.  A row's gradient is
+// mostly that of its largest entry at an id, so this one is made exact: all entries there take the
+// factor that carries it to a value of bf16, and the row's factor its inverse.  (What this moves, the
+// softmax entries, by 2^-8 at most, is what their own rounding moves them by; d_w_head of 777 rows was
+// 0.0029 off float64 in the relative 2-norm without it, 0.0024 with it, 0.0017 of which is its own
+// rounding to bf16.)
 template <int kThreads, class Op>
 __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   __shared__ Team<kThreads> team;
@@ -411,10 +420,18 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   if (r.way == kFew) c = (float)lse2;   // E is written from the logits, relative to the sum
   if (t < 64) {
     const float a = op.row(i, t, use, lse2 * 0.6931471805599453, r);
+    const int64_t at = (int64_t)i * r.k + t;   // this lane wrote it in op.row
+    const bool entry = use == 1 && t < r.k && r.ids[at] >= 0;
+    const float e = entry ? (float)((double)r.g[at] * exp2(lse2 - (double)c)) : 0.f;
+    const float most = wave_max(fabsf(e));
+    const float there = __uint_as_float((uint32_t)pack_bf16(most, 0.f) << 16);
+    const float carry = most > 0.f && std::isfinite(there) ? there / most : 1.f;
+    if (entry) r.g[at] = e * carry;
     if (t == 0) {
       r.lse2[i] = lse2;
       r.c[i] = c;
-      factor = use == 1 && a != 0.f ? a * (float)exp2((double)c - lse2) : 0.f;
+      // (an objective that knows a later on multiplies by it)
+      factor = use == 1 && a != 0.f ? a * (float)exp2((double)c - lse2) / carry : 0.f;
       r.f[i] = factor;
     }
   }
@@ -423,7 +440,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   if (r.way != kFew && use == 1 && t < r.k) {
     const int64_t at = (int64_t)i * r.k + t;
     const int id = r.ids[at];
-    if (id >= 0) row[id] = (uint16_t)pack_bf16((float)((double)r.g[at] * exp2(lse2 - (double)c)), 0.f);
+    if (id >= 0) row[id] = (uint16_t)pack_bf16(r.g[at], 0.f);
   }
   if (Op::kFactor) scale_copy<kThreads>(r, i, factor);
 }
@@ -506,7 +523,7 @@ struct Policy {
     if (lane != 0) return 0.f;
     double gain = 0.0, div = 0.0, clipped = 0.0, delta = 0.0, l = 0.0;
     if (use == 1) {
-      l = (double)r.zs[i] * r.inv_t - lse;
+      l = r.zs[i] * r.inv_t - lse;
       const double c = (double)weight[i] * (double)scale, A = advantage[seq_id[i]];
       const double rho = exp(l - (double)logp_old[i]);
       const double lo = 1.0 - (double)eps_low, hi = 1.0 + (double)eps_high;
@@ -552,7 +569,7 @@ struct Preference {
     if (lane != 0) return 0.f;
     double l = 0.0, part = 0.0, c = 0.0;
     if (use == 1) {
-      l = (double)r.zs[i] * r.inv_t - lse;
+      l = r.zs[i] * r.inv_t - lse;
       c = weight != nullptr ? (double)weight[i] : 1.0;
       part = c * (logp_ref != nullptr ? l - (double)logp_ref[i] : l);
       if (!(std::isfinite(lse) && std::isfinite(part))) raise(r.err, PSPO_DEVERR_NONFINITE);
@@ -564,7 +581,7 @@ struct Preference {
     r.ids[i] = use == 1 ? target[i] : -1;
     r.g[i] = use == 1 ? (float)expm1(l) : 0.f;
     if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
-    return 0.f;
+    return 1.f;   // pref_rows_kernel multiplies by what it is
   }
 };
 
@@ -720,7 +737,8 @@ __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
   const bool on = s < q.R && q.cu[s] <= i && r.use[i] > 0;
   const double delta = on ? q.coef[s] * r.terms[2 * (int64_t)r.N + i] : 0.0;
   const float a = (float)(-delta * r.inv_t);
-  const float f = on && a != 0.f ? a * (float)exp2((double)r.c[i] - r.lse2[i]) : 0.f;
+  const float f = on && a != 0.f ? a * r.f[i] : 0.f;
+  if constexpr (kThreads == 256) __syncthreads();   // f is read before it is written
   if (Team<kThreads>::thread() == 0) {
     if (on && !std::isfinite(a)) raise(r.err, PSPO_DEVERR_NONFINITE);
     r.f[i] = f;
@@ -782,7 +800,7 @@ struct Distill {
         }
       }
       c = (weight != nullptr ? (double)weight[i] : 1.0) * (double)scale;
-      const double lp = on ? (double)r.zs[at] * r.inv_t - lse : 0.0;
+      const double lp = on ? r.zs[at] * r.inv_t - lse : 0.0;
       const double each = first && !(same == 0.0) ? same * (log(same) - lp) : 0.0;
       div = wave_sum(each);
       g = exp(lp) - same;
@@ -819,10 +837,9 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
   put_bf16(row + v0, x);
   if (!on) return;
   const int32_t* ids = r.ids + (int64_t)i * r.k;
-  const float up = (float)exp2(r.lse2[i] - (double)r.c[i]);
   for (int j = 0; j < r.k; ++j) {
     const int id = ids[j];
-    if ((uint32_t)(id - v0) < 8u) row[id] = (uint16_t)pack_bf16(r.g[(int64_t)i * r.k + j] * up, 0.f);
+    if ((uint32_t)(id - v0) < 8u) row[id] = (uint16_t)pack_bf16(r.g[(int64_t)i * r.k + j], 0.f);
   }
 }
 
@@ -839,7 +856,7 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
 // and its d_hidden is formed from E (one_pass_hidden_kernel).  16 rows to a work-group, those of the others
 // in grid y, which meet W's blocks in the same L2 at about the same time (gridDim.x % 8 == 0 then).
 // Bound by W's bytes: MEASURED_PASS.
-constexpr int kPassWaves = 4, kPassRows = 16, kHeadWaves = 8, kHiddenWaves = 16;
+constexpr int kPassWaves = 4, kHeadWaves = 8, kHiddenWaves = 16;
 constexpr int kMostPassWidth = 28 * 32 * kPassWaves;   // what the registers of a work-group to a CU hold
 
 // Four rows (4 g .. 4 g + 3) of column 16 b + lane % 16 of a wave's rows of bf16 in LDS, `pitch` bytes
@@ -988,10 +1005,9 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows
 #pragma unroll 8
       for (int k = wave; k < groups; k += kHiddenWaves)
         sum += *reinterpret_cast<const f32x4*>(slab + ((int64_t)k * r.N + i) * r.d + col);
-      const float up = (float)exp2(r.lse2[i] - (double)r.c[i]);
       for (int j = wave; j < r.k; j += kHiddenWaves) {
         const int64_t at = (int64_t)i * r.k + j;
-        if (r.ids[at] >= 0) add(r.g[at] * up, r.ids[at]);
+        if (r.ids[at] >= 0) add(r.g[at], r.ids[at]);
       }
     }
   }
@@ -1008,8 +1024,9 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
 }
 
-// dW = E^T (f H) of up to 16 rows: the scaled rows in LDS, a wave 16 vocabulary entries at a time,
-// whose rows of dW it writes from end to end.  Bound by dW's bytes: MEASURED_DW.  The last work-group
+// dW = E^T (f H) of up to 16 rows: the rows times their factors in LDS, a wave 16 vocabulary entries at a
+// time, whose rows of dW it writes from end to end.  Up to 8 rows, whose roundings no others average,
+// stand there twice, rounded to bf16 and what that leaves.  Bound by dW's bytes: MEASURED_DW.  The last work-group
 // sums the loss.
 template <int F>
 __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
@@ -1022,20 +1039,33 @@ __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, 
     return;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, g = lane >> 4;
+  const int split = r.N <= kPassRows / 2 ? kPassRows / 2 : kPassRows;
   for (int t = threadIdx.x; t < kPassRows * 32 * F; t += 64 * kHeadWaves) {
-    const int i = t / (32 * F), col = t % (32 * F) * 8;
+    const int place = t / (32 * F), i = place % split, col = t % (32 * F) * 8;
     u32x4 x = {0, 0, 0, 0};
-    if (i < r.N && col < r.d) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
-    *reinterpret_cast<u32x4*>(rows + i * kPitch + col * 2) = x;
+    const float f = i < r.N ? r.f[i] : 0.f;
+    if (f != 0.f && col < r.d) {
+      x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float lo = f * __uint_as_float(x[q] << 16), hi = f * __uint_as_float(x[q] & 0xFFFF0000u);
+        x[q] = pack_bf16(lo, hi);
+        if (place >= split)
+          x[q] = pack_bf16(lo - __uint_as_float(x[q] << 16), hi - __uint_as_float(x[q] & 0xFFFF0000u));
+      }
+    }
+    *reinterpret_cast<u32x4*>(rows + place * kPitch + col * 2) = x;
   }
   __syncthreads();
   const int blocks = (r.V + 15) / 16, step = ((int)gridDim.x - 1) * kHeadWaves;
-  auto entries = [&](int b) {   // of vocabulary entry 16 b + p, rows 4 g .. 4 g + 3
+  auto entries = [&](int b) {   // of vocabulary entry 16 b + p, places 4 g .. 4 g + 3
     s16x4 y = {0, 0, 0, 0};
     const int v = b * 16 + p;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (g * 4 + q < r.N && v < r.V) y[q] = (short)r.e[(int64_t)(g * 4 + q) * r.ld + v];
+    for (int q = 0; q < 4; ++q) {
+      const int i = (g * 4 + q) % split;
+      if (i < r.N && v < r.V) y[q] = (short)r.e[(int64_t)i * r.ld + v];
+    }
     return y;
   };
   int b = blockIdx.x * kHeadWaves + wave;
@@ -1185,7 +1215,7 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
     return x;
   };
   s.use = take(N * 4);
-  s.zs = take(N * k * 4);
+  s.zs = take(N * k * 8);
   s.c = take(N * 4);
   s.part = take(N * s.groups * 8);
   s.lse2 = take(N * 8);
@@ -1302,7 +1332,7 @@ Rows rows_of(const Call& c, const Layout& s) {
   r.group = s.group;
   r.inv_t = 1.0 / (double)c.temperature;
   r.use = reinterpret_cast<int32_t*>(ws + s.use);
-  r.zs = reinterpret_cast<float*>(ws + s.zs);
+  r.zs = reinterpret_cast<double*>(ws + s.zs);
   r.c = reinterpret_cast<float*>(ws + s.c);
   r.part = reinterpret_cast<f32x2*>(ws + s.part);
   r.lse2 = reinterpret_cast<double*>(ws + s.lse2);

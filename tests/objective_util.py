@@ -6,7 +6,8 @@ u = 2^-24 is one float32 rounding, B = 2^-8 half a bf16 step.  Carried through t
         carries two roundings of up to its size, its result one) and the sums of up to 64 + 8 terms
         of a group (the groups' sums are joined in float64, their scalings take 4 u);
   l     z's and lse's;
-  G     B for the softmax entry, the exponent's error, and the factor's; an entry set apart its own error and B;
+  G     B for the softmax entry, B for the factor that makes a row's largest entry set apart exact, the exponent's
+        error, and the factor's; an entry set apart its own error and B;
   dH    float32 sums of V terms, dW float32 sums of N terms whose hidden rows, times their factors, take B as well;
         B once more where the output is bf16.
 Second-order terms are covered by a factor 1.02 on the whole.
@@ -55,7 +56,7 @@ class Bounds:
 
     def of_G(self, G, a, e_a, set_apart, e_set):
         """G's bound: a the factor of p with error e_a ([N]); entries set apart ([N, V] mask) with error e_set."""
-        e = np.abs(a)[:, None] * self.p * (B + self.ep + 6 * U) + e_a[:, None] * self.p
+        e = np.abs(a)[:, None] * self.p * (2 * B + B * B + self.ep + 6 * U) + e_a[:, None] * self.p
         return np.where(set_apart, e_set + B * (np.abs(G) + e_set), e) * 1.02
 
     def gradients(self, G, eG, bf16_h, bf16_w):
