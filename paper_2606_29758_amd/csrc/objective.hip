@@ -855,7 +855,8 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
 // reference, as in the tiles; their row's accumulators are then of no use (no other row's are touched),
 // and its d_hidden is formed from E (one_pass_hidden_kernel).  16 rows to a work-group, those of the others
 // in grid y, which meet W's blocks in the same L2 at about the same time (gridDim.x % 8 == 0 then).
-// Bound by W's bytes: MEASURED_PASS.
+// Bound by W's bytes: 16 rows, d = 3584, V = 152064 292 us, 1 row, d = 1536, V = 151936 127, 3.7 TB/s
+// each (torch's sum over as many bytes reads 4.0).
 constexpr int kPassWaves = 4, kHeadWaves = 8, kHiddenWaves = 16;
 constexpr int kMostPassWidth = 28 * 32 * kPassWaves;   // what the registers of a work-group to a CU hold
 
@@ -1026,8 +1027,9 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows
 
 // dW = E^T (f H) of up to 16 rows: the rows times their factors in LDS, a wave 16 vocabulary entries at a
 // time, whose rows of dW it writes from end to end.  Up to 8 rows, whose roundings no others average,
-// stand there twice, rounded to bf16 and what that leaves.  Bound by dW's bytes: MEASURED_DW.  The last work-group
-// sums the loss.
+// stand there twice, rounded to bf16 and what that leaves.  Bound by dW's bytes: 16 rows,
+// d = 3584, V = 152064 215 us, 5.1 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
+// work-group sums the loss.
 template <int F>
 __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
                                                                         LossSum loss) {
@@ -1171,6 +1173,113 @@ struct EpiGrad {
   }
 };
 
+// dW = E^T (f H) of 17 to 64 rows, whose tiles would be all way in and out (one stage of K): a work-group
+// keeps 256 columns of the scaled rows in its registers, 64 to a wave as the matrix instructions take
+// them, and goes over its share of the vocabulary, 64 entries a step; their E comes through LDS, the
+// next step's on the way meanwhile.  KS: steps of 32 rows.  The last row of the grid sums the loss.
+// Whole calls against tiles: 24 rows, d = 3584, V = 152064 770 -> 719 us, 160, 46996 52 -> 47.  (From 65
+// rows on both gradients' tiles in one launch are as good or better: 160 rows, d = 3584 1,106 / 1,183.)
+constexpr int kStreamPerCu = 2;
+template <int KS>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kStreamPerCu, kStreamPerCu)))
+void stream_head_kernel(Rows r, EpiGrad out) {
+  constexpr int kPitch = 64 * 2 + 16;   // odd in 16 bytes
+  __shared__ __attribute__((aligned(16))) unsigned char tile[2][KS * 32 * kPitch];
+  __shared__ double sh[64];
+  if (blockIdx.y == gridDim.y - 1) {
+    if (blockIdx.x == 0) out.loss.run(sh);
+    return;
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = lane & 15, g = lane >> 4;
+  const int col0 = (blockIdx.y * 4 + wave) * 64;   // this wave's columns of H
+  // eight rows (8 g .. 8 g + 7 of step ks) of column 16 b + p
+  auto operand = [&](const unsigned char* rows, int ks, int b) {
+    union {
+      s16x4 half[2];
+      bf16x8 v;
+    } u;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      u.half[q] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(rows + (ks * 32 + g * 8 + q * 4 + (p >> 2)) * kPitch + b * 32 + (p & 3) * 8));
+    return u.v;
+  };
+  // the rows' columns to registers, a wave's 64 at a time through the tile
+  bf16x8 h[KS][4];
+  for (int turn = 0; turn < 4; ++turn) {
+    for (int t = threadIdx.x; t < KS * 32 * 8; t += 256) {
+      const int i = t / 8, col = (blockIdx.y * 4 + turn) * 64 + t % 8 * 8;
+      u32x4 x = {0, 0, 0, 0};
+      if (i < r.N && col < r.d) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
+      *reinterpret_cast<u32x4*>(tile[0] + i * kPitch + t % 8 * 16) = x;
+    }
+    __syncthreads();
+    if (turn == wave) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) h[ks][b] = operand(tile[0], ks, b);
+    }
+    __syncthreads();
+  }
+  const int tiles = (r.V + 63) / 64, step = gridDim.x;
+  u32x4 e[KS];   // this thread's pieces of the next tile
+  auto load = [&](int at) {
+#pragma unroll
+    for (int q = 0; q < KS; ++q) {
+      const int i = q * 32 + threadIdx.x / 8;
+      e[q] = u32x4{0, 0, 0, 0};
+      if (i < r.N) e[q] = *reinterpret_cast<const u32x4*>(r.e + (int64_t)i * r.ld + at * 64 + threadIdx.x % 8 * 8);
+    }
+  };
+  int buf = 0;
+  if ((int)blockIdx.x < tiles) load(blockIdx.x);
+  for (int at = blockIdx.x; at < tiles; at += step) {
+#pragma unroll
+    for (int q = 0; q < KS; ++q)
+      *reinterpret_cast<u32x4*>(tile[buf] + (q * 32 + threadIdx.x / 8) * kPitch + threadIdx.x % 8 * 16) = e[q];
+    if (at + step < tiles) load(at + step);
+    stage_barrier<63>();   // (the loads stay in flight; a wave writes this half again behind the next barrier)
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const bf16x8 y = operand(tile[buf], ks, b);
+#pragma unroll
+        for (int a = 0; a < 4; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[ks][a], y, acc[a][b], 0, 0, 0);
+      }
+    buf ^= 1;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int v = at * 64 + b * 16 + p;
+      if (out.f32) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int col = col0 + a * 16 + g * 4;
+          if (v >= r.V || col >= r.d) continue;
+          f32x4* to = reinterpret_cast<f32x4*>(static_cast<float*>(out.out) + (int64_t)v * r.d + col);
+          *to = out.add ? *to + acc[a][b] : acc[a][b];
+        }
+      } else {
+#pragma unroll
+        for (int a = 0; a < 4; a += 2) {
+          const f32x4 x = acc[a][b], y = acc[a + 1][b];
+          const u32x4 o = eight_rows(u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])},
+                                     u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
+          const int col = col0 + a * 16 + eight_rows_at(lane);
+          if (v < r.V && col < r.d)
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out.out) + (int64_t)v * r.d + col) = o;
+        }
+      }
+    }
+  }
+}
+
 __global__ __launch_bounds__(256) void fill_zero_kernel(u32x4* __restrict__ p, int64_t n) {
   for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = u32x4{0, 0, 0, 0};
 }
@@ -1180,9 +1289,13 @@ constexpr int kMostVocab = 1 << 21, kMostWidth = 1 << 20;   // a tile's rows sta
 constexpr int kMostRows = 1 << 26;
 constexpr int64_t kMostEntries = int64_t(1) << 36;            // of a matrix: fewer tiles than a launch holds
 
+// One pass over W for each 16 rows against the tiles: 40 rows, d = 3584, V = 152064 927 us a call, 65
+// rows by tiles 966; 64 of them in one pass 1,097; 64 rows, 1536, 151936 456, 65 by tiles 455; 160, 46996
+// 55, by tiles 63.  Few: without gradients, or wider than one pass is built for.
 inline int way_of(int64_t N, int64_t d, bool grads) {
   if (N > kSkinnyTokens) return kTiles;
-  return d <= kMostPassWidth && grads ? kOnePass : kFew;
+  if (!grads || d > kMostPassWidth) return kFew;
+  return N <= 3 * kPassRows || d <= 12 * 32 * kPassWaves ? kOnePass : kTiles;
 }
 // Work-groups of one pass for each 16 rows: as many as run at once, but with four blocks of the
 // vocabulary to each beyond one a CU (their sums are read again: 5 rows, d = 376, V = 22700 47 us with
@@ -1227,11 +1340,9 @@ Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t 
   s.z = take(way == kFew ? N * s.ld * 4 : 0);
   s.e = take(way == kFew && !grads ? 0 : N * s.ld * 2);
   int64_t slab = way == kOnePass ? pass_groups(N, d, V) * N * d * 4 : way == kTiles ? slab_reserve(V, N, (int)d) : 0;
-  if (grads && (way != kOnePass || N > kPassRows)) {
-    const int64_t M[3] = {way == kOnePass ? 0 : d, d, 0}, C[3] = {N, V, 0};
-    const int64_t nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
-    if (way == kOnePass) slab = std::max(slab, jobs_reserve(M, C, nk));
-    else slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
+  if (grads && way != kOnePass) {
+    const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0}, nk[3] = {(V + kRowK - 1) / kRowK, (N + kRowK - 1) / kRowK, 0};
+    slab = std::max({slab, jobs_reserve(M, C, nk), slab_reserve(d, N, (int)V), slab_reserve(d, V, (int)N)});
   }
   s.slab = take(slab);
   s.seqs = take(R * 3 * 8);
@@ -1265,8 +1376,8 @@ Plan plan_square(int64_t M, int64_t N, int K) {
 // Both as one launch (against two, us a call: 1 row, d = 1536, V = 151936 411 / 472; 1,301, 1000, 50257 492 /
 // 528; 4,096, 3584, 152064 10,602 / 10,818; 4,999 of the same 13,024 / 12,871).  One alone goes as a product,
 // whose last round is split along K (8,192 rows, d = 3584: 13,536 against 14,105).
-JobPlan plan_gradients(int64_t N, int64_t d, int64_t V, bool dh) {
-  const int64_t M[3] = {dh ? d : 0, d, 0}, C[3] = {N, V, 0};
+JobPlan plan_gradients(int64_t N, int64_t d, int64_t V) {
+  const int64_t M[3] = {d, d, 0}, C[3] = {N, V, 0};
   const int nk[3] = {(int)((V + kRowK - 1) / kRowK), (int)((N + kRowK - 1) / kRowK), 0};
   const JobPlan big = plan_jobs(M, C, nk, 256), small = plan_jobs(M, C, nk, 128);
   return big.us <= small.us ? big : small;
@@ -1378,6 +1489,18 @@ int one_pass_head(const Call& c, const Rows& r, const LossSum& loss) {
   });
 }
 
+int stream_head(const Call& c, const Rows& r, const EpiGrad& out) {
+  const int64_t tiles = ((int64_t)c.V + 63) / 64, chunks = (c.d + 255) / 256;
+  return pass_width<1, 2>((c.N + 31) / 32, [&](auto ks) {
+    // as many work-groups as run at once, those of one share of the vocabulary on one XCD
+    const int64_t most = std::max<int64_t>(256 * kStreamPerCu / chunks / kNumXcd * kNumXcd, kNumXcd);
+    hipLaunchKernelGGL(stream_head_kernel<ks.value>, dim3((unsigned)std::min(tiles, most), (unsigned)chunks + 1), dim3(256),
+                       0, c.stream, r, out);
+    PSPO_LAUNCHED("stream_head_kernel", c.stream);
+    return (int)PSPO_OK;
+  });
+}
+
 // Steps 1 to 3 (N > 0).
 template <class Op>
 int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
@@ -1448,11 +1571,13 @@ int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss)
                          shape(r.copy, r.copy, c.d, c.d, r.e, s.ld, c.V, c.N), RowShape{}};
   const EpiGrad o[3] = {{c.dh, r.f, c.d, c.d, c.N, (c.flags & PSPO_OBJ_DH_F32) != 0, 0, loss},
                         {c.dw, nullptr, c.d, c.d, c.V, f32, add, LossSum{}}, EpiGrad{}};
-  if (r.way == kOnePass)
-    return run_jobs(plan_gradients(c.N, c.d, c.V, false), g, o, reinterpret_cast<unsigned char*>(slab), "objective_dw",
-                    c.stream);
+  if (r.way == kOnePass) {
+    EpiGrad head = o[1];
+    head.loss = loss;
+    return stream_head(c, r, head);
+  }
   if (both)
-    return run_jobs(plan_gradients(c.N, c.d, c.V, true), g, o, reinterpret_cast<unsigned char*>(slab), "objective_gradients",
+    return run_jobs(plan_gradients(c.N, c.d, c.V), g, o, reinterpret_cast<unsigned char*>(slab), "objective_gradients",
                     c.stream);
   if (c.dh != nullptr)
     return product<true, false>(g[0], plan_square(c.d, c.N, c.V), c.N, o[0], slab, "objective_dh", c.stream);
