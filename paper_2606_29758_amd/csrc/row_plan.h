@@ -9,7 +9,7 @@
 namespace pspo {
 
 // How a product of M x N entries over nk stages is covered: tiles of 256 x 256 (one
-// work-group to a CU), 128 x 128 (two) or 128 x 64 (three), the first `whole` of them launched
+// work-group to a CU; some epilogues have 160, 192 and 224 columns too), 128 x 128 (two) or 128 x 64 (three), the first `whole` of them launched
 // as they are and the rest in `parts` parts of K (parts = 1: all are whole).
 struct Plan {
   int tile, tile_n, tiles_m, tiles_n, whole, parts;
@@ -28,9 +28,10 @@ inline Plan plan_tile(int64_t M, int64_t N, int nk, int tile, int tile_n, bool d
   p.tiles_m = (int)((M + tile - 1) / tile);
   p.tiles_n = (int)((N + tile_n - 1) / tile_n);
   const int64_t total = (int64_t)p.tiles_m * p.tiles_n, slots = tile == 256 ? 256 : tile_n == 128 ? 512 : 768;
-  const double extra = tile == 256 ? (dh ? 55 : 20) : tile_n == 128 ? (dh ? 16 : 10) : 6;
-  const double stage = tile == 256 ? 1.45 : tile_n == 128 ? 1.1 : 0.9;
-  const double single = tile == 256 ? 1.45 : tile_n == 128 ? 0.7 : 0.5;
+  const double extra = tile == 256 ? (dh ? 55 : 20) * (tile_n / 256.0) : tile_n == 128 ? (dh ? 16 : 10) : 6;
+  const double big = 1.45 - 0.0028 * (256 - tile_n);   // 256 x 160 to 256 x 256
+  const double stage = tile == 256 ? big : tile_n == 128 ? 1.1 : 0.9;
+  const double single = tile == 256 ? big : tile_n == 128 ? 0.7 : 0.5;
   auto time = [&](int64_t groups, int stages, double per_tile) {
     const int64_t turns = (groups + slots - 1) / slots, rest = groups - (turns - 1) * slots;
     const double last = rest <= 256 ? single : stage;

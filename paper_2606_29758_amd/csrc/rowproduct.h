@@ -206,7 +206,12 @@ int launch(const RowShape& g, const Plan& p, const Epi<Op>& epi, const char* nam
   hipLaunchKernelGGL((row_gemm_kernel<BM, BN, RING, kOuterA, kOuterB, Op::kPair, Epi<Op>>), grid, dim3(256), 0, \
                      stream, g, epi)
   if (p.tile == 256) {
-    PSPO_ROW(8, 8, 2);
+    if constexpr (!kOuterB && HasTile<Op>::value) {   // (the pieces of row_pieces take 128 columns at a time)
+      if (p.tile_n == 160) PSPO_ROW(8, 5, 2);
+      if (p.tile_n == 192) PSPO_ROW(8, 6, 2);
+      if (p.tile_n == 224) PSPO_ROW(8, 7, 2);
+    }
+    if (p.tile_n == 256) PSPO_ROW(8, 8, 2);
   } else if (p.tile_n == 128) {
     if (deep) PSPO_ROW(4, 4, kDeep);
     else PSPO_ROW(4, 4, 2);
