@@ -21,8 +21,8 @@
  * Precision: logits and softmax sums are float32 sums of exact bf16 products,
  * per-row terms and the loss float64.  The softmax entries (with the entries of G at
  * the ids in their places) and, for d_w_head, the hidden rows times their factors are
- * rounded to bf16, the matrix cores' operand type, once each; sums of the gradient
- * products are float32.
+ * rounded to bf16, the matrix cores' operand type, once each (a row's largest entry at
+ * an id is kept exact); sums of the gradient products are float32.
  *
  * Memory: the softmax entries of all N rows are kept in the workspace, 2 bytes each
  * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time.
