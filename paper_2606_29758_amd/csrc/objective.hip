@@ -24,6 +24,7 @@
 // V = 152064, and 142 of 585 at 2,501, 520, 32003).  c is a logit of the row, so its largest E is
 // 2^-1/2 at least; a group that would pass 2^32 takes its own reference, and its row is brought to
 // one reference in finalize (a power of two: exact).
+#include <cfloat>
 #include <cmath>
 
 #include "objective_plan.h"
@@ -365,7 +366,7 @@ __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
 // factor that carries it to a value of bf16, and the row's factor its inverse.  (What this moves, the
 // softmax entries, by 2^-8 at most, is what their own rounding moves them by; d_w_head of 777 rows was
 // 0.0029 off float64 in the relative 2-norm without it, 0.0024 with it, 0.0017 of which is its own
-// rounding to bf16.)
+// rounding to bf16.)  Below the normal numbers bf16 is too coarse for that, and no entry matters.
 template <int kThreads, class Op>
 __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   __shared__ Team<kThreads> team;
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
     const float e = entry ? (float)((double)r.g[at] * exp2(lse2 - (double)c)) : 0.f;
     const float most = wave_max(fabsf(e));
     const float there = __uint_as_float((uint32_t)pack_bf16(most, 0.f) << 16);
-    const float carry = most > 0.f && std::isfinite(there) ? there / most : 1.f;
+    const float carry = most >= FLT_MIN && std::isfinite(there) ? there / most : 1.f;
     if (entry) r.g[at] = e * carry;
     if (t == 0) {
       r.lse2[i] = lse2;

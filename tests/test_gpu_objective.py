@@ -220,3 +220,22 @@ def test_everything_masked(N):
     for o in (run_policy(N, 64, 300, masked=1.1), run_preference(N, 64, 300, masked=1.1),
               run_distill(N, 64, 300, masked=1.1)):
         assert not o["d_hidden"].any() and not o["d_w_head"].any()
+
+
+@pytest.mark.parametrize("N", [5, 40, 150, 2100])
+def test_entries_below_the_normal_numbers(N):
+    """A row whose largest entry set apart is exp(-100): p is 1 and q is 1 at the first id (logit 0, the others' at most
+    -100), q is exp(-1000) = 0 at the second.  Every factor is at most 1 and every |w| at most 120, so no gradient passes
+    V 120 (exp(-100) + exp(-100)) < 1e-38."""
+    V, d = 40, 8
+    w = torch.zeros(V, d, dtype=BF, device="cuda")
+    w[1, 0], w[2:, 0] = -100, -120
+    h = torch.zeros(N, d, dtype=BF, device="cuda")
+    h[:, 0] = 1
+    ids = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").repeat(N, 1)
+    t = torch.tensor([[0.0, -1000.0]], device="cuda").repeat(N, 1)
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o = objective.distill_loss(h, w, ids, t, N, 1.0 / N, err_flag=err)
+    assert int(err) == 0 and float(o["loss"]) == 0 and bool((o["kl"] == 0).all())
+    for g in (o["d_hidden"], o["d_w_head"]):
+        assert bool((g.abs() < 1e-37).all())   # (a NaN is not)
