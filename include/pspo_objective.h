@@ -79,7 +79,7 @@ size_t pspo_distill_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t k, 
  *  target     device, int32 [N]; logp_old, weight: device, float32 [N]; seq_id: device,
  *             int32 [N] in [0, R); advantage: device, float32 [R].
  *  logp_ref   device, float32 [N], or NULL (then kl_coef must be 0).
- *  kl_kind    PSPO_KL_K1, _K2 or _K3;  temperature > 0.
+ *  kl_kind    PSPO_KL_K1, _K2 or _K3;  temperature > 0;  eps_low, eps_high in [0, 1).
  *  flags      PSPO_OBJ_DH_F32 | PSPO_OBJ_DW_F32 | PSPO_ACCUMULATE_DW or 0.
  *  loss       device, float64 [1] out.
  *  d_hidden   device, [N, d] out, or NULL (not wanted).
@@ -91,7 +91,7 @@ size_t pspo_distill_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t k, 
  *  err_flag   device, int32 [1] or NULL: PSPO_DEVERR_TARGET, PSPO_DEVERR_SEQ_ID,
  *             PSPO_DEVERR_NONFINITE (a value of a row that takes part is not finite).
  *  workspace  device, 256-byte aligned; contents on entry ignored.
- * Sizes: N <= 2^26, V <= 2^21, d <= 2^20, and N d, N V, V d <= 2^36 (PSPO_ERR_UNSUPPORTED
+ * Sizes: N <= 2^23, V <= 2^21, d <= 2^20, and N d, N V, V d <= 2^36 (PSPO_ERR_UNSUPPORTED
  * beyond).  Device pointers of matrices 16-byte aligned.
  */
 int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
@@ -120,7 +120,8 @@ int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, con
  *             (PSPO_PREF_SIGMOID only).
  *  seq_ratio  device, float32 [R] out, or NULL: ratio_r.
  *  margin     device, float32 [P] out, or NULL: beta (ratio[chosen] - ratio[rejected]).
- *  Other arguments as above; flags also PSPO_PREF_AVERAGE.  P = 0 and R = 0 are valid.
+ *  Other arguments as above; flags also PSPO_PREF_AVERAGE.  P = 0 and R = 0 are valid;
+ *  R <= 2^23 and R P <= 2^36 (PSPO_ERR_UNSUPPORTED beyond).
  */
 int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
                             const float* logp_ref, const float* weight, const int32_t* cu_seqlens,

@@ -865,8 +865,7 @@ __device__ __forceinline__ s16x4 transposed(const unsigned char* rows, int pitch
 template <int F>
 __global__ __attribute__((amdgpu_flat_work_group_size(64 * kPassWaves, 64 * kPassWaves),
                           amdgpu_waves_per_eu(pass_per_cu(F), pass_per_cu(F))))
-void one_pass_kernel(Rows r, const uint16_t* __restrict__ w,
-Exponent exponent, float* __restrict__ slab) {
+void one_pass_kernel(Rows r, const uint16_t* __restrict__ w, Exponent exponent, float* __restrict__ slab) {
   constexpr int kPitch = 64 * F + 16;   // odd in 16 bytes: a column's 16 rows lie in different banks
   __shared__ __attribute__((aligned(16))) unsigned char rows[kPassWaves][kPassRows * kPitch];
   __shared__ f32x4 sums[2][kPassWaves][64];
@@ -979,9 +978,8 @@ Exponent exponent, float* __restrict__ slab) {
 // d_hidden of a row from the work-groups' sums and the rows of W at its ids, in a fixed order; of a row
 // with entries past its reference from its E.  Grid (ceil(d / 256), N): 4 columns a thread, each wave a
 // sixteenth of the terms.
-__global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows r, const uint16_t* __restrict__ w,
-                                                              const float* __restrict__ slab, int groups, void* out,
-                                                              int f32) {
+__global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(
+    Rows r, const uint16_t* __restrict__ w, const float* __restrict__ slab, int groups, void* out, int f32) {
   __shared__ f32x4 sh[kHiddenWaves][64];
   const int i = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 256 + lane * 4;
   const float f = r.f[i];
@@ -1021,7 +1019,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(Rows
 // dW = E^T (f H) of up to 16 rows: the rows times their factors in LDS, a wave 16 vocabulary entries at a
 // time, whose rows of dW it writes from end to end.  Up to 8 rows, whose roundings no others average,
 // stand there twice, rounded to bf16 and what that leaves.  Bound by dW's bytes: 16 rows,
-// d = 3584, V = 152064 215 us, 5.1 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
+// d = 3584, V = 152064 222 us, 4.9 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
 // work-group sums the loss.
 template <int F>
 __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
@@ -1298,7 +1296,7 @@ int check(const Call& c) {
   PSPO_REQUIRE(c.d > 0 && c.V > 0, PSPO_ERR_INVALID_ARG, "d and V must be > 0");
   PSPO_REQUIRE(c.d % 8 == 0, PSPO_ERR_UNSUPPORTED, "d must be a multiple of 8");
   PSPO_REQUIRE(sizes_fit(c.N, c.d, c.V), PSPO_ERR_UNSUPPORTED,
-               "N is at most 2^26, d 2^20, V 2^21, and N d, N V and V d 2^36");
+               "N is at most 2^23, d 2^20, V 2^21, and N d, N V and V d 2^36");
   PSPO_REQUIRE((c.flags & ~c.allowed) == 0, PSPO_ERR_INVALID_ARG, "unknown flag bits");
   PSPO_REQUIRE((c.flags & PSPO_ACCUMULATE_DW) == 0 || (c.flags & PSPO_OBJ_DW_F32) != 0, PSPO_ERR_INVALID_ARG,
                "accumulating needs a float32 d_w_head");
@@ -1366,9 +1364,9 @@ int pass_width(int parts, const Run& run) {
 }
 int one_pass(const Call& c, const Rows& r, float* slab) {
   return pass_width<2, 4, 8, 12, 16, 20, 24, 28>((c.d + 32 * kPassWaves - 1) / (32 * kPassWaves), [&](auto f) {
-    hipLaunchKernelGGL(one_pass_kernel<f.value>, dim3((unsigned)pass_groups(c.N, c.d, c.V), (unsigned)((c.N + kPassRows - 1) / kPassRows)),
-                       dim3(64 * kPassWaves), 0, c.stream, r,
-                       c.w, exponent_of(r), slab);
+    hipLaunchKernelGGL(one_pass_kernel<f.value>,
+                       dim3((unsigned)pass_groups(c.N, c.d, c.V), (unsigned)((c.N + kPassRows - 1) / kPassRows)),
+                       dim3(64 * kPassWaves), 0, c.stream, r, c.w, exponent_of(r), slab);
     PSPO_LAUNCHED("one_pass_kernel", c.stream);
     return (int)PSPO_OK;
   });
@@ -1451,8 +1449,8 @@ int backward(const Call& c, const Layout& s, const Rows& r, const LossSum& loss)
   }
   if (r.way == kOnePass && c.dh != nullptr) {
     hipLaunchKernelGGL(one_pass_hidden_kernel, dim3((unsigned)((c.d + 255) / 256), (unsigned)c.N),
-                       dim3(64 * kHiddenWaves), 0, c.stream, r, c.w, (const float*)slab, (int)pass_groups(c.N, c.d, c.V), c.dh,
-                       (c.flags & PSPO_OBJ_DH_F32) != 0);
+                       dim3(64 * kHiddenWaves), 0, c.stream, r, c.w, (const float*)slab,
+                       (int)pass_groups(c.N, c.d, c.V), c.dh, (c.flags & PSPO_OBJ_DH_F32) != 0);
     PSPO_LAUNCHED("one_pass_hidden_kernel", c.stream);
   }
   if (r.way == kOnePass && c.dw == nullptr) return PSPO_OK;
@@ -1488,7 +1486,7 @@ size_t pspo_policy_loss_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t
   return pspo::workspace_size(N, d, V, 1, 0, 0, grads != 0);
 }
 size_t pspo_preference_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t R, int32_t P, int32_t grads) {
-  if (R < 0 || P < 0) return 0;
+  if (R < 0 || P < 0 || !pspo::pairs_fit(R, P)) return 0;
   return pspo::workspace_size(N, d, V, 1, R, P, grads != 0);
 }
 size_t pspo_distill_workspace_bytes(int32_t N, int32_t d, int32_t V, int32_t k, int32_t grads) {
@@ -1550,6 +1548,7 @@ int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, cons
                err_flag, workspace, workspace_bytes, stream};
   if (int rc = check(c)) return rc;
   PSPO_REQUIRE(R >= 0 && P >= 0, PSPO_ERR_INVALID_ARG, "R and P must be >= 0");
+  PSPO_REQUIRE(pairs_fit(R, P), PSPO_ERR_UNSUPPORTED, "R is at most 2^23, R P 2^36");
   PSPO_REQUIRE(kind == PSPO_PREF_SIGMOID || kind == PSPO_PREF_SQUARED, PSPO_ERR_INVALID_ARG, "unknown kind");
   PSPO_REQUIRE(std::isfinite(beta) && beta > 0.f && std::isfinite(1.f / beta), PSPO_ERR_INVALID_ARG,
                "beta must be positive and finite");

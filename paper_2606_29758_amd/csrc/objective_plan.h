@@ -20,7 +20,7 @@ constexpr int kMostPassWidth = 28 * 32 * kPassWaves;   // what the registers of 
 constexpr int pass_per_cu(int parts) { return parts <= 4 ? 4 : (parts <= 12 ? 2 : 1); }
 
 constexpr int kMostVocab = 1 << 21, kMostWidth = 1 << 20;   // a tile's rows stay below 2^31 bytes
-constexpr int kMostRows = 1 << 26;
+constexpr int kMostRows = 1 << 23;   // 256 threads to each: a launch holds fewer than 2^32
 constexpr int64_t kMostEntries = int64_t(1) << 36;            // of a matrix: fewer tiles than a launch holds
 
 // One pass over W for each 16 rows against the tiles: 40 rows, d = 3584, V = 152064 927 us a call, 65
@@ -38,7 +38,8 @@ inline int way_of(int64_t N, int64_t d, bool grads) {
 inline int64_t pass_groups(int64_t N, int64_t d, int64_t V) {
   const int64_t parts = (d + 32 * kPassWaves - 1) / (32 * kPassWaves);
   const int64_t per_cu = parts > 4 && N <= 32 ? 1 : pass_per_cu((int)parts);
-  const int64_t blocks = (V + kPassRows - 1) / kPassRows, one = 256 / ((std::max<int64_t>(N, 1) + kPassRows - 1) / kPassRows);
+  const int64_t blocks = (V + kPassRows - 1) / kPassRows;
+  const int64_t one = 256 / ((std::max<int64_t>(N, 1) + kPassRows - 1) / kPassRows);
   const int64_t most = std::min(one * per_cu, std::max(one, blocks / 4)) / kNumXcd * kNumXcd;
   return std::min(blocks, most);
 }
@@ -61,8 +62,10 @@ inline int64_t forward_reserve(int64_t V, int64_t N, int64_t d) {
   int64_t bytes = slab_reserve(V, N, (int)d);
   const int64_t most = std::min<int64_t>((d + kRowK - 1) / kRowK / 4, 32);   // parts, plan_tile's limits
   if (most < 2) return bytes;
-  for (const int64_t columns : kForwardColumns)
-    bytes = std::max(bytes, std::min<int64_t>(((V + 255) / 256) * ((N + columns - 1) / columns), 256) * most * 256 * columns * 4);
+  for (const int64_t columns : kForwardColumns) {
+    const int64_t tiles = ((V + 255) / 256) * ((N + columns - 1) / columns);
+    bytes = std::max(bytes, std::min<int64_t>(tiles, 256) * most * 256 * columns * 4);
+  }
   return std::min(bytes, kSlabBytes);
 }
 
@@ -111,6 +114,8 @@ inline bool sizes_fit(int64_t N, int64_t d, int64_t V) {
   return N >= 0 && d > 0 && V > 0 && d % 8 == 0 && d <= kMostWidth && V <= kMostVocab && N <= kMostRows &&
          N * d <= kMostEntries && N * V <= kMostEntries && V * d <= kMostEntries;
 }
+// Sequences (256 threads to each) and pairs; every sequence looks at every pair.
+inline bool pairs_fit(int64_t R, int64_t P) { return R <= 1 << 23 && R * P <= kMostEntries; }
 // Enough for any call of up to N rows (16, 32, 48 and 64 may take more than a few rows more do), with
 // gradients for the calls without them too.
 inline size_t workspace_size(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {

@@ -9,8 +9,9 @@
 namespace pspo {
 
 // How a product of M x N entries over nk stages is covered: tiles of 256 x 256 (one
-// work-group to a CU; some epilogues have 160, 192 and 224 columns too), 128 x 128 (two) or 128 x 64 (three), the first `whole` of them launched
-// as they are and the rest in `parts` parts of K (parts = 1: all are whole).
+// work-group to a CU; some epilogues have 160, 192 and 224 columns too), 128 x 128 (two) or
+// 128 x 64 (three), the first `whole` of them launched as they are and the rest in `parts`
+// parts of K (parts = 1: all are whole).
 struct Plan {
   int tile, tile_n, tiles_m, tiles_n, whole, parts;
   double us;

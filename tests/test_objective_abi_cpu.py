@@ -68,8 +68,8 @@ def distill(lib, **kw):
 SHARED = [
     (dict(N=-1), INVALID, "N must"), (dict(d=0), INVALID, "d and V"), (dict(V=0), INVALID, "d and V"),
     (dict(d=12), UNSUPPORTED, "multiple of 8"), (dict(d=(1 << 20) + 8), UNSUPPORTED, "at most"),
-    (dict(V=(1 << 21) + 1), UNSUPPORTED, "at most"), (dict(N=(1 << 26) + 1), UNSUPPORTED, "at most"),
-    (dict(N=1 << 26, V=1 << 11), UNSUPPORTED, "at most"), (dict(N=1 << 26, d=1 << 11), UNSUPPORTED, "at most"),
+    (dict(V=(1 << 21) + 1), UNSUPPORTED, "at most"), (dict(N=(1 << 23) + 1, d=8, V=8), UNSUPPORTED, "at most"),
+    (dict(N=1 << 23, d=8, V=(1 << 13) + 8), UNSUPPORTED, "at most"), (dict(N=1 << 23, d=(1 << 13) + 8, V=8), UNSUPPORTED, "at most"),
     (dict(V=1 << 21, d=1 << 16), UNSUPPORTED, "at most"),
     (dict(flags=1), INVALID, "float32 d_w_head"), (dict(flags=2), INVALID, "flag"), (dict(flags=1 << 20), INVALID, "flag"),
     (dict(T=0.0), INVALID, "temperature"), (dict(T=-1.0), INVALID, "temperature"), (dict(T=NAN), INVALID, "temperature"),
@@ -109,6 +109,16 @@ def test_preference_refusals(lib, kw, text):
     _says(lib, pref(lib, **kw), INVALID, text)
 
 
+@pytest.mark.parametrize("R,P", [((1 << 23) + 1, 1), (1 << 23, (1 << 13) + 1), (1 << 20, 1 << 20)])
+def test_preference_limits(lib, R, P):
+    """What a launch cannot hold, or sequences that would look at more pairs than a call should."""
+    assert objective.preference_workspace_bytes(4, 64, 100, R, P) == 0
+    _says(lib, pref(lib, R=R, P=P), UNSUPPORTED, "R is at most")
+    for r, p in ((1 << 23, 1 << 13), (1, 2 ** 31 - 1)):
+        assert objective.preference_workspace_bytes(4, 64, 100, r, p) > 0
+        _says(lib, pref(lib, R=r, P=p, n=100), WORKSPACE, "too small")
+
+
 @pytest.mark.parametrize("kw,want,text", [
     (dict(k=0), UNSUPPORTED, "k must"), (dict(k=65), UNSUPPORTED, "k must"), (dict(k=-1), UNSUPPORTED, "k must"),
     (dict(ids=None), INVALID, "null"), (dict(t=None), INVALID, "null"), (dict(ids=A + 2), INVALID, "misaligned"),
@@ -120,7 +130,7 @@ def test_distill_refusals(lib, kw, want, text):
 def test_workspace_sizes(lib):
     """0 for what the calls refuse; never less for fewer rows; without gradients no more than with them."""
     p, q, k = objective.policy_loss_workspace_bytes, objective.preference_workspace_bytes, objective.distill_workspace_bytes
-    for bad in (lambda: p(-1, 64, 100), lambda: p(4, 12, 100), lambda: p(4, 64, 0), lambda: p(1 << 26, 64, 1 << 21),
+    for bad in (lambda: p(-1, 64, 100), lambda: p(4, 12, 100), lambda: p(4, 64, 0), lambda: p(1 << 23, 64, 1 << 21), lambda: p((1 << 23) + 1, 8, 8),
                 lambda: q(4, 64, 100, -1, 1), lambda: q(4, 64, 100, 1, -1), lambda: k(4, 64, 100, 0), lambda: k(4, 64, 100, 65)):
         assert bad() == 0
     for d, V in ((64, 100), (1536, 151936), (520, 32003), (8, 1)):
