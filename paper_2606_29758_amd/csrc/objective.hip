@@ -533,7 +533,8 @@ struct Policy {
         if (kl_coef != 0.f) delta += (double)kl_coef * c * (kl == PSPO_KL_K1 ? 1.0 : kl == PSPO_KL_K2 ? u : -expm1(-u));
       }
       const double loss = kl_coef != 0.f ? (double)kl_coef * div - gain : -gain;
-      if (!(std::isfinite(lse) && std::isfinite((float)rho) && std::isfinite(loss) && std::isfinite((float)delta)))
+      if (!(std::isfinite(lse) && std::isfinite((float)rho) && std::isfinite(loss) &&
+            std::isfinite((float)(delta * r.inv_t))))
         raise(r.err, PSPO_DEVERR_NONFINITE);
     }
     const int64_t n = r.N;

@@ -244,6 +244,30 @@ def test_values_that_are_not_finite(N):
             assert int(err) == 16 and not o["loss"].isfinite(), (kind, spoil)
 
 
+@pytest.mark.parametrize("N", [12, 40, 150, 2100])
+def test_gradients_past_float32(N):
+    """Logits of 0, so that the log-probs and losses are small; at a temperature of 1e-36 the factors of p (weight 1 to 2
+    times 0.01, or beta 0.1 and scale 0.5, times 1e36) pass 3.5e38 from weights of 1e6 on."""
+    for kind in KINDS:
+        x = Inputs(N, 64, 300)
+        x.h.zero_()
+        x.old.fill_(-np.log(300))
+        x.adv.fill_(1)
+        x.cu = torch.tensor([0, N // 2, N, N, N], dtype=I4, device="cuda")
+        x.chosen, x.rejected = (torch.tensor([v] * x.P, dtype=I4, device="cuda") for v in (0, 1))
+        for many, want in ((1.0, 0), (1e6, 16)):
+            err = _flag()
+            x.weight.mul_(many)
+            if kind == "pref":   # equal weights: the log ratios of N // 2 and of N - N // 2 rows differ by one row's at most
+                x.weight.fill_(many)
+                x.ref.fill_(-np.log(300))
+            if kind == "distill":
+                x.t.fill_(0)
+            call = dict(temperature=1e-36, err_flag=err)
+            o = x.call(kind, **call)
+            assert int(err) == want and bool(o["loss"].isfinite()), (kind, many)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_streams(kind):
     """Calls on several streams at once, each with a workspace of its own, give the bits of calls one after another."""
