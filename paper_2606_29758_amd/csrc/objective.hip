@@ -276,16 +276,17 @@ __device__ __forceinline__ void raise(int32_t* err, int bit) {
 }
 
 // ---- 1. gather -------------------------------------------------------------------------
-// A team per row; its waves take four ids each in turn, whose rows of W are read beside the hidden
+// A team per row; kLanes lanes take an id each in turn, whose row of W is read beside the hidden
 // row.  Op::use(i, lane, r): as Rows::use, the same in all lanes; Op::id(i, j, r): the row's
-// j-th id or -1.
-template <int kThreads, class Op>
+// j-th id or -1.  Lists go 16 lanes to an id (2,501 rows of 50 ids, d = 520 25 us; 32 lanes 28, a wave
+// for four ids together 50), one to four ids a wave each.
+template <int kThreads, int kLanes, class Op>
 __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16_t* __restrict__ hidden,
                                                      const uint16_t* __restrict__ w) {
   __shared__ Team<kThreads> team;
-  const int i = team.row(), t = team.thread(), lane = t % 64, wave = t / 64;
+  const int i = team.row(), t = team.thread();
   if (i >= r.N) return;
-  const int use = op.use(i, lane, r);
+  const int use = op.use(i, t % 64, r);
   if (t == 0) r.use[i] = use;
   if (t < r.k) {   // (finalize writes what becomes of them)
     const int64_t at = (int64_t)i * r.k + t;
@@ -303,40 +304,28 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
     if (t == 0) r.c[i] = 0.f;
     return;
   }
-  constexpr int kAt = 4;
   float top = -INFINITY;
-  for (int j0 = wave * kAt; j0 < r.k; j0 += kThreads / 64 * kAt) {
-    const u32x4* row[kAt];
-    bool on[kAt];
-    double sum[kAt] = {};
-#pragma unroll
-    for (int j = 0; j < kAt; ++j) {
-      const int id = j0 + j < r.k ? op.id(i, j0 + j, r) : -1;
-      on[j] = id >= 0;
-      row[j] = reinterpret_cast<const u32x4*>(w + (int64_t)(on[j] ? id : 0) * r.d);
-    }
-#pragma unroll 4
-    for (int p = lane; p < pieces; p += 64) {
-      const u32x4 hv = from[p];
-#pragma unroll
-      for (int j = 0; j < kAt; ++j) {
-        if (!on[j]) continue;   // the same in all lanes
-        const u32x4 wv = row[j][p];
+  for (int j = t / kLanes; j < r.k; j += kThreads / kLanes) {
+    const int id = op.id(i, j, r);
+    double sum = 0.0;
+    if (id >= 0) {   // the same in the kLanes
+      const u32x4* row = reinterpret_cast<const u32x4*>(w + (int64_t)id * r.d);
+#pragma unroll 8
+      for (int p = t % kLanes; p < pieces; p += kLanes) {
+        const u32x4 hv = from[p], wv = row[p];
         float eight = 0.f;   // products are exact, their sums go on in float64: log-probs are summed over sequences
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           eight = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), eight);
           eight = fmaf(__uint_as_float(hv[q] & 0xFFFF0000u), __uint_as_float(wv[q] & 0xFFFF0000u), eight);
         }
-        sum[j] += eight;
+        sum += eight;
       }
-    }
 #pragma unroll
-    for (int j = 0; j < kAt; ++j) {
-      sum[j] = wave_sum(sum[j]);
-      if (lane == 0 && j0 + j < r.k) r.zs[(int64_t)i * r.k + j0 + j] = sum[j];
-      if (on[j]) top = fmaxf(top, (float)sum[j]);
+      for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+      top = fmaxf(top, (float)sum);
     }
+    if (t % kLanes == 0) r.zs[(int64_t)i * r.k + j] = sum;
   }
   top = team.max(top);
   if (t == 0) r.c[i] = rintf(top * (float)(r.inv_t * 1.4426950408889634));
@@ -1400,10 +1389,14 @@ template <class Op>
 int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   unsigned char* ws = static_cast<unsigned char*>(c.workspace);
   float *z = reinterpret_cast<float*>(ws + s.z), *slab = reinterpret_cast<float*>(ws + s.slab);
-  if (c.N < kTeamRows || c.k > 4)   // (a wave's turn takes four ids: 663 rows of lists 97 -> 121 us by waves)
-    hipLaunchKernelGGL((gather_kernel<256, Op>), dim3((unsigned)c.N), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
-  else
-    hipLaunchKernelGGL((gather_kernel<64, Op>), dim3((unsigned)((c.N + 3) / 4)), dim3(256), 0, c.stream, r, op, c.hidden, c.w);
+  auto gather = [&](auto threads, auto lanes) {
+    constexpr int kThreads = decltype(threads)::value, kLanes = decltype(lanes)::value;
+    hipLaunchKernelGGL((gather_kernel<kThreads, kLanes, Op>), dim3((unsigned)(((int64_t)c.N * kThreads + 255) / 256)),
+                       dim3(256), 0, c.stream, r, op, c.hidden, c.w);
+  };
+  if (c.k > 4) gather(std::integral_constant<int, 256>{}, std::integral_constant<int, 16>{});
+  else if (c.N < kTeamRows) gather(std::integral_constant<int, 256>{}, std::integral_constant<int, 64>{});
+  else gather(std::integral_constant<int, 64>{}, std::integral_constant<int, 64>{});
   PSPO_LAUNCHED("gather_kernel", c.stream);
   if (r.way == kOnePass) {
     if (int rc = one_pass(c, r, slab)) return rc;
