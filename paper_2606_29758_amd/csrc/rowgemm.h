@@ -130,6 +130,19 @@ struct RowSide {
     }
   }
 
+  // The same lanes on another tile.
+  __device__ __forceinline__ void move(const RowOperand& o, int tile) {
+    static_assert(!kPair, "rows of one matrix");
+    if constexpr (kOuter) {
+      col = (int64_t)tile * kTile * 2;
+      base[0] = base[1] = reinterpret_cast<const unsigned char*>(o.p[0]) + col;
+    } else {
+      const int64_t row0 = (int64_t)tile * kTile;
+      range = (uint32_t)(min((int64_t)o.rows - row0, (int64_t)kTile) * rows_bytes);
+      base[0] = reinterpret_cast<const unsigned char*>(o.p[0]) + row0 * rows_bytes;
+    }
+  }
+
   // Descriptor, scalar offset and lane addend of the stage to load next.
   struct Stage {
     u32x4 rsrc;
@@ -222,17 +235,28 @@ constexpr int kRowLds = kRing * (32 * BM + 32 * BN) * kRowK * 2;
 // Epilogue: epi.apply<BM, BN>(acc, tm, tn, wm, wn, lane, wave_lds, slab); a wave has its own part
 // of the LDS; slab = part * (tiles of the launch) + tile.  Lane l's accumulator [i][j][r] is
 // C(tm 32 BM + (wm BM + i) 16 + (l / 16) 4 + r, tn 32 BN + (wn BN + j) 16 + l % 16).
-template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, bool kPairA, class Epi>
+// kChain: also the tiles of work-groups bid + groups, bid + 2 groups, ... (groups % 8 == 0), whose first
+// stages take the places of the empty loads past the end: the loads of a tile run on while the one before
+// is stored.  For one segment of kRing stages or more, whole (g.parts 1), and an epilogue that leaves the
+// LDS alone.
+template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, bool kPairA, bool kChain = false, class Epi>
 __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi, int bid, int part,
-                                              unsigned char* lds) {
+                                              unsigned char* lds, int groups = 0) {
   using A = RowSide<BM, kOuterA, kPairA>;
   using B = RowSide<BN, kOuterB, false>;
   constexpr int kStage = A::kBytes + B::kBytes;
 
   const int index = row_index(g, bid);
   if (index < 0) return;
-  int tm, tn;
+  int tm, tn, next_m = 0, next_n = 0;
   row_tile_at(g, g.tile0 + index, tm, tn);
+  bool more = false;   // there is a next tile
+  auto look = [&] {
+    const int then = row_index(g, bid += groups);
+    more = then >= 0;
+    if (more) row_tile_at(g, g.tile0 + then, next_m, next_n);
+  };
+  if constexpr (kChain) look();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   A sa;
@@ -287,52 +311,81 @@ __device__ __forceinline__ void row_gemm_tile(const RowShape& g, const Epi& epi,
   constexpr int kEvery = kMfma / kLoads, kApart = kMfma / kReads;   // MFMAs per load, per read
   static_assert(kReads <= kMfma && kLoads <= kMfma, "one read and one load at most after each MFMA");
   uint32_t cur = 0;
-  for (int t = kb; t < ke; ++t) {
-    const uint32_t nxt = cur == (kRing - 1) * kStage ? 0u : cur + kStage;
-    // first half: K 0 .. 31 of this stage; its other half is read
-    repeat<kMfma>([&](auto ic) {
-      constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
-      mfma_agpr(acc[m][n], fa[0][m], fb[0][n]);
-      if constexpr (i % kApart == 0 && i / kApart < kReads) {
-        constexpr int r = i / kApart;
-        if constexpr (r < B::kReads) sb.template read<r, 1>(fb[1], lds + cur + A::kBytes);
-        else sa.template read<r - B::kReads, 1>(fa[1], lds + cur);
-      }
-      // where the next stage to load lies
-      if constexpr (i == kMfma - 6) step();
-      if constexpr (i == kMfma - 5) sa.next(ga, over, left, ahead < ke);
-      if constexpr (i == kMfma - 3) sb.next(gb, over, left, ahead < ke);
+  while (true) {
+    for (int t = kb; t < ke; ++t) {
+      const uint32_t nxt = cur == (kRing - 1) * kStage ? 0u : cur + kStage;
+      // first half: K 0 .. 31 of this stage; its other half is read
+      repeat<kMfma>([&](auto ic) {
+        constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
+        mfma_agpr(acc[m][n], fa[0][m], fb[0][n]);
+        if constexpr (i % kApart == 0 && i / kApart < kReads) {
+          constexpr int r = i / kApart;
+          if constexpr (r < B::kReads) sb.template read<r, 1>(fb[1], lds + cur + A::kBytes);
+          else sa.template read<r - B::kReads, 1>(fa[1], lds + cur);
+        }
+        // where the next stage to load lies
+        if constexpr (i == kMfma - 6) {
+          step();
+          if constexpr (kChain)
+            if (over && more) {
+              sa.move(g.a, next_m);
+              sb.move(g.b, next_n);
+            }
+        }
+        if constexpr (i == kMfma - 5) sa.next(ga, over, left, ahead < ke || (kChain && more));
+        if constexpr (i == kMfma - 3) sb.next(gb, over, left, ahead < ke || (kChain && more));
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      // every wave is done with this stage's buffer, and the next stage has landed
+      row_barrier<(kRing - 2) * kLoads>();
+      settle(ga, gb);
+      repeat<kMfma>([&](auto ic) {
+        constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
+        mfma_agpr(acc[m][n], fa[1][m], fb[1][n]);
+        if constexpr (i % kApart == 0 && i / kApart < kReads) {
+          constexpr int r = i / kApart;
+          if constexpr (r < B::kReads) sb.template read<r, 0>(fb[0], lds + nxt + A::kBytes);
+          else sa.template read<r - B::kReads, 0>(fa[0], lds + nxt);
+        }
+        if constexpr (i % kEvery == kEvery - 1 && i / kEvery < kLoads) {
+          constexpr int q = i / kEvery;
+          if constexpr (q < A::kLoads) sa.template load<q>(ga, lds0 + cur, wave);
+          else sb.template load<q - A::kLoads>(gb, lds0 + cur + A::kBytes, wave);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      cur = nxt;
+      // The accumulators are readable some passes after the last MFMA, which the compiler
+      // does not know of: the wait stands inside the loop, before any copy that it makes of
+      // them on the way out.
+      if (t + 1 == ke) mfma_drain();
       __builtin_amdgcn_sched_barrier(0);
-    });
-    // every wave is done with this stage's buffer, and the next stage has landed
-    row_barrier<(kRing - 2) * kLoads>();
-    settle(ga, gb);
-    repeat<kMfma>([&](auto ic) {
-      constexpr int i = decltype(ic)::value, m = i / BN, n = i % BN;
-      mfma_agpr(acc[m][n], fa[1][m], fb[1][n]);
-      if constexpr (i % kApart == 0 && i / kApart < kReads) {
-        constexpr int r = i / kApart;
-        if constexpr (r < B::kReads) sb.template read<r, 0>(fb[0], lds + nxt + A::kBytes);
-        else sa.template read<r - B::kReads, 0>(fa[0], lds + nxt);
-      }
-      if constexpr (i % kEvery == kEvery - 1 && i / kEvery < kLoads) {
-        constexpr int q = i / kEvery;
-        if constexpr (q < A::kLoads) sa.template load<q>(ga, lds0 + cur, wave);
-        else sb.template load<q - A::kLoads>(gb, lds0 + cur + A::kBytes, wave);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    });
-    cur = nxt;
-    // The accumulators are readable some passes after the last MFMA, which the compiler
-    // does not know of: the wait stands inside the loop, before any copy that it makes of
-    // them on the way out.
-    if (t + 1 == ke) mfma_drain();
-    __builtin_amdgcn_sched_barrier(0);
+    }
+
+    if constexpr (kChain) {
+      epi.template direct<BM, BN>(acc, tm, tn, wm, wn, lane);
+      if (!more) break;
+      tm = next_m;
+      tn = next_n;
+      ahead -= ke - kb;
+      look();
+      // written before the next tile's first MFMA by more than the wait states that the compiler does not
+      // know of
+      repeat<kMfma>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        acc[i / BN][i % BN] = f32x4{0.f, 0.f, 0.f, 0.f};
+        asm volatile("" : "+a"(acc[i / BN][i % BN]));
+      });
+      asm volatile("s_nop 7" : : : "memory");
+    } else {
+      break;
+    }
   }
 
   row_barrier<0>();   // the last (empty) loads have landed, every wave is done with the buffers
-  epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kRing * kStage / 4),
-                              part * g.count + index);
+  if constexpr (!kChain)
+    epi.template apply<BM, BN>(acc, tm, tn, wm, wn, lane, lds + wave * (kRing * kStage / 4),
+                                part * g.count + index);
 }
 
 // Work-groups of a CU (waves of a SIMD): what the LDS holds.
@@ -344,6 +397,14 @@ __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_pe
 void row_gemm_kernel(RowShape g, Epi epi) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
   row_gemm_tile<BM, BN, kRing, kOuterA, kOuterB, kPairA>(g, epi, blockIdx.x, blockIdx.y, lds);
+}
+
+// A work-group to a CU, each with one tile after another.
+template <int BM, int BN, int kRing, bool kOuterA, bool kOuterB, class Epi>
+__global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kRowGroups<BM, BN, kRing>)))
+void row_chain_kernel(RowShape g, Epi epi) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
+  row_gemm_tile<BM, BN, kRing, kOuterA, kOuterB, false, true>(g, epi, blockIdx.x, 0, lds, gridDim.x);
 }
 
 // Independent products in one launch, the first with A K-outer and B K-inner, the others with
@@ -358,7 +419,8 @@ struct RowJobs {
   Epi epi[kJobs];
   int blocks[kJobs];
 };
-template <int BM, int BN, int kRing, class Epi>
+// kChain: job 1 in chains of tiles, job 2 the tiles behind them.
+template <int BM, int BN, int kRing, bool kChain, class Epi>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kRowGroups<BM, BN, kRing>)))
 void row_jobs_kernel(RowJobs<Epi> jobs) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kRowLds<BM, BN, kRing>];
@@ -375,6 +437,12 @@ void row_jobs_kernel(RowJobs<Epi> jobs) {
     return;
   }
   bid -= jobs.blocks[0];
+  if constexpr (kChain) {
+    if (bid < jobs.blocks[1]) {
+      row_gemm_tile<BM, BN, kRing, true, true, false, true>(jobs.g[1], jobs.epi[1], bid, 0, lds, jobs.blocks[1]);
+      return;
+    }
+  }
   const int job = bid < jobs.blocks[1] ? 1 : 2;
   if (job == 2) bid -= jobs.blocks[1];
   const int per = (jobs.g[job].count + kNumXcd - 1) / kNumXcd * kNumXcd;

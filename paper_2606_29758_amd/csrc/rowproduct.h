@@ -113,6 +113,10 @@ struct Epi {
     if constexpr (kExtra) op.extra(lds);
   }
   template <int BM, int BN>
+  __device__ __forceinline__ void direct(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane) const {
+    op.template tile<BM, BN>(acc, tm, tn, wm, wn, lane);
+  }
+  template <int BM, int BN>
   __device__ __forceinline__ void apply(f32x4 (&acc)[BM][BN], int tm, int tn, int wm, int wn, int lane,
                                         unsigned char* lds, int index) const {
     if (slab.base != nullptr) put_slab(acc, tn, wm, wn, lane, index, slab);
@@ -198,15 +202,34 @@ int join_parts(const Op& op, const RowShape& g, int tile, int tile_n, const floa
   return PSPO_OK;
 }
 
+constexpr int kChainK = 32 * kRowK;   // longest K of the products that go in chains of tiles
 template <bool kOuterA, bool kOuterB, class Op>
 int launch(const RowShape& g, const Plan& p, const Epi<Op>& epi, const char* name, hipStream_t stream) {
   const dim3 grid((uint32_t)round_up(g.count, kNumXcd), (uint32_t)g.parts);
   const bool deep = deep_ring((int64_t)g.count * g.parts);
+  if constexpr (HasTile<Op>::value) {
+    // A work-group to a CU with tiles in turn, for the K where their way in and out counts: whole calls at
+    // 7,400 rows, d = 416, V = 21520 412 -> 393 us, 777, 1536, 151936 1,250 -> 1,240; with 56 stages work-groups
+    // of a tile each, taken when a CU is free, are better (4,096, 3584, 152064: 10,364 against 10,440).
+    if (p.tile == 256 && g.parts == 1 && g.count > 256 && g.segs == 1 && g.K > kRowK && g.K <= kChainK) {
+#define PSPO_CHAIN(BN)                                                                                     \
+  hipLaunchKernelGGL((row_chain_kernel<8, BN, 2, kOuterA, kOuterB, Epi<Op>>), dim3(256), dim3(256), 0, stream, g, epi)
+      if constexpr (!kOuterA) {
+        if (p.tile_n == 160) PSPO_CHAIN(5);
+        if (p.tile_n == 192) PSPO_CHAIN(6);
+        if (p.tile_n == 224) PSPO_CHAIN(7);
+      }
+      if (p.tile_n == 256) PSPO_CHAIN(8);
+#undef PSPO_CHAIN
+      PSPO_LAUNCHED(name, stream);
+      return PSPO_OK;
+    }
+  }
 #define PSPO_ROW(BM, BN, RING)                                                                                    \
   hipLaunchKernelGGL((row_gemm_kernel<BM, BN, RING, kOuterA, kOuterB, Op::kPair, Epi<Op>>), grid, dim3(256), 0, \
                      stream, g, epi)
   if (p.tile == 256) {
-    if constexpr (!kOuterB && HasTile<Op>::value) {   // (the pieces of row_pieces take 128 columns at a time)
+    if constexpr (!kOuterA && HasTile<Op>::value) {   // (the pieces of row_pieces take 128 columns at a time)
       if (p.tile_n == 160) PSPO_ROW(8, 5, 2);
       if (p.tile_n == 192) PSPO_ROW(8, 6, 2);
       if (p.tile_n == 224) PSPO_ROW(8, 7, 2);
@@ -266,12 +289,38 @@ int run_jobs(const JobPlan& p, const RowShape (&g)[3], const Op (&o)[3], unsigne
   }
   PSPO_REQUIRE(blocks < (int64_t(1) << 24), PSPO_ERR_UNSUPPORTED, "the products have more tiles than a launch holds");
   if (Epi<Op>::kExtra) ++blocks;
-  if (p.tile == 256)
-    hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
-  else if (deep_ring(blocks))
-    hipLaunchKernelGGL((row_jobs_kernel<4, 4, kDeep, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
-  else
-    hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, Epi<Op>>), dim3((uint32_t)blocks), dim3(256), 0, stream, jobs);
+  const dim3 threads(256);
+  bool chained = false;
+  if constexpr (HasTile<Op>::value) {
+    // The second of two products in chains of four tiles, all but its last two rounds (which fill the chip):
+    // whole calls at 777 rows, d = 1536, V = 151936 1,240 -> 1,229 us, 1,999 rows 2,591 -> 2,568 (chains of two
+    // 1,238 and 2,581).
+    constexpr int kLinks = 4, kBehind = 512;
+    RowShape &r = jobs.g[1], &rest = jobs.g[2];
+    if (p.tile == 256 && p.parts[1] == 1 && rest.count == 0 && r.count > 2 * kBehind && r.segs == 1 && r.K > kRowK &&
+        r.K <= kChainK) {
+      chained = true;
+      rest = r;
+      r.count -= kBehind;
+      rest.tile0 = r.count;
+      rest.count = kBehind;
+      jobs.epi[2] = jobs.epi[1];
+      blocks -= jobs.blocks[1];
+      jobs.blocks[1] = (int)round_up((r.count + kLinks - 1) / kLinks, kNumXcd);
+      jobs.blocks[2] = kBehind;
+      blocks += jobs.blocks[1] + jobs.blocks[2];
+      hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, true, Epi<Op>>), dim3((uint32_t)blocks), threads, 0, stream, jobs);
+    }
+  }
+  const dim3 grid((uint32_t)blocks);
+  if (chained) {   // launched above
+  } else if (p.tile == 256) {
+    hipLaunchKernelGGL((row_jobs_kernel<8, 8, 2, false, Epi<Op>>), grid, threads, 0, stream, jobs);
+  } else if (deep_ring(blocks)) {
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, kDeep, false, Epi<Op>>), grid, threads, 0, stream, jobs);
+  } else {
+    hipLaunchKernelGGL((row_jobs_kernel<4, 4, 2, false, Epi<Op>>), grid, threads, 0, stream, jobs);
+  }
   PSPO_LAUNCHED(name, stream);
   JoinJobs<Op> join{};
   int split = 0;

@@ -146,6 +146,41 @@ def test_head_gradient_added_to(kind, N, d, V):
     assert ((both.double() - (old.double() + alone.double())).abs() <= 2.0 ** -24 * (both.abs() + 1e-30)).all()
 
 
+@pytest.mark.parametrize("N,d,V,hidden,head", [
+    (2100, 72, 17003, True, True), (300, 1096, 60001, True, True), (300, 1096, 60001, False, True),
+    (130, 2040, 60001, True, True), (1301, 2040, 40001, True, True), (70000, 1024, 2000, True, False)])
+def test_tiles_in_chains(N, d, V, hidden, head):
+    """Sizes whose work-groups take several tiles in turn, every entry against the formulas in float64.
+
+    With B = 2^-8 for a rounding to bf16: a softmax entry takes one, its row's factor one, the scaled hidden row one; the
+    errors of a logit and of the log of the sum, (d + 2) 2^-24 sum |w h| + 2^-18 < 2^-8 each here, move p (and rho, which
+    is 1 up to that) by less than three more.  A gradient is off by at most 6 B (1.02 for the second order) of the sum of
+    its terms' sizes, and B of itself."""
+    h, w, target = matrices(N, d, V, 3)
+    g = torch.Generator("cuda").manual_seed(1)
+    weight = 1 + torch.rand(N, device="cuda", generator=g)
+    weight[::5] = 0
+    z = h.double() @ w.double().t()
+    lp = z.log_softmax(1)
+    del z
+    l = lp.gather(1, target.long()[:, None])[:, 0]
+    adv = torch.tensor([1.5], device="cuda")
+    o = objective.policy_loss(h, w, target, l.float(), weight, torch.zeros(N, dtype=I4, device="cuda"), adv, N, 0.2, 0.2, 1 / 64,
+                              want_hidden=hidden, want_head=head)
+    assert ((o["logp_new"] - l)[weight > 0].abs() < 2.0 ** -7).all()
+    G = lp.exp_()
+    G[torch.arange(N, device="cuda"), target.long()] -= 1
+    G *= (weight.double() * 1.5 / 64)[:, None]
+    size = G.abs()
+    B = 2.0 ** -8
+    if hidden:
+        want, terms = G @ w.double(), size @ w.double().abs()
+        assert ((o["d_hidden"].double() - want).abs() <= 6.12 * B * terms + B * want.abs()).all()
+    if head:
+        want, terms = G.t().contiguous() @ h.double(), size.t().contiguous() @ h.double().abs()
+        assert ((o["d_w_head"].double() - want).abs() <= 6.12 * B * terms + B * want.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", [BF, F4])
 @pytest.mark.parametrize("kind", KINDS)
 def test_no_rows(kind, dtype):
