@@ -10,7 +10,7 @@
 //
 // Schedule:
 //   1. gather: the rows that take part, copied (zeros for the others: a NaN there must not reach a
-//      sum over rows), the logits at the ids as float32 dot products, and from them the row's
+//      sum over rows), the logits at the ids, summed in float64, and from them the row's
 //      reference c, the nearest integer to the largest of them times s log2(e);
 //   2. product Z^T = W H^T; its epilogue writes E = 2^(s log2(e) z - c) in bf16 and, for each group
 //      of 64 vocabulary entries, the sum of the unrounded values;
