@@ -18,11 +18,14 @@
  * term, d_hidden row and per-token outputs are 0.  A row that has an invalid id
  * raises the error bit, takes no part either and has NaN in its per-token outputs.
  *
- * Precision: logits and softmax sums are float32 sums of exact bf16 products,
- * per-row terms and the loss float64.  The softmax entries (with the entries of G at
- * the ids in their places) and, for d_w_head, the hidden rows times their factors are
- * rounded to bf16, the matrix cores' operand type, once each (a row's largest entry at
- * an id is kept exact); sums of the gradient products are float32.
+ * Precision: logits and softmax sums are float32 sums of exact bf16 products (a logit
+ * at an id float32 sums of eight products each, added in float64; its entry joins the
+ * sum in float64 from that logit), per-row terms and the loss float64.  A log-prob is
+ * never positive, and 1 - p at an id keeps its relative accuracy as p goes to 1.  The
+ * softmax entries (with the entries of G at the ids in their places) and, for d_w_head,
+ * the hidden rows times their factors are rounded to bf16, the matrix cores' operand
+ * type, once each (a row's largest entry at an id is kept exact); sums of the gradient
+ * products are float32.
  *
  * Memory: the softmax entries of all N rows are kept in the workspace, 2 bytes each
  * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time.

@@ -5,17 +5,21 @@
 // the loss depends on row i through log p_i at a few ids (one, or a teacher's list), so its logit
 // gradient is G_i = a_i p_i with those entries replaced:
 //   log-prob l_i of one id o, delta_i = d loss / d l_i:  a_i = -s delta_i,
-//       G_io = s delta_i (1 - p_io) = -s delta_i expm1(l_i)  (no cancellation as p -> 1);
+//       G_io = s delta_i (1 - p_io);
 //   divergence from q_i with weight c_i:  a_i = s c_i,  G_ij = s c_i (p_ij - q_ij).
+// The entries at the ids stay out of the softmax sums: finalize adds them, in float64 and from the logits that
+// the log-probs take, so that with r the others' sum over the entry at o, l_i = -log1p(r) is never positive and
+// 1 - p_io = r / (1 + r) keeps its digits as p -> 1.  (Added in float32 from the product's own logit, the target's
+// share would differ from its log-prob's by 1e-6 to 1e-5, more than all the others of a peaked row.)
 //
 // Schedule:
 //   1. gather: the rows that take part, copied (zeros for the others: a NaN there must not reach a
 //      sum over rows), the logits at the ids, summed in float64, and from them the row's
 //      reference c, the nearest integer to the largest of them times s log2(e);
 //   2. product Z^T = W H^T; its epilogue writes E = 2^(s log2(e) z - c) in bf16 and, for each group
-//      of 64 vocabulary entries, the sum of the unrounded values;
-//   3. finalize: the sums merged into log sum exp, the objective's terms, the entries at the ids
-//      put into E (the preference loss takes three small steps more: sequences, pairs, rows);
+//      of 64 vocabulary entries, the sum of the unrounded values (zeros for the entries at the ids);
+//   3. finalize: the sums and the entries at the ids merged into log sum exp, the objective's terms, the
+//      entries at the ids put into E (the preference loss takes three small steps more: sequences, pairs, rows);
 //   4. products dH = f E W and dW = E^T (f H): a row's factor f = a 2^(c - lse log2(e)) goes into the
 //      epilogue of the first and into the copied hidden rows of the second.
 // The matrix-core work is that of the formulas, 6 N d V: no logit is computed twice, and between the
@@ -77,16 +81,29 @@ constexpr float kFar = 4294967296.f;   // largest sum of a group in its row's re
 struct EpiSoftmax {
   static constexpr bool kPair = false, kTile = true;
   uint16_t* e;       // [N][ld]
-  f32x2* part;       // [N][ld / 64]: reference, sum
+  f32x2* part;       // [N][ld / 64]: reference, sum (a wave that writes a group's has read its bits before)
   const float* c;    // [N]
+  const int32_t* id; // [N]: the row's only id, or NULL: a group's part holds the bits of its entries at ids
   int64_t ld;
   int V, N;
   Exponent exponent;
   struct Fetched {
     float c;
+    uint32_t at_ids;   // of the eight entries
   };
-  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t) const { return {n < N ? c[n] : 0.f}; }
-  __device__ __forceinline__ float values(float (&x)[8], const f32x4* v, int64_t m, float ref) const {
+  static __device__ __forceinline__ uint64_t bit_of(int32_t id, int64_t m) {   // of the group from entry m on
+    const uint32_t off = (uint32_t)(id - (int32_t)m);
+    return off < (uint32_t)kGroup ? uint64_t(1) << off : 0;
+  }
+  __device__ __forceinline__ uint64_t listed_at(int64_t n, int64_t m) const {   // of a group's 64 entries
+    return n < N && m < ld ? __builtin_bit_cast(uint64_t, part[n * (ld / kGroup) + m / kGroup]) : 0;
+  }
+  __device__ __forceinline__ Fetched fetch(int64_t n, int64_t m) const {
+    const int64_t from = m / kGroup * kGroup;
+    const uint64_t at = id == nullptr ? listed_at(n, from) : n < N ? bit_of(id[n], from) : 0;
+    return {n < N ? c[n] : 0.f, (uint32_t)(at >> (m - from)) & 255u};
+  }
+  __device__ __forceinline__ float values(float (&x)[8], const f32x4* v, int64_t m, float ref, uint32_t at_ids) const {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = exponent(v[k / 4][k % 4], ref);
@@ -94,19 +111,23 @@ struct EpiSoftmax {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] = m + k < V ? x[k] : 0.f;
     }
+    if (at_ids != 0) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = at_ids >> k & 1 ? 0.f : x[k];
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum += x[k];
     return sum_of_8_lanes(sum);
   }
   __device__ __forceinline__ void piece(int64_t n, int64_t m, const f32x4* v, const Fetched& row) const {
     float x[8], ref = row.c;
-    float sum = values(x, v, m, ref);
+    float sum = values(x, v, m, ref, row.at_ids);
     if (sum > kFar) {   // the same in the 8 lanes
       float top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < 8; ++k) top = fmaxf(top, m + k < V ? v[k / 4][k % 4] : -INFINITY);
       ref = rintf(max_of_8_lanes(top) * exponent.t);
-      sum = values(x, v, m, ref);
+      sum = values(x, v, m, ref, row.at_ids);
     }
     if (n >= N || m >= ld) return;
     put_bf16(e + n * ld + m, x);
@@ -119,10 +140,22 @@ struct EpiSoftmax {
     const int64_t n0 = (int64_t)(tn * 2 + wn) * BN * 16 + (lane & 15);
     const int m0 = (tm * 2 + wm) * BM * 16, g4 = (lane >> 4) * 4;
     float ref[BN];
+    int32_t only[BN];
+    uint64_t lists[BN][BM / 4] = {};
     repeat<BN>([&](auto jc) {
       constexpr int j = decltype(jc)::value;
-      ref[j] = n0 + j * 16 < N ? c[n0 + j * 16] : 0.f;
+      const int64_t n = n0 + j * 16;
+      ref[j] = n < N ? c[n] : 0.f;
+      only[j] = id != nullptr && n < N ? id[n] : -1;
     });
+    if (id == nullptr) {
+      repeat<BN>([&](auto jc) {
+        repeat<BM / 4>([&](auto gc) {
+          constexpr int j = decltype(jc)::value, g = decltype(gc)::value;
+          lists[j][g] = listed_at(n0 + j * 16, m0 + g * kGroup);
+        });
+      });
+    }
     repeat<BN>([&](auto jc) {
       constexpr int j = decltype(jc)::value;
       const int64_t n = n0 + j * 16;
@@ -130,28 +163,43 @@ struct EpiSoftmax {
         constexpr int i0 = decltype(gc)::value * 4;
         const int m = m0 + i0 * 16;
         float x[16];
-        auto values = [&](float from) {   // and the sum over the group
+        auto total = [&] {   // over the group
           float sum[4] = {};
+#pragma unroll
+          for (int q = 0; q < 16; ++q) sum[q % 4] += x[q];
+          return across_rows((sum[0] + sum[1]) + (sum[2] + sum[3]));
+        };
+        auto values = [&](float from) {
 #pragma unroll
           for (int q = 0; q < 16; ++q) x[q] = exponent(acc_read(acc[i0 + q / 4][j][q % 4]), from);
           if (m + kGroup > V) {   // the same in all lanes
 #pragma unroll
             for (int q = 0; q < 16; ++q) x[q] = m + q / 4 * 16 + g4 + q % 4 < V ? x[q] : 0.f;
           }
-#pragma unroll
-          for (int q = 0; q < 16; ++q) sum[q % 4] += x[q];
-          return across_rows((sum[0] + sum[1]) + (sum[2] + sum[3]));
+          return total();
         };
         float from = ref[j], sum = values(from);
-        if (__any(sum > kFar)) {
-          float top = -INFINITY;
+        const bool some = id == nullptr ? lists[j][i0 / 4] != 0 : (uint32_t)(only[j] - m) < (uint32_t)kGroup;
+        if (__any(some || sum > kFar)) {
+          const uint64_t at_ids = id == nullptr ? lists[j][i0 / 4] : bit_of(only[j], m);
+          const uint32_t low = (uint32_t)at_ids >> g4, high = (uint32_t)(at_ids >> 32) >> g4;
+          auto drop = [&] {   // the entries at ids
 #pragma unroll
-          for (int q = 0; q < 16; ++q)
-            top = fmaxf(top, m + q / 4 * 16 + g4 + q % 4 < V ? acc_read(acc[i0 + q / 4][j][q % 4]) : -INFINITY);
-          top = fmaxf(top, __shfl_xor(top, 16));
-          top = fmaxf(top, __shfl_xor(top, 32));
-          if (sum > kFar) from = rintf(top * exponent.t);
-          sum = values(from);
+            for (int q = 0; q < 16; ++q) x[q] = (q < 8 ? low : high) >> (q / 4 % 2 * 16 + q % 4) & 1 ? 0.f : x[q];
+            return total();
+          };
+          sum = drop();
+          if (__any(sum > kFar)) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+              top = fmaxf(top, m + q / 4 * 16 + g4 + q % 4 < V ? acc_read(acc[i0 + q / 4][j][q % 4]) : -INFINITY);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (sum > kFar) from = rintf(top * exponent.t);
+            values(from);
+            sum = drop();
+          }
         }
         const bool on = n < N && m < ld;
 #pragma unroll
@@ -229,21 +277,27 @@ __device__ __forceinline__ double block_total(double x, double* sh) {
   return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
-// (Reference, sum) of the groups of 2,048 logits of a row.  Grid (N, groups).
+// (Reference, sum) of the groups of 2,048 logits of a row, without those at its ids.  Grid (N, groups).
 __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict__ z, int64_t ld, int V,
+                                                         const int32_t* __restrict__ ids, int ids_of_row,
                                                          Exponent exponent, f32x2* __restrict__ part) {
   __shared__ Team<256> team;
   const int v0 = blockIdx.y * kFewGroup + threadIdx.x * 8;
   const float* row = z + (int64_t)blockIdx.x * ld;
+  uint32_t in = v0 + 8 <= V ? 255u : v0 < V ? (1u << (V - v0)) - 1u : 0u;
+  for (int j = 0; j < ids_of_row; ++j) {
+    const uint32_t off = (uint32_t)(ids[(int64_t)blockIdx.x * ids_of_row + j] - v0);
+    in &= off < 8u ? ~(1u << off) : 255u;
+  }
   float x[8], top = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    x[k] = v0 + k < V ? row[v0 + k] : -INFINITY;
+    x[k] = in >> k & 1 ? row[v0 + k] : -INFINITY;
     top = fmaxf(top, x[k]);
   }
   const float ref = rintf(team.max(top) * exponent.t);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sum += v0 + k < V ? exponent(x[k], ref) : 0.f;
+  for (int k = 0; k < 8; ++k) sum += in >> k & 1 ? exponent(x[k], ref) : 0.f;
   sum = (float)team.sum(sum);
   if (threadIdx.x == 0) part[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{ref, sum};
 }
@@ -251,6 +305,13 @@ __global__ __launch_bounds__(256) void few_groups_kernel(const float* __restrict
 constexpr int kRescaled = 2;   // of Rows::use
 
 // ---- what a call's kernels share ------------------------------------------------------
+// An id of a row (lane j has the j-th): its log-prob and probability, and the sum of all others' (1 - p,
+// without its cancellation).
+struct Listed {
+  int id;          // -1: none
+  bool first;      // the list has it at no place before
+  double lp, p, left;
+};
 struct Rows {
   int N, d, V, k;          // k ids a row
   int way, grads;          // kTiles, kFew or kOnePass; gradients wanted
@@ -291,6 +352,18 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
   if (t < r.k) {   // (finalize writes what becomes of them)
     const int64_t at = (int64_t)i * r.k + t;
     r.ids[at] = use == 1 ? op.id(i, t, r) : -1;
+  }
+  if (r.way == kTiles && r.k > 1) {   // the bits of each group's entries at ids, where its sum will stand
+    const int lane = t % 64, my = use == 1 && lane < r.k ? op.id(i, lane, r) : -1;
+    f32x2* bits = r.part + (int64_t)i * r.groups;
+    for (int g0 = t - lane; g0 < r.groups; g0 += kThreads) {
+      uint64_t mine = 0;
+      for (uint64_t here = __ballot(my >= 0 && my / (64 * kGroup) == g0 / 64); here != 0; here &= here - 1) {
+        const int id = __builtin_amdgcn_readlane(my, __builtin_ctzll(here));
+        if (id / kGroup == g0 + lane) mine |= uint64_t(1) << id % kGroup;
+      }
+      if (g0 + lane < r.groups) bits[g0 + lane] = __builtin_bit_cast(f32x2, mine);
+    }
   }
   const u32x4* from = reinterpret_cast<const u32x4*>(hidden + (int64_t)i * r.d);
   u32x4* to = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
@@ -347,8 +420,40 @@ __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
 }
 
 // ---- 3. finalize -----------------------------------------------------------------------
-// A team per row: log2 of the sum over its groups, in a fixed order (a row whose groups have
-// several references brought to the largest one); then op.row, called by the first wave, gives the
+__device__ __forceinline__ double lane_value(double x, int lane) {   // lane: the same in all lanes
+  const uint64_t v = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, lane), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// What a lane's value x leaves of the whole, `others` and the wave's sum of `once` (x, or 0 where another lane has
+// the same key): the whole less x, but where x is more than half of it (one key at most) the sum of all the rest.
+__device__ __forceinline__ double without(double x, double once, double others, int key, double& whole) {
+  whole = others + wave_sum(once);
+  double rest = whole - x;
+  const uint64_t most = __ballot(once > 0.5 * whole);
+  if (most != 0) {
+    const int at = __builtin_amdgcn_readlane(key, __builtin_ctzll(most));
+    const double all = others + wave_sum(key == at ? 0.0 : once);
+    if (key == at) rest = all;
+  }
+  return rest;
+}
+// Of a wave's lanes with the row's ids: own is an entry's 2^(z t - c), z its logit, others the sum over all
+// entries that stand at no id.  An id that a list has twice counts once.  lse2: log2 of the whole sum, and c.
+__device__ __forceinline__ Listed listed(int id, double own, double z, double others, float c, int lane, int k, double& lse2) {
+  Listed x{id, id >= 0, 0.0, 0.0, 0.0};
+  for (int j = 0; j < k; ++j) x.first = x.first && !(j < lane && __builtin_amdgcn_readlane(id, j) == id);
+  double total;
+  const double rest = without(own, x.first ? own : 0.0, others, id, total);
+  lse2 = (double)c + log2(total);
+  x.lp = own > rest ? -log1p(rest / own) : z - lse2 * 0.6931471805599453;
+  x.p = own / total;
+  x.left = rest / total;
+  return x;
+}
+
+// A team per row: log2 of the sum over its groups and the entries at its ids, in a fixed order (a row whose
+// groups have several references brought to the largest one); then op.row, called by the first wave, gives the
 // terms, the row's factor a of p and, in r.ids and r.g, the entries G / a at the ids.  E's own scale
 // is 2^(lse2 - c): the entries go in with it and the factor takes its inverse.  A row's gradient is
 // mostly that of its largest entry at an id, so this one is made exact: all entries there take the
@@ -365,7 +470,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
   float& factor = factors[threadIdx.x / kThreads];
   const int use = r.use[i];
   uint16_t* row = r.e + (int64_t)i * r.ld;
-  double lse2 = 0.0;
+  double others = 0.0;   // the sum without the entries at the row's ids, in units of 2^c
   float c = 0.f;
   if (use == 1) {
     const f32x2* part = r.part + (int64_t)i * r.groups;
@@ -381,7 +486,7 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
       far = far || p.x != c;
     }
     if (team.any(far)) {
-      top = team.max(top);
+      top = fmaxf(team.max(top), c);
       sum = 0.0;
       for (int g = t; g < r.groups; g += kThreads) {
         const f32x2 p = part[g];
@@ -399,12 +504,21 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
       c = top;
       if (t == 0) r.use[i] = kRescaled;
     }
-    lse2 = (double)c + log2(team.sum(sum));
+    others = team.sum(sum);
   }
-  if (r.way == kFew) c = (float)lse2;   // E is written from the logits, relative to the sum
   if (t < 64) {
-    const float a = op.row(i, t, use, lse2 * 0.6931471805599453, r);
-    const int64_t at = (int64_t)i * r.k + t;   // this lane wrote it in op.row
+    const int64_t at = (int64_t)i * r.k + t;   // this lane's, here and in op.row
+    double lse2 = 0.0;
+    Listed mine{-1, false, 0.0, 0.0, 0.0};
+    if (use == 1) {
+      const bool there = t < r.k && r.ids[at] >= 0;
+      const double z = there ? r.zs[at] * r.inv_t : 0.0;
+      double own = there ? exp2(z * 1.4426950408889634 - (double)c) : 0.0;
+      own = own < FLT_MIN ? 0.0 : own;   // as the other entries, which are float32
+      mine = listed(there ? r.ids[at] : -1, own, z, others, c, t, r.k, lse2);
+    }
+    if (r.way == kFew) c = (float)lse2;   // E is written from the logits, relative to the sum
+    const float a = op.row(i, t, use, lse2 * 0.6931471805599453, mine, r);
     const bool entry = use == 1 && t < r.k && r.ids[at] >= 0;
     const float e = entry ? (float)((double)r.g[at] * exp2(lse2 - (double)c)) : 0.f;
     const float most = wave_max(fabsf(e));
@@ -503,11 +617,11 @@ struct Policy {
     return -1;
   }
   __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
-  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Listed& mine, const Rows& r) const {
     if (lane != 0) return 0.f;
     double gain = 0.0, div = 0.0, clipped = 0.0, delta = 0.0, l = 0.0;
     if (use == 1) {
-      l = r.zs[i] * r.inv_t - lse;
+      l = mine.lp;
       const double c = (double)weight[i] * (double)scale, A = advantage[seq_id[i]];
       const double rho = exp(l - (double)logp_old[i]);
       const double lo = 1.0 - (double)eps_low, hi = 1.0 + (double)eps_high;
@@ -532,7 +646,7 @@ struct Policy {
     r.terms[2 * n + i] = clipped;
     r.terms[3 * n + i] = use == 1 ? 1.0 : 0.0;
     r.ids[i] = use == 1 ? target[i] : -1;
-    r.g[i] = use == 1 ? (float)expm1(l) : 0.f;
+    r.g[i] = use == 1 ? (float)-mine.left : 0.f;
     if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
     return (float)(-delta * r.inv_t);
   }
@@ -550,11 +664,11 @@ struct Preference {
   }
   __device__ __forceinline__ int id(int i, int, const Rows&) const { return target[i]; }
   // terms: the log-prob, the row's part of its sequence's log ratio, its weight
-  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Listed& mine, const Rows& r) const {
     if (lane != 0) return 0.f;
     double l = 0.0, part = 0.0, c = 0.0;
     if (use == 1) {
-      l = r.zs[i] * r.inv_t - lse;
+      l = mine.lp;
       c = weight != nullptr ? (double)weight[i] : 1.0;
       part = c * (logp_ref != nullptr ? l - (double)logp_ref[i] : l);
       if (!(std::isfinite(lse) && std::isfinite(part))) raise(r.err, PSPO_DEVERR_NONFINITE);
@@ -564,7 +678,7 @@ struct Preference {
     r.terms[n + i] = part;
     r.terms[2 * n + i] = c;
     r.ids[i] = use == 1 ? target[i] : -1;
-    r.g[i] = use == 1 ? (float)expm1(l) : 0.f;
+    r.g[i] = use == 1 ? (float)-mine.left : 0.f;
     if (logp_new != nullptr) logp_new[i] = use < 0 ? NAN : (float)l;
     return 1.f;   // pref_rows_kernel multiplies by what it is
   }
@@ -759,12 +873,10 @@ struct Distill {
     return entry(at) ? topk_ids[at] : -1;
   }
   // Lane j has the list's entry j.
-  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Rows& r) const {
+  __device__ __forceinline__ float row(int i, int lane, int use, double lse, const Listed& mine, const Rows& r) const {
     const int64_t at = (int64_t)i * r.k + lane;
-    const bool on = use == 1 && lane < r.k && entry(at);
-    const int my = on ? topk_ids[at] : -1;
+    const bool on = mine.id >= 0, first = mine.first;
     double div = 0.0, c = 0.0, g = 0.0;
-    bool first = on;
     if (use == 1) {
       const double x = on ? (double)topk[at] * r.inv_t : -INFINITY;
       double top = x;
@@ -775,25 +887,21 @@ struct Distill {
       }
       const double e = on ? exp(x - top) : 0.0;
       const double q = e / wave_sum(e);
-      double same = 0.0;   // the probability of this lane's id
+      double same = 0.0, all;   // the probability of this lane's id
       for (int j = 0; j < r.k; ++j) {
-        const int other = __shfl(my, j);
-        const double qj = __shfl(q, j);
-        if (on && other == my) {
-          same += qj;
-          first = first && j >= lane;
-        }
+        const double qj = lane_value(q, j);
+        same += __builtin_amdgcn_readlane(mine.id, j) == mine.id ? qj : 0.0;
       }
+      const double away = without(same, first ? same : 0.0, 0.0, mine.id, all);   // of the others
       c = (weight != nullptr ? (double)weight[i] : 1.0) * (double)scale;
-      const double lp = on ? r.zs[at] * r.inv_t - lse : 0.0;
-      const double each = first && !(same == 0.0) ? same * (log(same) - lp) : 0.0;
+      const double each = first && !(same == 0.0) ? same * ((same > 0.5 ? log1p(-away) : log(same)) - mine.lp) : 0.0;
       div = wave_sum(each);
-      g = exp(lp) - same;
+      g = mine.p > 0.5 ? away - mine.left : mine.p - same;   // (1 - q) - (1 - p) where p is near 1
       if (lane == 0 && !(std::isfinite(lse) && std::isfinite(c * div) && std::isfinite((float)(c * r.inv_t))))
         raise(r.err, PSPO_DEVERR_NONFINITE);
     }
     if (lane < r.k) {
-      r.ids[at] = first ? my : -1;
+      r.ids[at] = first ? mine.id : -1;
       r.g[at] = first ? (float)g : 0.f;
     }
     if (lane != 0) return 0.f;
@@ -835,8 +943,8 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
 // worked on), goes from there into the matrix instructions of the logits and into its own LDS; the
 // waves' sums are exchanged, every wave forms the block's 16 x 16 softmax entries, and reads its part
 // again, transposed, for their product with it, which stays in its accumulators: W is read once for
-// the logits and d_hidden.  Entries at the rows' ids count in the sums but not in the product (they
-// are added at the end with what becomes of them).  The entries of a block that pass 2^32 take their own
+// the logits and d_hidden.  Entries at the rows' ids are left out (they are added at the end, to the sums as
+// they are and to the product with what becomes of them).  The entries of a block that pass 2^32 take their own
 // reference, as in the tiles; their row's accumulators are then of no use (no other row's are touched),
 // and its d_hidden is formed from E (one_pass_hidden_kernel).  16 rows to a work-group, those of the others
 // in grid y, which meet W's blocks in the same L2 at about the same time (gridDim.x % 8 == 0 then).
@@ -923,10 +1031,14 @@ void one_pass_kernel(Rows r, const uint16_t* __restrict__ w, Exponent exponent, 
     auto values = [&] {
       sum = 0.f;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        y[q] = v0 + q < r.V ? exponent(z[q], from) : 0.f;
-        sum += y[q];
+      for (int q = 0; q < 4; ++q) y[q] = v0 + q < r.V ? exponent(z[q], from) : 0.f;
+      for (int j = 0; j < own; ++j) {
+        const int at = ids[j] - (v0 | p << 21);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = at == q ? 0.f : y[q];
       }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum += y[q];
       sum = across_rows(sum);
     };
     values();
@@ -938,11 +1050,6 @@ void one_pass_kernel(Rows r, const uint16_t* __restrict__ w, Exponent exponent, 
       top = fmaxf(top, __shfl_xor(top, 32));
       if (sum > kFar) from = rintf(top * exponent.t);
       values();
-    }
-    for (int j = 0; j < own; ++j) {
-      const int at = ids[j] - (v0 | p << 21);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) y[q] = at == q ? 0.f : y[q];
     }
     const u32x2 e = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
     if (wave == (b / (int)gridDim.x) % kPassWaves && p < n) {
@@ -1405,12 +1512,12 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
                            c.stream))
       return rc;
     hipLaunchKernelGGL(few_groups_kernel, dim3((unsigned)c.N, (unsigned)s.groups), dim3(256), 0, c.stream, z, s.ld,
-                       c.V, exponent_of(r), r.part);
+                       c.V, (const int32_t*)r.ids, c.k, exponent_of(r), r.part);
     PSPO_LAUNCHED("few_groups_kernel", c.stream);
   } else {
     const Plan p = plan_forward(c.V, c.N, c.d);
     if (int rc = product<false, false>(shape(c.w, c.w, c.d, c.V, r.copy, c.d, c.N, c.d), p, c.N,
-                                       EpiSoftmax{r.e, r.part, r.c, s.ld, c.V, c.N, exponent_of(r)}, slab,
+                                       EpiSoftmax{r.e, r.part, r.c, c.k == 1 ? r.ids : nullptr, s.ld, c.V, c.N, exponent_of(r)}, slab,
                                        "objective_logits", c.stream))
       return rc;
   }
