@@ -113,7 +113,8 @@ int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, con
  * A sequence may stand in any number of pairs.
  *
  *  cu_seqlens device, int32 [R + 1], non-decreasing: sequence r is rows cu[r] .. cu[r+1] - 1.
- *             Rows outside every sequence get zero gradient.  Offsets that decrease or lie
+ *             Rows outside every sequence get their log-prob and zero gradient, take no part
+ *             otherwise and may hold values that are not finite.  Offsets that decrease or lie
  *             outside [0, N] raise PSPO_DEVERR_SEQ_ID and are clamped to [0, N].
  *  chosen, rejected  device, int32 [P] in [0, R); a pair with an index outside raises
  *             PSPO_DEVERR_SEQ_ID and counts nothing (its margin is NaN).

@@ -670,8 +670,7 @@ struct Preference {
     if (use == 1) {
       l = mine.lp;
       c = weight != nullptr ? (double)weight[i] : 1.0;
-      part = c * (logp_ref != nullptr ? l - (double)logp_ref[i] : l);
-      if (!(std::isfinite(lse) && std::isfinite(part))) raise(r.err, PSPO_DEVERR_NONFINITE);
+      part = c * (logp_ref != nullptr ? l - (double)logp_ref[i] : l);   // its sequence looks whether it is finite
     }
     const int64_t n = r.N;
     r.terms[i] = l;
@@ -723,6 +722,7 @@ __global__ __launch_bounds__(256) void pref_sequences_kernel(Pairs q, int N, con
   for (int i = lo + threadIdx.x; i < hi; i += 256) {
     part += terms[(int64_t)N + i];
     c += terms[2 * (int64_t)N + i];
+    if (!std::isfinite(terms[(int64_t)N + i])) raise(q.err, PSPO_DEVERR_NONFINITE);
   }
   part = block_total(part, sh);
   c = block_total(c, sh);
@@ -799,6 +799,7 @@ __global__ __launch_bounds__(64 * kPrefWaves) void pref_all_kernel(Pairs q, int 
     for (int i = lo + lane; i < hi; i += 64) {
       part += terms[(int64_t)N + i];
       c += terms[2 * (int64_t)N + i];
+      if (!std::isfinite(terms[(int64_t)N + i])) raise(q.err, PSPO_DEVERR_NONFINITE);
     }
     sequence_ratio(q, r, wave_sum(part), wave_sum(c), lane == 0);
   }
@@ -822,7 +823,8 @@ __global__ __launch_bounds__(64 * kPrefWaves) void pref_all_kernel(Pairs q, int 
   *loss = x;
 }
 
-// The row's factor, from its sequence's; a team per row.
+// The row's factor, from its sequence's; a team per row.  A row that no sequence holds may hold anything: where
+// its entries are not finite they become zeros, which a factor of 0 makes of the others in d_w_head.
 template <int kThreads>
 __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
   const int i = Team<kThreads>::row();
@@ -833,7 +835,10 @@ __global__ __launch_bounds__(256) void pref_rows_kernel(Rows r, Pairs q) {
     if (q.cu[mid + 1] > i) e = mid;
     else s = mid + 1;
   }
-  const bool on = s < q.R && q.cu[s] <= i && r.use[i] > 0;
+  const bool held = s < q.R && q.cu[s] <= i, on = held && r.use[i] > 0;
+  if (!held && r.use[i] > 0 && r.way != kFew && !std::isfinite(r.terms[i]))   // (the entries of few rows are written later)
+    for (int64_t v0 = Team<kThreads>::thread() * 8; v0 < r.ld; v0 += kThreads * 8)
+      *reinterpret_cast<u32x4*>(r.e + (int64_t)i * r.ld + v0) = u32x4{0, 0, 0, 0};
   const double delta = on ? q.coef[s] * r.terms[2 * (int64_t)r.N + i] : 0.0;
   const float a = (float)(-delta * r.inv_t);
   const float f = on && a != 0.f ? a * r.f[i] : 0.f;
