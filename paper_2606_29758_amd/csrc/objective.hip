@@ -323,7 +323,6 @@ struct Rows {
   double* zs;              // [N][k] logits at the ids
   float* c;                // reference of the row
   f32x2* part;
-  double* lse2;            // log2 of the sum of 2^(z t)
   float* f;                // factor of E
   int32_t* ids;            // [N][k] places of the entries set apart (-1: none) and their values
   float* g;
@@ -386,7 +385,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
 #pragma unroll 8
       for (int p = t % kLanes; p < pieces; p += kLanes) {
         const u32x4 hv = from[p], wv = row[p];
-        float eight = 0.f;   // products are exact, their sums go on in float64: log-probs are summed over sequences
+        float eight = 0.f;   // of exact products, their sums go on in float64: log-probs are summed over sequences
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           eight = fmaf(__uint_as_float(hv[q] << 16), __uint_as_float(wv[q] << 16), eight);
@@ -526,7 +525,6 @@ __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
     const float carry = most >= FLT_MIN && std::isfinite(there) ? there / most : 1.f;
     if (entry) r.g[at] = e * carry;
     if (t == 0) {
-      r.lse2[i] = lse2;
       r.c[i] = c;
       // (an objective that knows a later on multiplies by it)
       factor = use == 1 && a != 0.f ? a * (float)exp2((double)c - lse2) / carry : 0.f;
@@ -1441,7 +1439,6 @@ Rows rows_of(const Call& c, const Layout& s) {
   r.zs = reinterpret_cast<double*>(ws + s.zs);
   r.c = reinterpret_cast<float*>(ws + s.c);
   r.part = reinterpret_cast<f32x2*>(ws + s.part);
-  r.lse2 = reinterpret_cast<double*>(ws + s.lse2);
   r.f = reinterpret_cast<float*>(ws + s.f);
   r.ids = reinterpret_cast<int32_t*>(ws + s.ids);
   r.g = reinterpret_cast<float*>(ws + s.g);

@@ -72,7 +72,7 @@ inline int64_t forward_reserve(int64_t V, int64_t N, int64_t d) {
 struct Layout {
   int64_t ld, groups;
   int group;
-  int64_t use, zs, c, part, lse2, f, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
+  int64_t use, zs, c, part, f, ids, g, terms, copy, e, z, slab, seqs, pairs, total;
 };
 // R, P: sequences and pairs of the preference loss.
 inline Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, int64_t P, bool grads) {
@@ -91,7 +91,6 @@ inline Layout layout_of(int64_t N, int64_t d, int64_t V, int64_t k, int64_t R, i
   s.zs = take(N * k * 8);
   s.c = take(N * 4);
   s.part = take(N * s.groups * 8);
-  s.lse2 = take(N * 8);
   s.f = take(N * 4);
   s.ids = take(N * k * 4);
   s.g = take(N * k * 4);

@@ -4,8 +4,8 @@ the stores, and the loads of what is added to, that run while the next tile's fi
 Every entry against the formulas in float64.  With B = 2^-8 for a rounding to bf16: a softmax entry takes one, its row's
 factor one, the scaled hidden row one; the errors of a logit and of the log of the sum, (d + 2) 2^-24 sum |w h| + 2^-18
 < 2^-8 each here, move p (and rho, which is 1 up to that) by less than three more; a float32 sum of n terms takes n 2^-24.
-A gradient is off by at most
-6 B + n 2^-24 (1.02 for the second order) of the sum of its terms' sizes, where an entry at an id of a list counts p + q.
+A gradient is off by at most 6 B + n 2^-24 (1.02 for the second order) of the sum of its terms' sizes, where an entry at
+an id of a list counts p + q.
 """
 import pytest
 import torch
