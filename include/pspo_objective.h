@@ -25,7 +25,8 @@
  * softmax entries (with the entries of G at the ids in their places) and, for d_w_head,
  * the hidden rows times their factors are rounded to bf16, the matrix cores' operand
  * type, once each (a row's largest entry at an id is kept exact); sums of the gradient
- * products are float32.
+ * products are float32.  For up to 48 rows of d <= 3584 and up to 64 of d <= 1536
+ * d_w_head takes the hidden rows as they are.
  *
  * Memory: the softmax entries of all N rows are kept in the workspace, 2 bytes each
  * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time.

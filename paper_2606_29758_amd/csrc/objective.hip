@@ -21,7 +21,8 @@
 //   3. finalize: the sums and the entries at the ids merged into log sum exp, the objective's terms, the
 //      entries at the ids put into E (the preference loss takes three small steps more: sequences, pairs, rows);
 //   4. products dH = f E W and dW = E^T (f H): a row's factor f = a 2^(c - lse log2(e)) goes into the
-//      epilogue of the first and into the copied hidden rows of the second.
+//      epilogue of the first and into the copied hidden rows of the second (of up to 64 rows, whose
+//      roundings average out in no sum, into E, in two bf16 parts).
 // The matrix-core work is that of the formulas, 6 N d V: no logit is computed twice, and between the
 // forward and the gradient products nothing passes over the N V entries (a conversion of them to G,
 // with a maximum of each group as reference, took 634 of 13,320 us at 4,999 rows, d = 3584,
@@ -403,10 +404,10 @@ __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16
   if (t == 0) r.c[i] = rintf(top * (float)(r.inv_t * 1.4426950408889634));
 }
 
-// The row's hidden entries times its factor, the second operand of dW.
+// The row's hidden entries times its factor, the second operand of dW in tiles.
 template <int kThreads>
 __device__ __forceinline__ void scale_copy(const Rows& r, int i, float f) {
-  if (r.way == kOnePass && r.N <= kPassRows) return;   // one_pass_head_kernel does
+  if (r.way == kOnePass) return;   // (its head kernels take the rows as they are)
   u32x4* row = reinterpret_cast<u32x4*>(r.copy + (int64_t)i * r.d);
 #pragma unroll 4
   for (int p = Team<kThreads>::thread(); p < r.d / 8; p += kThreads) {
@@ -1116,10 +1117,11 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
 }
 
-// dW = E^T (f H) of up to 16 rows: the rows times their factors in LDS, a wave 16 vocabulary entries at a
-// time, whose rows of dW it writes from end to end.  Up to 8 rows, whose roundings no others average,
-// stand there twice, rounded to bf16 and what that leaves.  Bound by dW's bytes: 16 rows,
-// d = 3584, V = 152064 222 us, 4.9 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
+// dW = (f E)^T H of up to 16 rows: the rows as they are in LDS, a wave 16 vocabulary entries at a time, whose
+// rows of dW it writes from end to end.  The roundings of so few rows average out in no sum, so f E goes in
+// rounded to bf16 and what that leaves, two matrix instructions on one operand of rows (f H rounded instead,
+// d_w_head of 16 rows, d = 3584, V = 152064, lists of 16 was 0.0024 off float64 in the relative 2-norm; now 0.0017).  Bound by dW's
+// bytes: 16 rows, d = 3584, V = 152064 222 us, 4.9 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
 // work-group sums the loss.
 template <int F>
 __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
@@ -1132,45 +1134,45 @@ __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, 
     return;
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane & 15, g = lane >> 4;
-  const int split = r.N <= kPassRows / 2 ? kPassRows / 2 : kPassRows;
   for (int t = threadIdx.x; t < kPassRows * 32 * F; t += 64 * kHeadWaves) {
-    const int place = t / (32 * F), i = place % split, col = t % (32 * F) * 8;
+    const int i = t / (32 * F), col = t % (32 * F) * 8;
     u32x4 x = {0, 0, 0, 0};
-    const float f = i < r.N ? r.f[i] : 0.f;
-    if (f != 0.f && col < r.d) {
-      x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float lo = f * __uint_as_float(x[q] << 16), hi = f * __uint_as_float(x[q] & 0xFFFF0000u);
-        x[q] = pack_bf16(lo, hi);
-        if (place >= split)
-          x[q] = pack_bf16(lo - __uint_as_float(x[q] << 16), hi - __uint_as_float(x[q] & 0xFFFF0000u));
-      }
-    }
-    *reinterpret_cast<u32x4*>(rows + place * kPitch + col * 2) = x;
+    if (i < r.N && col < r.d && r.f[i] != 0.f) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
+    *reinterpret_cast<u32x4*>(rows + i * kPitch + col * 2) = x;
   }
   __syncthreads();
   const int blocks = (r.V + 15) / 16, step = ((int)gridDim.x - 1) * kHeadWaves;
-  auto entries = [&](int b) {   // of vocabulary entry 16 b + p, places 4 g .. 4 g + 3
+  float f[4];   // of rows 4 g .. 4 g + 3
+#pragma unroll
+  for (int q = 0; q < 4; ++q) f[q] = g * 4 + q < r.N ? r.f[g * 4 + q] : 0.f;
+  auto entries = [&](int b) {   // of vocabulary entry 16 b + p and these rows
     s16x4 y = {0, 0, 0, 0};
     const int v = b * 16 + p;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int i = (g * 4 + q) % split;
-      if (i < r.N && v < r.V) y[q] = (short)r.e[(int64_t)i * r.ld + v];
-    }
+    for (int q = 0; q < 4; ++q)
+      if (f[q] != 0.f && v < r.V) y[q] = (short)r.e[(int64_t)(g * 4 + q) * r.ld + v];
     return y;
   };
   int b = blockIdx.x * kHeadWaves + wave;
   s16x4 next = b < blocks ? entries(b) : s16x4{0, 0, 0, 0};
   for (; b < blocks; b += step) {
-    const s16x4 y = next;
+    float y[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] = f[q] * __uint_as_float((uint32_t)(uint16_t)next[q] << 16);
     if (b + step < blocks) next = entries(b + step);
+    const u32x2 high = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) y[q] -= __uint_as_float(q % 2 ? high[q / 2] & 0xFFFF0000u : high[q / 2] << 16);
+    const s16x4 yh = __builtin_bit_cast(s16x4, high),
+                yl = __builtin_bit_cast(s16x4, u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
     const int v = b * 16 + p;
     for (int k = 0; k * 32 < r.d; ++k) {
       const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-      const f32x4 c0 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(transposed(rows, kPitch, 2 * k, lane), y, zero, 0, 0, 0);
-      const f32x4 c1 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(transposed(rows, kPitch, 2 * k + 1, lane), y, zero, 0, 0, 0);
+      const s16x4 h0 = transposed(rows, kPitch, 2 * k, lane), h1 = transposed(rows, kPitch, 2 * k + 1, lane);
+      f32x4 c0 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(h0, yl, zero, 0, 0, 0);
+      f32x4 c1 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(h1, yl, zero, 0, 0, 0);
+      c0 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(h0, yh, c0, 0, 0, 0);
+      c1 = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(h1, yh, c1, 0, 0, 0);
       if (f32) {
         const int col = k * 32 + g * 4;
         float* to = static_cast<float*>(out) + (int64_t)v * r.d + col;
@@ -1264,18 +1266,19 @@ struct EpiGrad {
   }
 };
 
-// dW = E^T (f H) of 17 to 64 rows, whose tiles would be all way in and out (one stage of K): a work-group
-// keeps 256 columns of the scaled rows in its registers, 64 to a wave as the matrix instructions take
-// them, and goes over its share of the vocabulary, 64 entries a step; their E comes through LDS, the
-// next step's on the way meanwhile.  KS: steps of 32 rows.  The last row of the grid sums the loss.
-// Whole calls against tiles: 24 rows, d = 3584, V = 152064 770 -> 719 us, 160, 46996 52 -> 47.  (From 65
+// dW = (f E)^T H of 17 to 64 rows, whose tiles would be all way in and out (one stage of K): a work-group
+// keeps 256 columns of the rows in its registers, 64 to a wave as the matrix instructions take them, and goes
+// over its share of the vocabulary, 64 entries a step; their f E comes through LDS, the next step's E on the way
+// meanwhile.  f E in two parts as above (24 rows, d = 1536, V = 21936, lists of 16: 0.0025 off float64 with f H
+// rounded, 0.0018 so; 24 rows, d = 3584, V = 152064 721 -> 728 us a call).  KS: steps of 32 rows.  The last row of
+// the grid sums the loss.  Whole calls against tiles: 24 rows of the same 770 / 728, 160, 46996 52 / 48.  (From 65
 // rows on both gradients' tiles in one launch are as good or better: 160 rows, d = 3584 1,106 / 1,183.)
 constexpr int kStreamPerCu = 2;
 template <int KS>
 __global__ __attribute__((amdgpu_flat_work_group_size(256, 256), amdgpu_waves_per_eu(kStreamPerCu, kStreamPerCu)))
 void stream_head_kernel(Rows r, EpiGrad out) {
   constexpr int kPitch = 64 * 2 + 16;   // odd in 16 bytes
-  __shared__ __attribute__((aligned(16))) unsigned char tile[2][KS * 32 * kPitch];
+  __shared__ __attribute__((aligned(16))) unsigned char tile[2][2 * KS * 32 * kPitch];   // f E, and what its rounding leaves
   __shared__ double sh[64];
   if (blockIdx.y == gridDim.y - 1) {
     if (blockIdx.x == 0) out.loss.run(sh);
@@ -1301,7 +1304,7 @@ void stream_head_kernel(Rows r, EpiGrad out) {
     for (int t = threadIdx.x; t < KS * 32 * 8; t += 256) {
       const int i = t / 8, col = (blockIdx.y * 4 + turn) * 64 + t % 8 * 8;
       u32x4 x = {0, 0, 0, 0};
-      if (i < r.N && col < r.d) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
+      if (i < r.N && col < r.d && r.f[i] != 0.f) x = *reinterpret_cast<const u32x4*>(r.copy + (int64_t)i * r.d + col);
       *reinterpret_cast<u32x4*>(tile[0] + i * kPitch + t % 8 * 16) = x;
     }
     __syncthreads();
@@ -1315,20 +1318,33 @@ void stream_head_kernel(Rows r, EpiGrad out) {
   }
   const int tiles = (r.V + 63) / 64, step = gridDim.x;
   u32x4 e[KS];   // this thread's pieces of the next tile
+  float f[KS];   // and their rows' factors
+#pragma unroll
+  for (int q = 0; q < KS; ++q) f[q] = q * 32 + (int)threadIdx.x / 8 < r.N ? r.f[q * 32 + threadIdx.x / 8] : 0.f;
   auto load = [&](int at) {
 #pragma unroll
     for (int q = 0; q < KS; ++q) {
       const int i = q * 32 + threadIdx.x / 8;
       e[q] = u32x4{0, 0, 0, 0};
-      if (i < r.N) e[q] = *reinterpret_cast<const u32x4*>(r.e + (int64_t)i * r.ld + at * 64 + threadIdx.x % 8 * 8);
+      if (f[q] != 0.f) e[q] = *reinterpret_cast<const u32x4*>(r.e + (int64_t)i * r.ld + at * 64 + threadIdx.x % 8 * 8);
     }
   };
   int buf = 0;
   if ((int)blockIdx.x < tiles) load(blockIdx.x);
   for (int at = blockIdx.x; at < tiles; at += step) {
 #pragma unroll
-    for (int q = 0; q < KS; ++q)
-      *reinterpret_cast<u32x4*>(tile[buf] + (q * 32 + threadIdx.x / 8) * kPitch + threadIdx.x % 8 * 16) = e[q];
+    for (int q = 0; q < KS; ++q) {
+      u32x4 high, low;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = f[q] * __uint_as_float(e[q][k] << 16), y = f[q] * __uint_as_float(e[q][k] & 0xFFFF0000u);
+        high[k] = pack_bf16(x, y);
+        low[k] = pack_bf16(x - __uint_as_float(high[k] << 16), y - __uint_as_float(high[k] & 0xFFFF0000u));
+      }
+      unsigned char* to = tile[buf] + (q * 32 + threadIdx.x / 8) * kPitch + threadIdx.x % 8 * 16;
+      *reinterpret_cast<u32x4*>(to) = high;
+      *reinterpret_cast<u32x4*>(to + KS * 32 * kPitch) = low;
+    }
     if (at + step < tiles) load(at + step);
     stage_barrier<63>();   // (the loads stay in flight; a wave writes this half again behind the next barrier)
     f32x4 acc[4][4];
@@ -1340,7 +1356,9 @@ void stream_head_kernel(Rows r, EpiGrad out) {
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const bf16x8 y = operand(tile[buf], ks, b);
+        const bf16x8 y = operand(tile[buf], ks, b), rest = operand(tile[buf], KS + ks, b);
+#pragma unroll
+        for (int a = 0; a < 4; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[ks][a], rest, acc[a][b], 0, 0, 0);
 #pragma unroll
         for (int a = 0; a < 4; ++a) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[ks][a], y, acc[a][b], 0, 0, 0);
       }
