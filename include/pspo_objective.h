@@ -29,7 +29,8 @@
  * d_w_head takes the hidden rows as they are.
  *
  * Memory: the softmax entries of all N rows are kept in the workspace, 2 bytes each
- * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time.
+ * (2.5 GB at 8,192 rows of V = 152064), instead of being computed a second time; a call
+ * of more than 64 rows without gradients writes and reserves them too.
  *
  * Every result is deterministic: the same arguments give the same bits.  The order of
  * a row's sums follows from N and from its place among the rows.
@@ -126,7 +127,8 @@ int pspo_policy_loss_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, con
  *  seq_ratio  device, float32 [R] out, or NULL: ratio_r.
  *  margin     device, float32 [P] out, or NULL: beta (ratio[chosen] - ratio[rejected]).
  *  Other arguments as above; flags also PSPO_PREF_AVERAGE.  P = 0 and R = 0 are valid;
- *  R <= 2^23 and R P <= 2^36 (PSPO_ERR_UNSUPPORTED beyond).
+ *  R <= 2^23 and R P <= 2^36 (PSPO_ERR_UNSUPPORTED beyond).  Every sequence looks at
+ *  every pair (10^5 of each: some 5 ms).
  */
 int pspo_preference_fwd_bwd(const uint16_t* hidden, const uint16_t* w_head, const int32_t* target,
                             const float* logp_ref, const float* weight, const int32_t* cu_seqlens,

@@ -340,7 +340,7 @@ __device__ __forceinline__ void raise(int32_t* err, int bit) {
 // A team per row; kLanes lanes take an id each in turn, whose row of W is read beside the hidden
 // row.  Op::use(i, lane, r): as Rows::use, the same in all lanes; Op::id(i, j, r): the row's
 // j-th id or -1.  Lists go 16 lanes to an id (2,501 rows of 50 ids, d = 520 25 us; 32 lanes 28, a wave
-// for four ids together 50), one to four ids a wave each.
+// for four ids together 50; 29 since the bits of the ids' places are written), one to four ids a wave each.
 template <int kThreads, int kLanes, class Op>
 __global__ __launch_bounds__(256) void gather_kernel(Rows r, Op op, const uint16_t* __restrict__ hidden,
                                                      const uint16_t* __restrict__ w) {
@@ -459,7 +459,7 @@ __device__ __forceinline__ Listed listed(int id, double own, double z, double ot
 // mostly that of its largest entry at an id, so this one is made exact: all entries there take the
 // factor that carries it to a value of bf16, and the row's factor its inverse.  (What this moves, the
 // softmax entries, by 2^-8 at most, is what their own rounding moves them by; d_w_head of 777 rows was
-// 0.0029 off float64 in the relative 2-norm without it, 0.0024 with it, 0.0017 of which is its own
+// 0.0029 off float64 in the relative 2-norm without it, 0.0023 with it, 0.0017 of which is its own
 // rounding to bf16.)  Below the normal numbers bf16 is too coarse for that, and no entry matters.
 template <int kThreads, class Op>
 __global__ __launch_bounds__(256) void finalize_kernel(Rows r, Op op) {
@@ -950,7 +950,8 @@ __global__ __launch_bounds__(256) void few_entries_kernel(Rows r, const float* _
 // the logits and d_hidden.  Entries at the rows' ids are left out (they are added at the end, to the sums as
 // they are and to the product with what becomes of them).  The entries of a block that pass 2^32 take their own
 // reference, as in the tiles; their row's accumulators are then of no use (no other row's are touched),
-// and its d_hidden is formed from E (one_pass_hidden_kernel).  16 rows to a work-group, those of the others
+// and its d_hidden is formed from E (one_pass_hidden_kernel; W read again by few work-groups: one such row costs
+// about 2 ms, 553 -> 2,580 us at 16 rows, d = 3584, V = 152064).  16 rows to a work-group, those of the others
 // in grid y, which meet W's blocks in the same L2 at about the same time (gridDim.x % 8 == 0 then).
 // Bound by W's bytes: 16 rows, d = 3584, V = 152064 292 us, 1 row, d = 1536, V = 151936 127, 3.7 TB/s
 // each (torch's sum over as many bytes reads 4.0).
@@ -1119,10 +1120,10 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void one_pass_hidden_kernel(
 
 // dW = (f E)^T H of up to 16 rows: the rows as they are in LDS, a wave 16 vocabulary entries at a time, whose
 // rows of dW it writes from end to end.  The roundings of so few rows average out in no sum, so f E goes in
-// rounded to bf16 and what that leaves, two matrix instructions on one operand of rows (f H rounded instead,
-// d_w_head of 16 rows, d = 3584, V = 152064, lists of 16 was 0.0024 off float64 in the relative 2-norm; now 0.0017).  Bound by dW's
-// bytes: 16 rows, d = 3584, V = 152064 222 us, 4.9 TB/s; 1 row, d = 1536, V = 151936 78, 6.0 TB/s.  The last
-// work-group sums the loss.
+// rounded to bf16 and what that leaves, two matrix instructions on one operand of rows (with f H rounded
+// instead d_w_head of 16 rows, d = 3584, V = 152064, lists of 16 was 0.0024 off float64 in the relative 2-norm,
+// so it is 0.0017).  Bound by dW's bytes: the same rows 214 us, 5.1 TB/s; 1 row, d = 1536, V = 151936 78,
+// 6.0 TB/s.  The last work-group sums the loss.
 template <int F>
 __global__ __launch_bounds__(64 * kHeadWaves) void one_pass_head_kernel(Rows r, void* out, int f32, int add,
                                                                         LossSum loss) {
@@ -1537,8 +1538,8 @@ int forward(const Call& c, const Layout& s, const Rows& r, const Op& op) {
   } else {
     const Plan p = plan_forward(c.V, c.N, c.d);
     if (int rc = product<false, false>(shape(c.w, c.w, c.d, c.V, r.copy, c.d, c.N, c.d), p, c.N,
-                                       EpiSoftmax{r.e, r.part, r.c, c.k == 1 ? r.ids : nullptr, s.ld, c.V, c.N, exponent_of(r)}, slab,
-                                       "objective_logits", c.stream))
+                                       EpiSoftmax{r.e, r.part, r.c, c.k == 1 ? r.ids : nullptr, s.ld, c.V, c.N, exponent_of(r)},
+                                       slab, "objective_logits", c.stream))
       return rc;
   }
   if (c.N < kTeamRows)
