@@ -205,7 +205,8 @@ def preference_loss(hidden, w_head, target, cu_seqlens, chosen, rejected, N: int
     u = ratio[chosen] - ratio[rejected];  loss = loss_scale times the sum over the pairs of
     -(1 - smoothing) log s(beta u) - smoothing log s(-beta u) ("sigmoid", s the logistic function) or
     (u - 1 / (2 beta))^2 ("squared").  cu_seqlens: int32 [R + 1]; chosen, rejected: int32 [P]; logp_ref (None:
-    zeros) and weight (None: ones): float32 [>=N]; the other arguments as in policy_loss.
+    zeros) and weight (None: ones): float32 [>=N]; the other arguments as in policy_loss.  Rows outside every
+    sequence get their log-prob and zero gradient, whatever they hold.
     Returns loss, d_hidden, d_w_head, logp_new [N], seq_ratio [R] and margin [P] (beta u).
     """
     N = _count(N)
